@@ -56,6 +56,11 @@ typedef enum {
 
 typedef enum { LASNET_F32 = 0, LASNET_BF16 = 1 } lasnet_dtype;
 
+/* 8-bit types of the row operators (see "Rows and experts"); no feature map has them.
+ * E4M3: 1 sign, 4 exponent, 3 fraction bits, bias 7, no infinity, 0x7f / 0xff = NaN, largest value 448.
+ * A scale of 8-bit rows is a byte b that stands for 2^(b - 127) (255: NaN). */
+enum { LASNET_E4M3 = 2 };
+
 /* Dense NHWC feature map in device memory: element (n,h,w,c) at ((n*H+h)*W+w)*C+c. */
 typedef struct {
   void* data;
@@ -282,6 +287,129 @@ LASNET_API int lasnet_dense_bottleneck(const lasnet_tensor* x, int M,
 /* Whether (dtype, C, M, S) has a matrix-core kernel (1) or only the generic one (0);
  * negative status if even the generic kernel cannot take it.  Host-only query. */
 LASNET_API int lasnet_has_fast_path(int dtype, int C, int M, int S);
+
+/*
+ * Rows and experts: the path above with a choice among several sets of weights.  A row (a token, or a pixel of a
+ * feature map: a dense NHWC map is N*H*W rows of C columns) is normalised, sent to k of E experts, multiplied by their weights
+ * and added back to the residual, weighted:
+ *
+ *   lasnet_norm_rows -> lasnet_route -> lasnet_dispatch_rows -> lasnet_expert_product ... -> lasnet_combine_rows
+ *
+ * as the masker's list, the gather, the convolutions and the scatter-add do for one set of weights.  As with that list,
+ * what was decided stays on the device: `offsets` and `position` are read there, and no call waits for a count.
+ *
+ * Rows: `rows` rows of `cols` columns; row i starts at data + i * stride elements (stride >= cols; 0 means cols).
+ * No alignment is required beyond that of the element; rows of which address, stride and width are whole multiples of 16 bytes run
+ * faster in the products.  rows may be 0 (data then may be NULL, and nothing is enqueued but what the other outputs
+ * need).  Limits: rows (and tokens * k) up to 2^30, cols up to 2^20 (norms: 16384), E up to 4096, k up to 64; beyond them
+ * LASNET_EUNSUPPORTED.
+ * An output must not overlap an input or another output, unless its description says so (the same address: LASNET_EALIAS; the
+ * rest is not checked).
+ * The entry points allocate nothing; what needs device memory beyond its arguments takes a workspace from the caller
+ * (256-byte aligned, LASNET_EINVAL if too small), owned by the call until its work on the stream has finished.  They can be
+ * stream-captured.  Results do not depend on what else runs: no sum is made by atomics.
+ */
+typedef struct {
+  void* data;
+  int64_t rows;
+  int64_t stride; /* elements from one row to the next; 0 = cols */
+  int32_t cols;
+  int32_t dtype; /* LASNET_F32, LASNET_BF16 or LASNET_E4M3 */
+} lasnet_rows;
+
+/*
+ * Root-mean-square norm of rows, with the residual's addition in front:
+ *   s = x + residual        sum_out = s, rounded to x's dtype (before the norm, which takes the unrounded s)
+ *   rstd = 1 / sqrt(mean_c s[c]^2 + eps)
+ *   out[c] = s[c] * rstd * weight[c]
+ * x: F32 or BF16.  residual, sum_out: NULL or of x's dtype and shape (residual NULL: s = x); sum_out may be the same rows as
+ * x or as residual.  weight: [cols] float.  rstd_out: NULL or [rows] float.  Sums in fp32; a row whose squares overflow fp32 comes out 0.
+ * out: x's dtype (may then be the same rows as x or residual, if sum_out is not), or E4M3 with scale [rows] bytes (else scale is
+ * NULL): the scale is the smallest power of two, at least 2^-126, with max_c |out[c]| <= 448 * scale (NaN elements aside), and
+ * the row holds out / scale, rounded to nearest even.  A power of two costs no precision: it moves the exponent alone.
+ */
+LASNET_API int lasnet_norm_rows(const lasnet_rows* x, const lasnet_rows* residual, const float* weight, float eps,
+                                const lasnet_rows* sum_out, const lasnet_rows* out, uint8_t* scale, float* rstd_out,
+                                void* hip_stream);
+
+/*
+ * Gradients of lasnet_norm_rows' out = s * rstd * weight, and of what else reads s:
+ *   dx = dsum + rstd * (h - s * rstd^2 * mean_c(h * s))      h = dy * weight
+ *   dweight[c] = sum_rows dy * s * rstd
+ * s: the rows as the forward call stored them (sum_out, or x without a residual); rstd: [rows] float, as it wrote them.
+ * dsum: NULL or the gradient that reaches s beside the norm.  dx (= that of x and of the residual) may be the same rows as dsum
+ * or dy.  dy, s, dsum, dx: one dtype (F32 or BF16) and shape.  dweight: [cols] float, written (not added to), summed in a
+ * fixed order.  workspace: lasnet_norm_rows_backward_workspace_bytes(rows, cols) bytes.
+ */
+LASNET_API size_t lasnet_norm_rows_backward_workspace_bytes(int64_t rows, int cols);
+LASNET_API int lasnet_norm_rows_backward(const lasnet_rows* dy, const lasnet_rows* s, const float* weight,
+                                         const float* rstd, const lasnet_rows* dsum, const lasnet_rows* dx,
+                                         float* dweight, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Slots sorted by expert.  Token t sends a row to expert experts[t*k + j] for each slot j < k; an entry outside [0, E)
+ * sends nothing (a slot beyond an expert's capacity, a token that is not routed).  A stable sort: the slots of an expert keep their order.
+ *   offsets  [E + 1]       the rows of expert e are offsets[e] .. offsets[e+1]; offsets[E] = number of slots sent
+ *   order    [tokens * k]  the slot (t*k + j) that row p comes from; -1 from offsets[E] on.  NULL: not written
+ *   position [tokens * k]  the row that slot t*k + j goes to; -1 where nothing is sent
+ * workspace: lasnet_route_workspace_bytes(tokens, k, E) bytes (0: NULL will do).
+ */
+LASNET_API size_t lasnet_route_workspace_bytes(int64_t tokens, int k, int E);
+LASNET_API int lasnet_route(const int32_t* experts, int64_t tokens, int k, int E, int32_t* offsets, int32_t* order,
+                            int32_t* position, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Rows laid out by expert: out[position[t*k + j]] = x[t].  x: tokens rows of any dtype; out: tokens * k rows of the same dtype and cols;
+ * rows from offsets[E] on, which no expert has, are set to zero.  scale, out_scale: both NULL, or the rows' scales in bytes, moved with them (127
+ * from offsets[E] on).  position: unique, as lasnet_route writes it (entries outside [0, tokens * k) send nothing).
+ * Its gradient is lasnet_combine_rows without weights.
+ */
+LASNET_API int lasnet_dispatch_rows(const lasnet_rows* x, const uint8_t* scale, const int32_t* position,
+                                    const int32_t* offsets, int k, int E, const lasnet_rows* out, uint8_t* out_scale,
+                                    void* hip_stream);
+
+/*
+ * ... and back, weighted, into the residual:  out[t] = base[t] + sum_j weights[t*k + j] * y[position[t*k + j]]
+ * over the slots that were sent, in the order of j, in fp32, rounded once.  y: tokens * k rows, F32 or BF16; out: tokens rows of the same
+ * dtype and cols; base: NULL (0), or as out, and may be the same rows as out.  weights: [tokens * k] float, NULL = 1.  A token that sent nothing
+ * gets base.  What y holds in rows that no slot points at is not read.
+ */
+LASNET_API int lasnet_combine_rows(const lasnet_rows* y, const float* weights, const int32_t* position, int k,
+                                   const lasnet_rows* base, const lasnet_rows* out, void* hip_stream);
+
+/*
+ * Gradients of lasnet_combine_rows (that of base is dout itself):
+ *   dy[position[t*k + j]] = weights[t*k + j] * dout[t]     rows from offsets[E] on are set to zero
+ *   dweights[t*k + j] = sum_c dout[t][c] * y[position[t*k + j]][c]      0 for a slot that was not sent
+ * dout: tokens rows; y, dy: tokens * k rows; one dtype (F32 or BF16) and cols.  dy may be the same rows as y.  weights: NULL = 1; dweights: NULL = not wanted.
+ */
+LASNET_API int lasnet_combine_rows_backward(const lasnet_rows* dout, const lasnet_rows* y, const float* weights,
+                                            const int32_t* position, const int32_t* offsets, int k, int E,
+                                            const lasnet_rows* dy, float* dweights, void* hip_stream);
+
+/*
+ * The experts' products: for every row p of expert e (offsets[e] <= p < offsets[e+1])
+ *   out[p][i] = sum_c x[p][c] * W[e][i][c]                          W: [E][out.cols][x.cols], dense, of x's dtype
+ * BF16: fp32 sums, rounded once.  E4M3: the matrix core's own sum (fp32 from instruction to instruction; within one, products are cut 2^-13
+ * below the largest of their group), then times 2^(scale[p] - 127) and wscale[e][i] in fp32, rounded once (scale: [x.rows] bytes, wscale:
+ * [E][out.cols] float; either NULL = 1; both NULL for BF16).  out: BF16, as many rows as x; rows from offsets[E] on are set to zero.
+ * flags: LASNET_POST_RELU (before the rounding).  offsets are taken as lasnet_route writes them: ascending, within
+ * [0, rows]; values beyond are cut to that, so no other memory is reached.  F32 has no such product (LASNET_EUNSUPPORTED).
+ */
+LASNET_API int lasnet_expert_product(const lasnet_rows* x, const uint8_t* scale, const int32_t* offsets, int E,
+                                     const void* W, const float* wscale, const lasnet_rows* out, uint32_t flags,
+                                     void* hip_stream);
+
+/*
+ * Their gradients, BF16 with fp32 sums:
+ *   dx[p][c]    = sum_i dy[p][i] * W[e][i][c]                        rows from offsets[E] on are set to zero
+ *   dW[e][i][c] = sum over the rows p of expert e of dy[p][i] * x[p][c]        zero for an expert without rows
+ * dW: [E][dy.cols][x.cols], dense, dw_dtype F32 or BF16; written, not added to.
+ */
+LASNET_API int lasnet_expert_product_dx(const lasnet_rows* dy, const int32_t* offsets, int E, const void* W,
+                                        const lasnet_rows* dx, void* hip_stream);
+LASNET_API int lasnet_expert_product_dw(const lasnet_rows* dy, const lasnet_rows* x, const int32_t* offsets, int E,
+                                        void* dW, int dw_dtype, void* hip_stream);
 
 /*
  * Microbenchmarks for the measurement harness (what this GPU sustains, beside the data-sheet peaks the

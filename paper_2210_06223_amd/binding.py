@@ -18,7 +18,7 @@ _LIB_PATH = os.environ.get("LASNET_LIBRARY") or os.path.join(
 _lib = None
 _marshal = None
 
-LASNET_F32, LASNET_BF16 = 0, 1
+LASNET_F32, LASNET_BF16, LASNET_E4M3 = 0, 1, 2
 LASNET_POST_RELU, LASNET_FORCE_GENERIC, LASNET_SKIP_IDENTITY, LASNET_FORCE_FUSED, LASNET_FORCE_TILED = 1, 2, 4, 8, 16
 LASNET_OK, LASNET_EINVAL, LASNET_ESHAPE, LASNET_EUNSUPPORTED, LASNET_EALIAS, LASNET_EHIP = 0, -1, -2, -3, -4, -5
 LASNET_ETOOBIG = -6
@@ -31,6 +31,9 @@ EXPORTS = (
     "lasnet_sparse_bottleneck_packed", "lasnet_sparse_bottleneck_noalloc",
     "lasnet_workspace_bytes", "lasnet_sparse_bottleneck_planned",
     "lasnet_microbench_mfma", "lasnet_microbench_copy", "lasnet_microbench_weight_stream",
+    "lasnet_norm_rows", "lasnet_norm_rows_backward", "lasnet_norm_rows_backward_workspace_bytes",
+    "lasnet_route", "lasnet_route_workspace_bytes", "lasnet_dispatch_rows", "lasnet_combine_rows",
+    "lasnet_combine_rows_backward", "lasnet_expert_product", "lasnet_expert_product_dx", "lasnet_expert_product_dw",
 )
 
 
@@ -44,6 +47,11 @@ class LasnetError(RuntimeError):
 class lasnet_tensor(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("n", ctypes.c_int32), ("h", ctypes.c_int32),
                 ("w", ctypes.c_int32), ("c", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class lasnet_rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("rows", ctypes.c_int64), ("stride", ctypes.c_int64),
+                ("cols", ctypes.c_int32), ("dtype", ctypes.c_int32)]
 
 
 def load_library(path: str) -> ctypes.CDLL:
@@ -94,6 +102,21 @@ def load_library(path: str) -> ctypes.CDLL:
     L.lasnet_sparse_bottleneck_packed.restype = ip
     L.lasnet_sparse_bottleneck_packed.argtypes = [tp, vp, vp, ip, ip, vp, vp, vp, vp, tp,
                                                   ctypes.c_uint32, vp]
+    rp, sz, i64 = ctypes.POINTER(lasnet_rows), ctypes.c_size_t, ctypes.c_int64
+    for name, result, args in (
+            ("norm_rows", ip, [rp, rp, vp, ctypes.c_float, rp, rp, vp, vp, vp]),
+            ("norm_rows_backward_workspace_bytes", sz, [i64, ip]),
+            ("norm_rows_backward", ip, [rp, rp, vp, vp, rp, rp, vp, vp, sz, vp]),
+            ("route_workspace_bytes", sz, [i64, ip, ip]),
+            ("route", ip, [vp, i64, ip, ip, vp, vp, vp, vp, sz, vp]),
+            ("dispatch_rows", ip, [rp, vp, vp, vp, ip, ip, rp, vp, vp]),
+            ("combine_rows", ip, [rp, vp, vp, ip, rp, rp, vp]),
+            ("combine_rows_backward", ip, [rp, rp, vp, vp, vp, ip, ip, rp, vp, vp]),
+            ("expert_product", ip, [rp, vp, vp, ip, vp, vp, rp, ctypes.c_uint32, vp]),
+            ("expert_product_dx", ip, [rp, vp, ip, vp, rp, vp]),
+            ("expert_product_dw", ip, [rp, rp, vp, ip, vp, ip, vp])):
+        f = getattr(L, "lasnet_" + name)
+        f.restype, f.argtypes = result, args
     # the entry points that _marshal calls, by address
     L.at_masker_ex, L.at_ex, L.at_dense, L.at_packed, L.at_planned, L.at_packed_bytes = (
         ctypes.cast(f, vp).value for f in (L.lasnet_masker_ex, L.lasnet_sparse_bottleneck_ex, L.lasnet_dense_bottleneck,
@@ -450,3 +473,236 @@ def lasnet_microbench_copy(src: torch.Tensor, dst: torch.Tensor, stream=None) ->
         raise ValueError("src and dst must have the same size")
     _check(lib().lasnet_microbench_copy(_ptr(src), _ptr(dst), nbytes, _stream(stream)), "lasnet_microbench_copy")
     return nbytes
+
+
+# ---- rows and experts ----
+# Rows are tensors of two dimensions whose rows are dense (their distance is free), or dense tensors of more, whose last dimension
+# is a row's: a feature map [N,H,W,C] is N*H*W rows.  8-bit rows are torch.float8_e4m3fn, their scales torch.float8_e8m0fnu (or uint8: the same
+# bytes).  A call without an output makes it.
+
+_ROW_DTYPES = {torch.float32: LASNET_F32, torch.bfloat16: LASNET_BF16, torch.float8_e4m3fn: LASNET_E4M3}
+_SCALE_DTYPES = (torch.float8_e8m0fnu, torch.uint8)
+
+
+def _rows(t: Optional[torch.Tensor], name: str) -> Optional[lasnet_rows]:
+    if t is None:
+        return None
+    dt = _ROW_DTYPES.get(t.dtype)
+    if dt is None:
+        raise ValueError("%s: rows are float32, bfloat16 or float8_e4m3fn" % name)
+    if not t.is_cuda:
+        raise ValueError("%s: rows live in device memory" % name)
+    shape = t.shape
+    if len(shape) < 2 or shape[-1] == 0:
+        raise ValueError("%s: rows are a tensor [..., cols] of at least two dimensions" % name)
+    cols = shape[-1]
+    n = t.numel() // cols
+    if n <= 1 or t.is_contiguous():
+        if n == 1 and cols > 1 and t.stride(-1) != 1:
+            raise ValueError("%s: the elements of a row must be contiguous" % name)
+        stride = cols
+    else:
+        if len(shape) != 2 or (cols > 1 and t.stride(1) != 1) or t.stride(0) < cols:
+            raise ValueError("%s: rows are dense, and apart from each other, in two dimensions; tensors of more are contiguous" % name)
+        stride = t.stride(0)
+    return lasnet_rows(t.data_ptr() or None, n, stride, cols, dt)
+
+
+def _ref(d: Optional[lasnet_rows]):
+    return None if d is None else ctypes.byref(d)
+
+
+def _dense(t: Optional[torch.Tensor], name: str, numel: int, *dtypes) -> Optional[int]:
+    """Address of a dense tensor of one of these types and this many elements (None: None)."""
+    if t is None:
+        return None
+    if t.dtype not in dtypes or t.numel() != numel or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError("%s must be a contiguous device tensor of %d elements of %s" % (name, numel, " or ".join(str(d) for d in dtypes)))
+    return t.data_ptr()
+
+
+def _workspace(t: Optional[torch.Tensor], need: int, device, stream):
+    """(address, bytes, tensor to keep until the call is enqueued).  What is made here belongs to the call's stream from then on."""
+    if t is None and need:
+        t = torch.empty(need, dtype=torch.uint8, device=device)
+        if stream is not None:
+            t.record_stream(stream)
+    return (None, 0, None) if t is None else (t.data_ptr(), t.numel() * t.element_size(), t)
+
+
+def lasnet_norm_rows(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: Optional[torch.Tensor] = None,
+                     out: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                     sum_out: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None,
+                     out_dtype: Optional[torch.dtype] = None, stream=None):
+    """(out, scale, sum_out): out = s / rms(s) * weight with s = x + residual.  out_dtype (where out is not given): x's, or
+    torch.float8_e4m3fn; scale: of 8-bit rows, else None.  sum_out = s, made where there is a residual.  rstd [rows] float32: written where given."""
+    d = _rows(x, "x")
+    if out is None:
+        out = torch.empty(x.shape, dtype=out_dtype or x.dtype, device=x.device)
+    elif out_dtype is not None and out.dtype != out_dtype:
+        raise ValueError("out has another type than out_dtype")
+    if scale is None and out.dtype == torch.float8_e4m3fn:
+        scale = torch.empty(d.rows, dtype=torch.float8_e8m0fnu, device=x.device)
+    if sum_out is None and residual is not None:
+        sum_out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    r, s, o = _rows(residual, "residual"), _rows(sum_out, "sum_out"), _rows(out, "out")
+    st = lib().lasnet_norm_rows(ctypes.byref(d), _ref(r), _dense(weight, "weight", d.cols, torch.float32), eps, _ref(s), ctypes.byref(o),
+                                _dense(scale, "scale", d.rows, *_SCALE_DTYPES), _dense(rstd, "rstd", d.rows, torch.float32), _stream(stream))
+    _check(st, "lasnet_norm_rows")
+    return out, scale, sum_out
+
+
+def lasnet_norm_rows_backward(dy: torch.Tensor, s: torch.Tensor, weight: torch.Tensor, rstd: torch.Tensor,
+                              dsum: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None,
+                              dweight: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """(dx, dweight) from the gradient dy of lasnet_norm_rows' out and dsum of its sum; s, rstd: as the forward call wrote them."""
+    y, d, g = _rows(dy, "dy"), _rows(s, "s"), _rows(dsum, "dsum")
+    if dx is None:
+        dx = torch.empty(s.shape, dtype=s.dtype, device=s.device)
+    if dweight is None:
+        dweight = torch.empty(d.cols, dtype=torch.float32, device=s.device)
+    o, L = _rows(dx, "dx"), lib()
+    at, size, keep = _workspace(workspace, L.lasnet_norm_rows_backward_workspace_bytes(d.rows, d.cols), s.device, stream)
+    st = L.lasnet_norm_rows_backward(ctypes.byref(y), ctypes.byref(d), _dense(weight, "weight", d.cols, torch.float32),
+                                     _dense(rstd, "rstd", d.rows, torch.float32), _ref(g), ctypes.byref(o),
+                                     _dense(dweight, "dweight", d.cols, torch.float32), at, size, _stream(stream))
+    _check(st, "lasnet_norm_rows_backward")
+    return dx, dweight
+
+
+def lasnet_route(experts: torch.Tensor, E: int, offsets: Optional[torch.Tensor] = None, order: Optional[torch.Tensor] = None,
+                 position: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """(offsets [E+1], order [tokens*k], position [tokens,k]), int32, of experts int32 [tokens,k] (outside [0,E): not sent)."""
+    if experts.dim() != 2 or experts.dtype != torch.int32 or not experts.is_cuda or not experts.is_contiguous():
+        raise ValueError("experts must be a contiguous int32 device tensor [tokens, k]")
+    tokens, k = experts.shape
+    if offsets is None:
+        offsets = torch.empty(E + 1, dtype=torch.int32, device=experts.device)
+    if order is None:
+        order = torch.empty(tokens * k, dtype=torch.int32, device=experts.device)
+    if position is None:
+        position = torch.empty((tokens, k), dtype=torch.int32, device=experts.device)
+    L = lib()
+    at, size, keep = _workspace(workspace, L.lasnet_route_workspace_bytes(tokens, k, E), experts.device, stream)
+    st = L.lasnet_route(_ptr(experts), tokens, k, E, _dense(offsets, "offsets", E + 1, torch.int32), _dense(order, "order", tokens * k, torch.int32),
+                        _dense(position, "position", tokens * k, torch.int32), at, size, _stream(stream))
+    _check(st, "lasnet_route")
+    return offsets, order, position
+
+
+def _slots(position: torch.Tensor):
+    if position.dim() != 2 or position.dtype != torch.int32 or not position.is_cuda or not position.is_contiguous():
+        raise ValueError("position must be a contiguous int32 device tensor [tokens, k]")
+    return position.shape
+
+
+def _offsets(offsets: torch.Tensor) -> int:
+    if offsets.dim() != 1 or offsets.numel() < 2 or offsets.dtype != torch.int32 or not offsets.is_cuda or not offsets.is_contiguous():
+        raise ValueError("offsets must be a contiguous int32 device tensor [E + 1]")
+    return offsets.numel() - 1
+
+
+def lasnet_dispatch_rows(x: torch.Tensor, position: torch.Tensor, offsets: torch.Tensor, scale: Optional[torch.Tensor] = None,
+                         out: Optional[torch.Tensor] = None, out_scale: Optional[torch.Tensor] = None, stream=None):
+    """(out [tokens*k, cols], out_scale): out[position[t, j]] = x[t], zeros where no expert has a row; the scales of 8-bit rows go along."""
+    tokens, k = _slots(position)
+    E, d = _offsets(offsets), _rows(x, "x")
+    if d.rows != tokens:
+        raise ValueError("x and position must have as many tokens")
+    if out is None:
+        out = torch.empty((tokens * k, d.cols), dtype=x.dtype, device=x.device)
+    if out_scale is None and scale is not None:
+        out_scale = torch.empty(tokens * k, dtype=scale.dtype, device=x.device)
+    o = _rows(out, "out")
+    st = lib().lasnet_dispatch_rows(ctypes.byref(d), _dense(scale, "scale", tokens, *_SCALE_DTYPES), _ptr(position), _ptr(offsets), k, E,
+                                    ctypes.byref(o), _dense(out_scale, "out_scale", tokens * k, *_SCALE_DTYPES), _stream(stream))
+    _check(st, "lasnet_dispatch_rows")
+    return out, out_scale
+
+
+def lasnet_combine_rows(y: torch.Tensor, position: torch.Tensor, weights: Optional[torch.Tensor] = None,
+                        base: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """out[t] = base[t] + sum_j weights[t, j] * y[position[t, j]] over the slots that were sent."""
+    tokens, k = _slots(position)
+    d, b = _rows(y, "y"), _rows(base, "base")
+    if out is None:
+        out = torch.empty((tokens, d.cols) if base is None else base.shape, dtype=y.dtype, device=y.device)
+    o = _rows(out, "out")
+    if o.rows != tokens:
+        raise ValueError("out and position must have as many tokens")
+    st = lib().lasnet_combine_rows(ctypes.byref(d), _dense(weights, "weights", tokens * k, torch.float32), _ptr(position), k, _ref(b),
+                                   ctypes.byref(o), _stream(stream))
+    _check(st, "lasnet_combine_rows")
+    return out
+
+
+def lasnet_combine_rows_backward(dout: torch.Tensor, y: torch.Tensor, position: torch.Tensor, offsets: torch.Tensor,
+                                 weights: Optional[torch.Tensor] = None, dy: Optional[torch.Tensor] = None,
+                                 dweights: Optional[torch.Tensor] = None, stream=None):
+    """(dy, dweights [tokens, k]) of lasnet_combine_rows; that of base is dout."""
+    tokens, k = _slots(position)
+    E, d, v = _offsets(offsets), _rows(dout, "dout"), _rows(y, "y")
+    if d.rows != tokens:
+        raise ValueError("dout and position must have as many tokens")
+    if dy is None:
+        dy = torch.empty(y.shape, dtype=y.dtype, device=y.device)
+    if dweights is None:
+        dweights = torch.empty((tokens, k), dtype=torch.float32, device=y.device)
+    o = _rows(dy, "dy")
+    st = lib().lasnet_combine_rows_backward(ctypes.byref(d), ctypes.byref(v), _dense(weights, "weights", tokens * k, torch.float32), _ptr(position),
+                                            _ptr(offsets), k, E, ctypes.byref(o), _dense(dweights, "dweights", tokens * k, torch.float32),
+                                            _stream(stream))
+    _check(st, "lasnet_combine_rows_backward")
+    return dy, dweights
+
+
+def _matrices(W: torch.Tensor, E: int, n: int, k: int, *dtypes) -> Optional[int]:
+    if tuple(W.shape) != (E, n, k):
+        raise ValueError("the experts' matrices are [%d, %d, %d], not %s" % (E, n, k, tuple(W.shape)))
+    return _dense(W, "the experts' matrices", E * n * k, *dtypes)
+
+
+def lasnet_expert_product(x: torch.Tensor, offsets: torch.Tensor, W: torch.Tensor, scale: Optional[torch.Tensor] = None,
+                          wscale: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, flags: int = 0, stream=None) -> torch.Tensor:
+    """out[p] = W[e] x[p] for the rows p of each expert e (W [E, n, cols]); bfloat16, or e4m3 with scale [rows], wscale [E, n]."""
+    E, d = _offsets(offsets), _rows(x, "x")
+    if W.dim() != 3:
+        raise ValueError("the experts' matrices are [E, n, cols]")
+    n = W.shape[1]
+    if out is None:
+        out = torch.empty((d.rows, n), dtype=torch.bfloat16, device=x.device)
+    o = _rows(out, "out")
+    if o.cols != n:
+        raise ValueError("out must have %d columns" % n)
+    st = lib().lasnet_expert_product(ctypes.byref(d), _dense(scale, "scale", d.rows, *_SCALE_DTYPES), _ptr(offsets), E,
+                                     _matrices(W, E, n, d.cols, x.dtype), _dense(wscale, "wscale", E * n, torch.float32), ctypes.byref(o),
+                                     flags, _stream(stream))
+    _check(st, "lasnet_expert_product")
+    return out
+
+
+def lasnet_expert_product_dx(dy: torch.Tensor, offsets: torch.Tensor, W: torch.Tensor, dx: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """dx[p] = W[e]^T dy[p]."""
+    E, d = _offsets(offsets), _rows(dy, "dy")
+    if W.dim() != 3:
+        raise ValueError("the experts' matrices are [E, n, cols]")
+    if dx is None:
+        dx = torch.empty((d.rows, W.shape[2]), dtype=dy.dtype, device=dy.device)
+    o = _rows(dx, "dx")
+    st = lib().lasnet_expert_product_dx(ctypes.byref(d), _ptr(offsets), E, _matrices(W, E, d.cols, o.cols, dy.dtype), ctypes.byref(o), _stream(stream))
+    _check(st, "lasnet_expert_product_dx")
+    return dx
+
+
+def lasnet_expert_product_dw(dy: torch.Tensor, x: torch.Tensor, offsets: torch.Tensor, dW: Optional[torch.Tensor] = None,
+                             dtype: Optional[torch.dtype] = None, stream=None) -> torch.Tensor:
+    """dW[e] = sum over the rows p of expert e of dy[p] x[p]^T; dW [E, n, cols] in bfloat16 (or dtype: float32)."""
+    E, d, v = _offsets(offsets), _rows(dy, "dy"), _rows(x, "x")
+    if dW is None:
+        dW = torch.empty((E, d.cols, v.cols), dtype=dtype or x.dtype, device=x.device)
+    elif dtype is not None and dW.dtype != dtype:
+        raise ValueError("dW has another type than dtype")
+    st = lib().lasnet_expert_product_dw(ctypes.byref(d), ctypes.byref(v), _ptr(offsets), E,
+                                        _matrices(dW, E, d.cols, v.cols, torch.bfloat16, torch.float32), _ROW_DTYPES[dW.dtype], _stream(stream))
+    _check(st, "lasnet_expert_product_dw")
+    return dW

@@ -18,7 +18,7 @@ CHECK_FLAGS = ("-DLASNET_DRAIN_AT_BARRIERS",)
 # The binding's native argument marshalling: host code against torch's headers, no HIP in it.
 MARSHAL = os.path.join(PKG, "_marshal.so")
 SOURCES = ["tiled_stages.hip", "mfma_stage3.hip", "mfma_stage2.hip", "mfma_stage1.hip", "mfma_stage4.hip",   # slowest first
-           "rows_generic.hip", "slab_stages.hip",
+           "rows_generic.hip", "slab_stages.hip", "expert_product.hip", "norm_rows.hip", "route_rows.hip", "row_api.hip",
            "api.hip", "masker.hip", "bottleneck_generic.hip", "bottleneck_mfma.hip", "microbench.hip"]
 
 FLAGS = [

@@ -8,6 +8,15 @@
 
 using namespace lasnet;
 
+bool lasnet::device_ok() {
+  int n = 0;
+  if (hipGetDeviceCount(&n) != hipSuccess || n <= 0) {
+    (void)hipGetLastError();
+    return false;
+  }
+  return true;
+}
+
 namespace {
 
 // Device memory the library owns: one buffer per (device, stream) for what a call needs beyond its arguments
@@ -90,15 +99,6 @@ void* scratch_for_current_device() {
     g_scratch_ptr[dev] = p;
   }
   return g_scratch_ptr[dev];
-}
-
-bool device_ok() {
-  int n = 0;
-  if (hipGetDeviceCount(&n) != hipSuccess || n <= 0) {
-    (void)hipGetLastError();
-    return false;
-  }
-  return true;
 }
 
 int check_tensor(const lasnet_tensor* t) {

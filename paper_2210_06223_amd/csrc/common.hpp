@@ -50,6 +50,8 @@ __device__ __forceinline__ bool unit_and_slice(int nunits, int nsl, int& unit, i
 }
 inline long long sliced_grid(long long nunits, int nsl) { return (nunits + 7) / 8 * 8 * nsl; }
 
+bool device_ok();                    // is there a device at all
+
 // ---- launchers (each returns a hipError_t from the launch, never synchronises) ----
 hipError_t launch_masker(const lasnet_tensor& x, const float* Wm, float bm, int S, float thr,
                          uint8_t* mask, int32_t* idx, int32_t* count, double* logits,

@@ -1,0 +1,321 @@
+// Root-mean-square norm of rows with the residual's addition, and its gradients.
+//
+//   s = x + r;  rstd = (mean s^2 + eps)^-1/2;  y = s rstd g;  in 8 bits q = e4m3(y / 2^e), 2^e least with max|y| <= 448 2^e
+//
+// Bound by memory: a row is read once into the registers of W waves (1, 4 or 16), N pieces of 16 bytes a lane, and everything follows from
+// there: the sum of squares and, for 8 bits, the maximum are two reductions over lanes.
+#include "row_ops.hpp"
+
+namespace lasnet {
+namespace {
+
+struct NormArgs {
+  RowsArg x, res, sum, out;
+  const float* weight;
+  uint8_t* scale;
+  float* rstd;
+  long long rows;
+  int cols;
+  float eps;
+};
+
+__device__ __forceinline__ void load_weights(const float* w, int n, float* f, int per) {
+#pragma unroll
+  for (int i = 0; i < 8; i += 4) {
+    if (i >= per) break;
+    const uint4_t v = load_piece<float>((const unsigned char*)(w + i), n - i);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[i + j] = __uint_as_float(v[j]);
+  }
+}
+
+// Exponent field (127 + e) of the row's scale 2^e: a = M 2^E with 1 <= M < 2 needs e = E - 8 up to M = 1.75 (448 = 1.75 2^8), else E - 7.
+__device__ __forceinline__ int scale_byte(float a) {
+  const unsigned u = __float_as_uint(a);
+  const int e = (int)(u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u);
+  return e < 1 ? 1 : e;
+}
+
+// T: the rows' type; E4M3: out has 8 bits.
+template <class T, bool E4M3, int W, int N>
+__global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void norm_rows_kernel(NormArgs a) {
+  using E = Elem<T>;
+  constexpr int ROWS = W < 4 ? 4 / W : 1;                     // rows of a workgroup
+  __shared__ float join[2][W < 4 ? 4 : W];
+  const int tid = (int)threadIdx.x, lane = tid % (64 * W);
+  const long long row = (long long)blockIdx.x * ROWS + tid / (64 * W);
+  if (W == 1 && row >= a.rows) return;                        // (W > 1: a workgroup has one row, and there are as many)
+  const unsigned char* x = a.x.data + row * a.x.pitch;
+  float s[N][E::PER], g[N][E::PER], ss = 0.f;
+  uint4_t px[N], pr[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int c = (i * 64 * W + lane) * E::PER;
+    px[i] = load_piece<T>(x + (size_t)c * E::BYTES, a.cols - c);
+  }
+  if (a.res.data) {
+    const unsigned char* r = a.res.data + row * a.res.pitch;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int c = (i * 64 * W + lane) * E::PER;
+      pr[i] = load_piece<T>(r + (size_t)c * E::BYTES, a.cols - c);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int c = (i * 64 * W + lane) * E::PER;
+    load_weights(a.weight + c, a.cols - c, g[i], E::PER);
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    E::widen(px[i], s[i]);
+    if (a.res.data) {
+      float r[E::PER];
+      E::widen(pr[i], r);
+#pragma unroll
+      for (int j = 0; j < E::PER; ++j) s[i][j] += r[j];
+    }
+#pragma unroll
+    for (int j = 0; j < E::PER; ++j) ss += s[i][j] * s[i][j];
+  }
+  ss = row_join<W, false>(ss, join[0]);
+  const float rstd = 1.0f / sqrtf(ss / (float)a.cols + a.eps);
+  if (a.sum.data) {
+    unsigned char* o = a.sum.data + row * a.sum.pitch;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int c = (i * 64 * W + lane) * E::PER;
+      if (c < a.cols) store_piece<T>(o + (size_t)c * E::BYTES, a.cols - c, E::narrow(s[i]));
+    }
+  }
+  if (a.rstd && lane == 0) a.rstd[row] = rstd;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int j = 0; j < E::PER; ++j) s[i][j] *= rstd * g[i][j];
+  unsigned char* o = a.out.data + row * a.out.pitch;
+  if constexpr (!E4M3) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int c = (i * 64 * W + lane) * E::PER;
+      if (c < a.cols) store_piece<T>(o + (size_t)c * E::BYTES, a.cols - c, E::narrow(s[i]));
+    }
+  } else {
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int j = 0; j < E::PER; ++j) top = fmaxf(top, fabsf(s[i][j]));
+    top = row_join<W, true>(top, join[1]);
+    const int byte = scale_byte(top);
+    const float up = __uint_as_float((unsigned)(254 - byte) << 23);            // 2^-e, exact
+    if (lane == 0) a.scale[row] = (uint8_t)byte;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int c = (i * 64 * W + lane) * E::PER;
+      unsigned q[E::PER / 4];
+#pragma unroll
+      for (int j = 0; j < E::PER / 4; ++j) {
+        int v = __builtin_amdgcn_cvt_pk_fp8_f32(s[i][4 * j] * up, s[i][4 * j + 1] * up, 0, false);
+        q[j] = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(s[i][4 * j + 2] * up, s[i][4 * j + 3] * up, v, true);
+      }
+      const int n = a.cols - c;
+      if (n >= E::PER) {
+        if constexpr (E::PER == 8) {
+          typedef unsigned uint2_any __attribute__((ext_vector_type(2), aligned(1)));
+          *(uint2_any*)(o + c) = uint2_any{q[0], q[1]};
+        } else {
+          typedef unsigned uint_any __attribute__((aligned(1)));
+          *(uint_any*)(o + c) = q[0];
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < E::PER; ++j)
+          if (j < n) o[c + j] = (uint8_t)(q[j / 4] >> (8 * (j % 4)));
+      }
+    }
+  }
+}
+
+template <class T, bool E4M3, int W, int N>
+hipError_t go(const NormArgs& a, hipStream_t st) {
+  constexpr int ROWS = W < 4 ? 4 / W : 1, THREADS = W < 4 ? 256 : 64 * W;
+  constexpr long long most = (1ll << 31) / THREADS * ROWS;      // rows of a launch: one of 2^32 threads is an error
+  for (long long done = 0; done < a.rows; done += most) {
+    NormArgs b = a;
+    b.rows = a.rows - done < most ? a.rows - done : most;
+    for (RowsArg* r : {&b.x, &b.res, &b.sum, &b.out})
+      if (r->data) r->data += done * r->pitch;
+    if (b.scale) b.scale += done;
+    if (b.rstd) b.rstd += done;
+    norm_rows_kernel<T, E4M3, W, N><<<dim3((unsigned)((b.rows + ROWS - 1) / ROWS)), dim3(THREADS), 0, st>>>(b);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+template <class T, bool E4M3>
+hipError_t pick(const NormArgs& a, hipStream_t st) {
+  const int pieces = (a.cols + Elem<T>::PER - 1) / Elem<T>::PER;
+  if (pieces <= 64) return go<T, E4M3, 1, 1>(a, st);
+  if (pieces <= 128) return go<T, E4M3, 1, 2>(a, st);
+  if (pieces <= 256) return go<T, E4M3, 4, 1>(a, st);
+  if (pieces <= 512) return go<T, E4M3, 4, 2>(a, st);
+  if (pieces <= 1024) return go<T, E4M3, 4, 4>(a, st);
+  return go<T, E4M3, 16, kNormCols / 1024 / Elem<T>::PER>(a, st);
+}
+
+// ---- the gradients ----
+struct NormGradArgs {
+  RowsArg dy, s, dsum, dx;
+  const float* weight;
+  const float* rstd;
+  float* part;                     // [workgroups][cols]
+  long long rows;
+  int cols;
+};
+
+// A workgroup takes the rows blockIdx.x, blockIdx.x + gridDim.x, ... (times ROWS) and keeps its columns' sums of dy s rstd in registers.
+template <class T, int W, int N>
+__global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void norm_grad_kernel(NormGradArgs a) {
+  using E = Elem<T>;
+  constexpr int ROWS = W < 4 ? 4 / W : 1;
+  __shared__ float join[2][W < 4 ? 4 : W];
+  const int tid = (int)threadIdx.x, lane = tid % (64 * W), sub = tid / (64 * W);
+  float dg[N][E::PER] = {};
+  int turn = 0;
+  for (long long row = (long long)blockIdx.x * ROWS + sub; row < a.rows; row += (long long)gridDim.x * ROWS, turn ^= 1) {
+    const float rstd = a.rstd[row];
+    uint4_t py[N], ps[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int c = (i * 64 * W + lane) * E::PER;
+      py[i] = load_piece<T>(a.dy.data + row * a.dy.pitch + (size_t)c * E::BYTES, a.cols - c);
+      ps[i] = load_piece<T>(a.s.data + row * a.s.pitch + (size_t)c * E::BYTES, a.cols - c);
+    }
+    float dot = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int c = (i * 64 * W + lane) * E::PER;
+      float y[E::PER], s[E::PER], g[E::PER];
+      E::widen(py[i], y);
+      E::widen(ps[i], s);
+      load_weights(a.weight + c, a.cols - c, g, E::PER);
+#pragma unroll
+      for (int j = 0; j < E::PER; ++j) {
+        dg[i][j] += y[j] * (s[j] * rstd);
+        dot += y[j] * g[j] * s[j];
+      }
+    }
+    dot = row_join<W, false>(dot, join[turn]);
+    const float pull = dot / (float)a.cols * rstd * rstd;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int c = (i * 64 * W + lane) * E::PER;
+      if (c >= a.cols) continue;
+      float y[E::PER], s[E::PER], g[E::PER], d[E::PER] = {};
+      E::widen(py[i], y);
+      E::widen(ps[i], s);
+      load_weights(a.weight + c, a.cols - c, g, E::PER);
+      if (a.dsum.data) E::widen(load_piece<T>(a.dsum.data + row * a.dsum.pitch + (size_t)c * E::BYTES, a.cols - c), d);
+#pragma unroll
+      for (int j = 0; j < E::PER; ++j) d[j] += rstd * (y[j] * g[j] - s[j] * pull);
+      store_piece<T>(a.dx.data + row * a.dx.pitch + (size_t)c * E::BYTES, a.cols - c, E::narrow(d));
+    }
+  }
+  // the ROWS rows' sums of a column are added in order
+  if constexpr (ROWS > 1) {
+    __shared__ float rest[(ROWS - 1) * 64 * W * E::PER];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      __syncthreads();
+      if (sub)
+#pragma unroll
+        for (int j = 0; j < E::PER; ++j) rest[((sub - 1) * E::PER + j) * 64 * W + lane] = dg[i][j];
+      __syncthreads();
+      if (!sub)
+#pragma unroll
+        for (int j = 0; j < E::PER; ++j)
+#pragma unroll
+          for (int r = 0; r < ROWS - 1; ++r) dg[i][j] += rest[(r * E::PER + j) * 64 * W + lane];
+    }
+    if (sub) return;
+  }
+  float* part = a.part + (size_t)blockIdx.x * a.cols;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int c = (i * 64 * W + lane) * E::PER;
+#pragma unroll
+    for (int j = 0; j < E::PER; ++j)
+      if (c + j < a.cols) part[c + j] = dg[i][j];
+  }
+}
+
+// dweight[c] = sum of the workgroups' parts, 16 waves a column block of 64, each its share of the workgroups in order.
+__global__ __launch_bounds__(1024) void norm_grad_join_kernel(const float* part, int groups, int cols, float* dweight) {
+  __shared__ float sum[16][64];
+  const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
+  const int c = (int)blockIdx.x * 64 + lane;
+  float v = 0.f;
+  if (c < cols)
+    for (int b = wave; b < groups; b += 16) v += part[(size_t)b * cols + c];
+  sum[wave][lane] = v;
+  __syncthreads();
+  if (wave || c >= cols) return;
+#pragma unroll
+  for (int i = 1; i < 16; ++i) v += sum[i][lane];
+  dweight[c] = v;
+}
+
+// Workgroups of the backward pass: as many as the chip runs at once, so that the parts stay few.
+int grad_groups(long long rows, int cols) {
+  const long long most = 1024;
+  const long long need = cols <= 1024 ? (rows + 3) / 4 : rows;
+  return (int)(need < most ? need : most);
+}
+
+template <class T, int W, int N>
+hipError_t go_grad(const NormGradArgs& a, int groups, float* dweight, hipStream_t st) {
+  norm_grad_kernel<T, W, N><<<dim3((unsigned)groups), dim3(W < 4 ? 256 : 64 * W), 0, st>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  norm_grad_join_kernel<<<dim3((unsigned)((a.cols + 63) / 64)), dim3(1024), 0, st>>>(a.part, groups, a.cols, dweight);
+  return hipGetLastError();
+}
+
+template <class T>
+hipError_t pick_grad(const NormGradArgs& a, int groups, float* dweight, hipStream_t st) {
+  const int pieces = (a.cols + Elem<T>::PER - 1) / Elem<T>::PER;
+  if (pieces <= 64) return go_grad<T, 1, 1>(a, groups, dweight, st);
+  if (pieces <= 128) return go_grad<T, 1, 2>(a, groups, dweight, st);
+  if (pieces <= 256) return go_grad<T, 4, 1>(a, groups, dweight, st);
+  if (pieces <= 512) return go_grad<T, 4, 2>(a, groups, dweight, st);
+  if (pieces <= 1024) return go_grad<T, 4, 4>(a, groups, dweight, st);
+  return go_grad<T, 16, kNormCols / 1024 / Elem<T>::PER>(a, groups, dweight, st);
+}
+
+}  // namespace
+
+hipError_t launch_norm_rows(int dtype, int out_dtype, long long rows, int cols, RowsArg x, RowsArg residual, const float* weight, float eps,
+                            RowsArg sum, RowsArg out, uint8_t* scale, float* rstd, hipStream_t st) {
+  const NormArgs a{x, residual, sum, out, weight, scale, rstd, rows, cols, eps};
+  const bool q = out_dtype == LASNET_E4M3;
+  if (dtype == LASNET_F32) return q ? pick<float, true>(a, st) : pick<float, false>(a, st);
+  return q ? pick<__bf16, true>(a, st) : pick<__bf16, false>(a, st);
+}
+
+size_t norm_backward_workspace_bytes(long long rows, int cols) { return (size_t)grad_groups(rows, cols) * cols * sizeof(float); }
+
+hipError_t launch_norm_rows_backward(int dtype, long long rows, int cols, RowsArg dy, RowsArg s, const float* weight, const float* rstd,
+                                     RowsArg dsum, RowsArg dx, float* dweight, void* workspace, hipStream_t st) {
+  const NormGradArgs a{dy, s, dsum, dx, weight, rstd, (float*)workspace, rows, cols};
+  const int groups = grad_groups(rows, cols);
+  if (rows == 0) {                                             // no rows, no parts: dweight = 0
+    norm_grad_join_kernel<<<dim3((unsigned)((cols + 63) / 64)), dim3(1024), 0, st>>>(nullptr, 0, cols, dweight);
+    return hipGetLastError();
+  }
+  return dtype == LASNET_F32 ? pick_grad<float>(a, groups, dweight, st) : pick_grad<__bf16>(a, groups, dweight, st);
+}
+
+}  // namespace lasnet
