@@ -8,6 +8,8 @@
 // consecutive i in a lane.  An operand is held by ROWS (k is contiguous in memory: x, dy, and W in the forward product) or by COLUMNS (i or j
 // is: W for dx, both for dW).  In LDS a tile by rows lies as it is read, 128 bytes of k a row; one by columns lies as it is in memory, and
 // the transposing LDS read (ds_read_b64_tr_b16: 4 k x 16 columns for 16 lanes) turns it.
+#include <type_traits>
+
 #include "row_ops.hpp"
 
 namespace lasnet {
@@ -120,6 +122,52 @@ __device__ __forceinline__ uint4_t load_some(const unsigned char* p, int n) {
   return v;
 }
 
+// The wave's NI x NJ blocks of 16 x 16, from column oi0 and row oj0 of the output on, scaled, rounded and stored.
+template <bool FP8, bool F32OUT, int NI, int NJ>
+__device__ __forceinline__ void store_tile(const ProductArgs& a, unsigned char* out, int expert, int oi0, int oj0, int j_end,
+                                           const floatx4 (&acc)[NI][NJ]) {
+  const int lane = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));      // (made anew: no register holds it through the loop)
+  const float floor = a.relu ? 0.f : -INFINITY;               // (NaN passes)
+  float up[NJ];
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    up[j] = 1.0f;
+    if constexpr (FP8) {
+      const int oj = oj0 + 16 * j + (lane & 15);
+      if (a.scale && expert < a.E && oj < j_end) up[j] = scale_value(a.scale[oj]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const int oi = oi0 + 16 * i + (lane >> 4) * 4;
+    float w[4] = {1.0f, 1.0f, 1.0f, 1.0f};
+    if constexpr (FP8)
+      if (a.wscale && expert < a.E) Elem<float>::widen(load_piece<float>((const unsigned char*)(a.wscale + (size_t)expert * a.ni + oi), a.ni - oi), w);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const int oj = oj0 + 16 * j + (lane & 15);
+      if (oj >= j_end) continue;
+      float v[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        v[r] = acc[i][j][r];
+        if constexpr (FP8) v[r] *= w[r] * up[j];
+        v[r] = v[r] < floor ? floor : v[r];
+      }
+      unsigned char* o = out + (long long)oj * a.out.pitch + (long long)oi * (F32OUT ? 4 : 2);
+      if constexpr (F32OUT) {
+        store_piece<float>(o, a.ni - oi, Elem<float>::narrow(v));
+      } else if (oi + 4 <= a.ni) {
+        *(uint2_any*)o = uint2_t{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
+      } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (oi + r < a.ni) Elem<__bf16>::put(o + 2 * r, bf16_pair(v[r], 0.f));
+      }
+    }
+  }
+}
+
 // 128 x 128 of the output by 4 waves, 64 x 64 each; rows and weights through registers into two LDS stages.
 // FP8: e4m3, else bf16.  IC, JC: held by columns.  RAGGED: the reduction runs over an expert's rows (dW).
 template <bool FP8, bool IC, bool JC, bool RAGGED, bool F32OUT>
@@ -221,42 +269,714 @@ __global__ __launch_bounds__(256) void product_kernel(ProductArgs a) {
   }
 
   unsigned char* out = a.out.data + (RAGGED ? (long long)expert * a.out_expert : 0);
+  store_tile<FP8, F32OUT>(a, out, expert, i0 + wi, j0 + wj, j_end, acc);
+}
+
+// ---- whole pieces: rows, widths and addresses that are multiples of 16 bytes ----
+// BI x BJ of the output by WI x WJ waves; tiles go from memory to LDS without passing registers, two stages.
+//
+// A stage is 128 bytes of k of both tiles.  A wave holds the fragments of its J blocks for the whole stage and walks its I blocks with a ring of
+// four fragments, each read three blocks ahead, over the end of the stage too: after the block third from last every read of the stage
+// has been answered, so one barrier there frees the stage for the loads of the one after next and opens the next, whose first
+// fragments are read while the last two blocks' MFMAs run.  The MFMAs of a block (NJ, or 2 NJ in bf16) are independent of each other.
+typedef __attribute__((address_space(3))) unsigned char lds_byte;
+
+__device__ __forceinline__ void load_to_lds(const unsigned char* base, unsigned off, unsigned to) {     // 64 x 16 bytes to 1 KiB
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(to) : "memory");
+}
+// Every load of the wave has landed and every read has been answered; then all waves' have.
+__device__ __forceinline__ void stage_barrier() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+union Fragment { uint4_t h[2]; intx8 all; };
+
+// One operand's tile: B rows (columns), loaded by NW waves.
+template <bool COLS, int B, int NW>
+struct Stage {
+  static constexpr int BYTES = B * 128, SEGS = B / 8 / NW;   // segments of 1 KiB, one load instruction each, of a wave
+  static constexpr int PITCH = COLS ? B * 2 : 128;           // of the tile's rows in LDS
+  static constexpr int TURNS = B / 16 < 8 ? B / 16 - 1 : 7;
+  static_assert(B % (8 * NW) == 0, "whole segments");
+  unsigned off[SEGS];        // of this lane's piece from the tile's start in memory
+
+  // of the piece that a lane loads for segment seg: its row (by columns: its k) and its first byte there
+  static __device__ __forceinline__ int row(int seg, int lane) { return COLS ? seg * (1024 / PITCH) + lane / (PITCH / 16) : seg * 8 + (lane >> 3); }
+  static __device__ __forceinline__ int byte(int seg, int lane) {
+    const int r = row(seg, lane);
+    if constexpr (COLS) {
+      const int c = lane % (PITCH / 16);
+      return (((c >> 1) ^ (turn(r) & TURNS)) * 2 + (c & 1)) * 16;
+    } else {
+      return ((lane & 7) ^ (r >> 1 & 7)) * 16;
+    }
+  }
+  // pitch: of the operand in memory; left: rows (by rows) or bytes of a row (by columns) from the tile's start to the operand's end.  What lies beyond
+  // is loaded from the last one within: it only reaches outputs that are not stored.
+  __device__ __forceinline__ void init(int wave, int lane, unsigned pitch, int left) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int oj = j0 + wj + 16 * j + (lane & 15);
-    if (oj >= j_end) continue;
-    float up = 1.0f;
+    for (int s = 0; s < SEGS; ++s) {
+      int r = row(wave * SEGS + s, lane), b = byte(wave * SEGS + s, lane);
+      if (COLS && b > left - 16) b = left - 16;
+      if (!COLS && r > left - 1) r = left - 1;
+      off[s] = (unsigned)r * pitch + (unsigned)b;
+    }
+  }
+  // A stage from `from` to LDS byte `to`; left: bytes of k (by rows) or k (by columns) that there are: what is beyond becomes zero.
+  __device__ __forceinline__ void load(const unsigned char* from, unsigned to, int wave, int lane, int left) const {
+    if (left >= (COLS ? 64 : 128)) {
+#pragma unroll
+      for (int s = 0; s < SEGS; ++s) load_to_lds(from, off[s], to + (wave * SEGS + s) * 1024);
+    } else {
+#pragma unroll
+      for (int s = 0; s < SEGS; ++s) {
+        if ((COLS ? row(wave * SEGS + s, lane) : byte(wave * SEGS + s, lane)) < left)
+          load_to_lds(from, off[s], to + (wave * SEGS + s) * 1024);
+        else
+          *(__attribute__((address_space(3))) uint4_t*)(size_t)(to + (wave * SEGS + s) * 1024 + lane * 16) = uint4_t{0, 0, 0, 0};
+      }
+    }
+  }
+  // Where a lane reads block 0 of the wave's from (w0: its first row or column); block i, half h lie at this address with some bits
+  // turned over (a swizzle is an exclusive or) plus constants.
+  static __device__ __forceinline__ unsigned lane_base(int w0, int lane) {
+    if constexpr (COLS) {
+      const int k = (lane >> 4) * 8 + (lane >> 2 & 3);
+      return k * PITCH + ((w0 >> 4) ^ (turn(k) & TURNS)) * 32 + (lane & 3) * 8;
+    } else {
+      return (w0 + (lane & 15)) * 128 + ((lane >> 4) ^ (lane >> 1 & 7)) * 16;
+    }
+  }
+  // Block i (16 rows or columns) of the tile at LDS byte `tile`: 128 bytes of k for two MFMAs of 32 (bf16) or one of 128 (e4m3).
+  static __device__ __forceinline__ void fragment(unsigned base, unsigned tile, int i, Fragment& f) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      if constexpr (COLS) {
+        typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) bf16x4_t* p4;
+        const unsigned p = (base ^ (i * 32)) + tile + h * 32 * PITCH;
+        union { bf16x4_t h[2]; uint4_t u; } v;
+        v.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((p4)(size_t)p);
+        v.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((p4)(size_t)(p + 4 * PITCH));
+        f.h[h] = v.u;
+      } else {
+        f.h[h] = *(const __attribute__((address_space(3))) uint4_t*)(size_t)((base ^ (h * 64)) + tile + i * 2048);
+      }
+  }
+};
+
+// Row tiles of all experts and of the rows without one.
+template <int BJ>
+__device__ __forceinline__ int row_tiles(const ProductArgs& a) {
+  const int lane = (int)threadIdx.x & 63;
+  int n = 0;
+  for (int e = lane; e <= a.E; e += 64) {
+    const int lo = bound(a, e), hi = e < a.E ? bound(a, e + 1) : (int)a.rows;
+    n += hi > lo ? (hi - lo + BJ - 1) / BJ : 0;
+  }
+#pragma unroll
+  for (int d = 32; d; d >>= 1) n += __shfl_xor(n, d);
+  return __builtin_amdgcn_readfirstlane(n);
+}
+// Workgroup -> tile of `total`: each XCD (workgroups are dealt to the eight in turn) takes consecutive ones.  -1: none left.
+__device__ __forceinline__ int xcd_tile(int total) {
+  const int chunk = (total + 7) / 8, i = (int)blockIdx.x >> 3, t = ((int)blockIdx.x & 7) * chunk + i;
+  return i < chunk && t < total ? t : -1;
+}
+// Tile t of ni x nj: four rows of tiles at a time, so that workgroups that run together share both operands.
+__device__ __forceinline__ void tile_at(int t, int ni, int nj, int& i, int& j) {
+  const int g = t / (4 * ni), r = t - g * 4 * ni, n = nj - 4 * g < 4 ? nj - 4 * g : 4;
+  i = r / n;
+  j = 4 * g + r % n;
+}
+
+// One tile.
+template <bool FP8, bool IC, bool JC, bool RAGGED, bool F32OUT, int BI, int BJ, int WI, int WJ>
+__device__ __forceinline__ void tile_product(const ProductArgs& a, unsigned char* product_lds, int expert, int i0, int j0, int j_end, int k0, int k_end) {
+  constexpr int BYTES = FP8 ? 1 : 2, KS = 128 / BYTES, NI = BI / WI / 16, NJ = BJ / WJ / 16;
+  using SI = Stage<IC, BI, WI * WJ>;
+  using SJ = Stage<JC, BJ, WI * WJ>;
+  constexpr int STAGE = SI::BYTES + SJ::BYTES;
+  static_assert(NI % 4 == 0, "a ring of four fragments");
+  const unsigned lds = (unsigned)(size_t)(lds_byte*)product_lds;
+  int lane = (int)threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  asm volatile("" : "+v"(lane));                               // (nothing of this is worked out before its time and kept)
+  // where the tiles begin in memory, and how far a stage takes them
+  const unsigned char* pi = a.I.data + (RAGGED ? 0 : (long long)(expert < a.E ? expert : 0) * a.i_expert);
+  pi += IC ? (long long)k0 * a.I.pitch + (long long)i0 * BYTES : (long long)i0 * a.I.pitch;
+  const unsigned char* pj = a.J.data + (JC ? (long long)k0 * a.J.pitch + (long long)j0 * BYTES : (long long)j0 * a.J.pitch);
+  const long long di = IC ? KS * a.I.pitch : 128, dj = JC ? KS * a.J.pitch : 128;
+  SI si;
+  SJ sj;
+  si.init(wave, lane, (unsigned)a.I.pitch, IC ? (a.ni - i0) * BYTES : a.ni - i0);
+  sj.init(wave, lane, (unsigned)a.J.pitch, JC ? (j_end - j0) * BYTES : j_end - j0);
+
+  floatx4 acc[NI][NJ] = {};
+  Fragment fi[4], fj[2][NJ];
+  const int wi = wave % WI * (BI / WI), wj = wave / WI * (BJ / WJ);
+  const int steps = k_end > k0 ? (k_end - k0 + KS - 1) / KS : 0;
+  auto load = [&](int step) {                                  // to stage step & 1
+    const int k = k_end - k0 - step * KS;
+    const unsigned to = lds + (step & 1) * STAGE;
+    si.load(pi, to, wave, lane, IC ? k : k * BYTES);
+    sj.load(pj, to + SI::BYTES, wave, lane, JC ? k : k * BYTES);
+    pi += di;
+    pj += dj;
+  };
+  unsigned bi = SI::lane_base(wi, lane), bj = SJ::lane_base(wj, lane);
+  auto read_i = [&](int stage, int i) { SI::fragment(bi, lds + stage * STAGE, i, fi[i % 4]); };
+  auto read_j = [&](auto stage) {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) SJ::fragment(bj, lds + stage.value * STAGE + SI::BYTES, j, fj[stage.value][j]);
+  };
+  auto step = [&](auto stage, int s) {
+    constexpr int S = decltype(stage)::value;
+    asm volatile("" : "+v"(bi), "+v"(bj));                     // (addresses are made where they are used, not kept in registers throughout)
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      if (i + 3 < NI) read_i(S, i + 3);
+      if (i == NI - 2) {
+        stage_barrier();
+        if (s + 2 < steps) load(s + 2);
+        read_j(std::integral_constant<int, S ^ 1>{});
+        read_i(S ^ 1, 0);
+        read_i(S ^ 1, 1);
+      }
+      if (i == NI - 1) read_i(S ^ 1, 2);
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (FP8) {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fi[i % 4].all, fj[S][j].all, acc[i][j], 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
+      } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int j = 0; j < NJ; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fi[i % 4].h[h]), __builtin_bit_cast(bf16x8, fj[S][j].h[h]),
+                                                                acc[i][j], 0, 0, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  if (steps) {
+    load(0);
+    stage_barrier();
+    if (steps > 1) load(1);
+    read_j(std::integral_constant<int, 0>{});
+    read_i(0, 0);
+    read_i(0, 1);
+    read_i(0, 2);
+    for (int s = 0; s < steps; s += 2) {
+      step(std::integral_constant<int, 0>{}, s);
+      if (s + 1 < steps) step(std::integral_constant<int, 1>{}, s + 1);
+    }
+  }
+  unsigned char* out = a.out.data + (RAGGED ? (long long)expert * a.out_expert : 0);
+  store_tile<FP8, F32OUT>(a, out, expert, i0 + wi, j0 + wj, j_end, acc);
+}
+
+template <bool FP8, bool IC, bool JC, bool RAGGED, bool F32OUT, int BI, int BJ, int WI, int WJ>
+__global__ __launch_bounds__(64 * WI * WJ, 2) void product_tile_kernel(ProductArgs a) {
+  extern __shared__ __attribute__((aligned(1024))) unsigned char product_lds[];
+  int expert, ti, j0, j_end, k0, k_end;
+  if constexpr (RAGGED) {
+    const int per = a.tiles_i * a.tiles_j, t = xcd_tile(a.E * per);
+    if (t < 0) return;
+    int tj;
+    expert = t / per;
+    tile_at(t - expert * per, a.tiles_i, a.tiles_j, ti, tj);
+    j0 = tj * BJ;
+    j_end = a.nj;
+    k0 = __builtin_amdgcn_readfirstlane(bound(a, expert));
+    k_end = __builtin_amdgcn_readfirstlane(bound(a, expert + 1));
+  } else {
+    const int tiles = row_tiles<BJ>(a), t = xcd_tile(tiles * a.tiles_i);
+    int tj;
+    if (t < 0) return;
+    tile_at(t, a.tiles_i, tiles, ti, tj);
+    if (!find_rows<BJ>(a, tj, expert, j0, j_end)) return;
+    expert = __builtin_amdgcn_readfirstlane(expert);
+    j0 = __builtin_amdgcn_readfirstlane(j0);
+    j_end = __builtin_amdgcn_readfirstlane(j_end);
+    k0 = 0;
+    k_end = expert < a.E ? a.nk : 0;
+  }
+  tile_product<FP8, IC, JC, RAGGED, F32OUT, BI, BJ, WI, WJ>(a, product_lds, expert, ti * BI, j0, j_end, k0, k_end);
+}
+
+template <bool FP8, bool IC, bool JC, bool RAGGED, bool F32OUT, int BI, int BJ, int WI, int WJ>
+hipError_t go_tile(ProductArgs a, hipStream_t st) {
+  a.tiles_i = (a.ni + BI - 1) / BI;
+  a.tiles_j = (a.nj + BJ - 1) / BJ;
+  const long long tiles = (RAGGED ? (long long)a.E * a.tiles_j : a.rows / BJ + a.E + 1) * a.tiles_i;     // (each expert and the rest may have one that is not full)
+  constexpr int bytes = 2 * (BI + BJ) * 128;
+  auto kernel = product_tile_kernel<FP8, IC, JC, RAGGED, F32OUT, BI, BJ, WI, WJ>;
+  static std::atomic<unsigned long long> allowed{0};
+  const hipError_t e = allow_lds((const void*)kernel, bytes, allowed);
+  if (e != hipSuccess) return e;
+  kernel<<<dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(64 * WI * WJ), bytes, st>>>(a);
+  return hipGetLastError();
+}
+
+// ---- many tiles: 256 x 256 by eight waves, one workgroup a CU that goes from tile to tile without letting its loads run dry ----
+// LDS holds five units of 32 KiB, each the 128 bytes of k of one operand's tile, loaded in the order J0 I0 J1 I1 ... of the workgroup's steps, whatever
+// tile they belong to.  In step s a wave multiplies the I fragments of its eight blocks, a ring of four read three blocks ahead, with the four J fragments it
+// holds, and reads the J fragments of step s + 1.  Two barriers a step, each of which waits for one unit, frees one and is followed by the loads of one:
+//   Y, before block 1: J of s + 1 has landed, J of s has been read by all -> I of s + 2
+//   X, before block 5: I of s + 1 has landed, I of s and J of s + 1 have been read by all -> J of s + 3
+// so each load has a step and a half (some 2 us) to arrive.  Behind a barrier MFMAs come first, loads and reads between them: all eight waves are at the
+// same place there, and whatever came before the MFMAs would leave the matrix cores idle.
+//
+// Loads go through buffers that end where the operand does: rows and k beyond come back as zeros, and nothing has to be clamped or counted apart.  The
+// loop over a tile's steps has no branch but that at a tile's end: past the last tile the loads read an empty buffer.
+constexpr int kUnit = 32768, kUnits = 5;
+typedef int intx4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ void buffer_to_lds(intx4 rsrc, unsigned off, unsigned to) {                  // 64 x 16 bytes to 1 KiB
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(rsrc), "s"(to) : "memory");
+}
+// All but the youngest 8 loads of the wave (two units') have landed and every read has been answered; then all waves' have.  stored: a tile's stores
+// are younger than the unit that is waited for too (memory operations are counted off in the order they were issued in).
+constexpr int kTileStores = 32;
+__device__ __forceinline__ void unit_barrier(bool stored) {
+  __builtin_amdgcn_sched_barrier(0);
+#ifdef LASNET_DRAIN_AT_BARRIERS
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#else
+  if (stored)
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(8 + kTileStores) : "memory");
+  else
+    asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#endif
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+typedef __amdgpu_buffer_rsrc_t product_rsrc_t;
+__device__ __forceinline__ product_rsrc_t product_rsrc(const void* p, unsigned bytes) {
+  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)(size_t)p), hi = __builtin_amdgcn_readfirstlane((unsigned)((size_t)p >> 32));
+  return __builtin_amdgcn_make_buffer_rsrc((void*)(((unsigned long long)hi << 32) | lo), 0, (int)__builtin_amdgcn_readfirstlane(bytes), 0x00020000);
+}
+
+// A tile with a reduction.
+struct TileWork {
+  int expert, i0, j0, j_end, k0, k_end, steps;
+};
+
+// Where an operand's loads are: the tile at the next step's k, and how many bytes of the operand there are from there on.
+struct Walk {
+  const unsigned char* at;
+  long long bytes;
+  __device__ __forceinline__ void move(long long by) {
+    at += by;
+    bytes -= by;
+  }
+  __device__ __forceinline__ intx4 rsrc() const {
+    const unsigned n = bytes <= 0 ? 0u : bytes > 0xffffffffll ? 0xffffffffu : (unsigned)bytes;
+    return intx4{(int)(unsigned)(size_t)at, (int)((size_t)at >> 32 & 0xffff), (int)n, 0x00020000};
+  }
+};
+
+// The wave's 128 x 64 of a tile: scaled, rounded, stored through a buffer that ends with the tile's last row.  Always kTileStores stores (by hand: they are
+// counted, see unit_barrier).
+template <bool FP8, bool F32OUT>
+__device__ __forceinline__ void store_big_tile(const ProductArgs& a, unsigned char* out, const TileWork& t, int wi, int wj, int lane, const floatx4 (&acc)[8][4]) {
+  constexpr int OB = F32OUT ? 4 : 2;
+  asm volatile("" : "+v"(lane));
+  const unsigned pitch = (unsigned)a.out.pitch;
+  const int rows = t.j_end - t.j0 < 256 ? t.j_end - t.j0 : 256;
+  const intx4 to = Walk{out + (long long)t.j0 * a.out.pitch + (long long)t.i0 * OB, (long long)(rows - 1) * a.out.pitch + (long long)(a.ni - t.i0) * OB}.rsrc();
+  const float floor = a.relu ? 0.f : -INFINITY;               // (NaN passes)
+  // the scales of the wave's 64 rows and 128 columns, one and two a lane, all asked for before the first store
+  float row_scale = 1.f, col_scale[2] = {1.f, 1.f};
+  if constexpr (FP8) {
+    unsigned byte = 127;
+    if (a.scale) byte = __builtin_amdgcn_raw_buffer_load_b8(product_rsrc(a.scale + t.j0, (unsigned)rows), wj + lane, 0, 0);
+    if (a.wscale) {
+      const product_rsrc_t ws = product_rsrc(a.wscale + (size_t)t.expert * a.ni, (unsigned)a.ni * 4);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) col_scale[h] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(ws, (t.i0 + wi + 64 * h + lane) * 4, 0, 0));
+    }
+    row_scale = scale_value(byte);
+  }
+  float up[4] = {1.f, 1.f, 1.f, 1.f};
+  if constexpr (FP8)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) up[j] = __shfl(row_scale, 16 * j + (lane & 15));
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int oi = wi + 16 * i + (lane >> 4) * 4;
+    float w[4] = {1.f, 1.f, 1.f, 1.f};
     if constexpr (FP8)
-      if (a.scale && expert < a.E) up = scale_value(a.scale[oj]);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int oi = i0 + wi + 16 * i + (lane >> 4) * 4;
+      for (int r = 0; r < 4; ++r) w[r] = __shfl(col_scale[i / 4], 16 * (i % 4) + (lane >> 4) * 4 + r);
+    // (ni is a multiple of 4: a lane's four are stored or not)
+    unsigned off = t.i0 + oi < a.ni ? (unsigned)(wj + (lane & 15)) * pitch + (unsigned)oi * OB : 0xffffffffu;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
       float v[4];
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         v[r] = acc[i][j][r];
-        if constexpr (FP8) {
-          if (a.wscale && oi + r < a.ni && expert < a.E) v[r] *= a.wscale[(size_t)expert * a.ni + oi + r];
-          v[r] *= up;
-        }
-        if (a.relu) v[r] = v[r] < 0.f ? 0.f : v[r];
+        if constexpr (FP8) v[r] *= w[r] * up[j];
+        v[r] = v[r] < floor ? floor : v[r];
       }
-      unsigned char* o = out + (long long)oj * a.out.pitch + (long long)oi * (F32OUT ? 4 : 2);
-      if constexpr (F32OUT) {
-        store_piece<float>(o, a.ni - oi, Elem<float>::narrow(v));
-      } else if (oi + 4 <= a.ni) {
-        *(uint2_any*)o = uint2_t{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
-      } else {
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (oi + r < a.ni) Elem<__bf16>::put(o + 2 * r, bf16_pair(v[r], 0.f));
-      }
+      const unsigned o = off == 0xffffffffu ? off : off + (unsigned)j * 16 * pitch;
+      // (s_nop: the registers of a store of more than 8 bytes may not be written by the very next instruction)
+      if constexpr (F32OUT)
+        asm volatile("buffer_store_dwordx4 %0, %1, %2, 0 offen\n\ts_nop 1" ::"v"(Elem<float>::narrow(v)), "v"(o), "s"(to) : "memory");
+      else
+        asm volatile("buffer_store_dwordx2 %0, %1, %2, 0 offen" ::"v"(uint2_t{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])}), "v"(o), "s"(to) : "memory");
     }
   }
 }
 
 template <bool FP8, bool IC, bool JC, bool RAGGED, bool F32OUT>
+__global__ __launch_bounds__(512, 2) void product_stream_kernel(ProductArgs a) {
+  constexpr int BYTES = FP8 ? 1 : 2, KS = 128 / BYTES, OB = F32OUT ? 4 : 2;
+  constexpr int PAIR = FP8 ? 1 : 2;                           // steps of the loop's body: bf16 holds the J fragments of two steps, which change places
+  using SI = Stage<IC, 256, 8>;
+  using SJ = Stage<JC, 256, 8>;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char product_lds[];
+  const unsigned lds = (unsigned)(size_t)(lds_byte*)product_lds;
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int wi = wave % 2 * 128, wj = wave / 2 * 64;
+
+  // The experts' rows, one expert a lane (up to 63 of them; else they are looked up anew for each tile): first row, and tiles up to and with it (dW: the
+  // number of experts with more rows).
+  int lo = 0, upto = 0, tiles_j = a.tiles_j;
+  const bool kept = a.E <= 63;
+  if (kept) lo = bound(a, lane < a.E ? lane : a.E);
+  const int hi = __shfl(lo, lane < 63 ? lane + 1 : 63);
+  if constexpr (RAGGED) {
+    if (kept)
+      for (int e = 0; e < a.E; ++e) {
+        const int n = __builtin_amdgcn_readlane(hi - lo, e);
+        upto += n > hi - lo || (n == hi - lo && e < lane);
+      }
+    if (lane >= a.E) upto = 64;
+  } else {
+    if (kept) {
+      upto = hi > lo ? (hi - lo + 255) / 256 : 0;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const int u = __shfl_up(upto, d);
+        if (lane >= d) upto += u;
+      }
+      tiles_j = __builtin_amdgcn_readlane(upto, 63);
+    } else {
+      const int rest = (int)a.rows - __builtin_amdgcn_readfirstlane(bound(a, a.E));
+      tiles_j = row_tiles<256>(a) - (rest + 255) / 256;
+    }
+    // the rows that no expert has
+    const int width = a.ni * OB;
+    for (long long r = bound(a, a.E) + (long long)blockIdx.x; r < a.rows; r += gridDim.x)
+      for (int c = (int)threadIdx.x * 4 * OB; c < width; c += 512 * 4 * OB)
+        if constexpr (F32OUT)
+          *(uint4_t*)(a.out.data + r * a.out.pitch + c) = uint4_t{0, 0, 0, 0};
+        else
+          *(uint2_t*)(a.out.data + r * a.out.pitch + c) = uint2_t{0, 0};
+  }
+  // Workgroups are dealt to the eight XCDs in turn, each of which has an L2.  Products of rows: an XCD takes consecutive tiles.  dW: an XCD takes its eighth of
+  // every expert's tiles (or, of few, every eighth tile), so that none is left with the longest reductions, and the experts with most rows come first.
+  // Within the XCD its `stride` workgroups take a tile each in turn (dW: there and back, the longest with the shortest).
+  const int xcd = (int)blockIdx.x & 7, slot = (int)blockIdx.x >> 3, stride = (int)gridDim.x >> 3;
+  const int per = RAGGED ? a.tiles_i * a.tiles_j : 1;
+  const bool eighths = RAGGED && per >= 64;
+  const int per_first = eighths ? (int)((long long)per * xcd / 8) : 0, per_mine = eighths ? (int)((long long)per * (xcd + 1) / 8) - per_first : 1;
+  const int total = RAGGED ? a.E * per : tiles_j * a.tiles_i;
+  const int chunk = (total + 7) / 8;
+  int end = RAGGED ? (eighths ? a.E * per_mine : (total - xcd + 7) / 8) : total - xcd * chunk < chunk ? total - xcd * chunk : chunk;      // this XCD's tiles
+  // A last round that would leave half of the XCD idle or more is cut into quarters of tiles.
+  const int rest = end > 0 && end % stride <= stride / 2 ? end % stride : 0;
+  end -= rest;
+
+  auto work = [&](int p) {                                    // the XCD's tile p
+    TileWork w;
+    int ti, tj;
+    if constexpr (RAGGED) {
+      int rank, u;
+      if (eighths) {
+        rank = p / per_mine;
+        u = per_first + p - rank * per_mine;
+      } else {
+        rank = (p * 8 + xcd) / per;
+        u = p * 8 + xcd - rank * per;
+      }
+      w.expert = kept ? __ffsll((long long)__ballot(upto == rank)) - 1 : rank;
+      tile_at(u, a.tiles_i, a.tiles_j, ti, tj);
+      w.j0 = tj * 256;
+      w.j_end = a.nj;
+      w.k0 = kept ? __builtin_amdgcn_readlane(lo, w.expert) : __builtin_amdgcn_readfirstlane(bound(a, w.expert));
+      w.k_end = kept ? __builtin_amdgcn_readlane(hi, w.expert) : __builtin_amdgcn_readfirstlane(bound(a, w.expert + 1));
+    } else {
+      tile_at(xcd * chunk + p, a.tiles_i, tiles_j, ti, tj);
+      if (kept) {
+        const int l = __ffsll((long long)__ballot(tj < upto)) - 1;
+        const int before = l ? __builtin_amdgcn_readlane(upto, l - 1) : 0;
+        w.expert = l;
+        w.j0 = __builtin_amdgcn_readlane(lo, l) + (tj - before) * 256;
+        w.j_end = __builtin_amdgcn_readlane(lo, l + 1);
+      } else {
+        int e = 0, j0 = 0, j1 = 0;
+        find_rows<256>(a, tj, e, j0, j1);
+        w.expert = __builtin_amdgcn_readfirstlane(e);
+        w.j0 = __builtin_amdgcn_readfirstlane(j0);
+        w.j_end = __builtin_amdgcn_readfirstlane(j1);
+      }
+      w.k0 = 0;
+      w.k_end = a.nk;
+    }
+    w.i0 = ti * 256;
+    // four at least (so loads are never further ahead than the next tile), with zeros behind the end
+    const int n = w.k_end > w.k0 ? (w.k_end - w.k0 + PAIR * KS - 1) / (PAIR * KS) * PAIR : 0;
+    w.steps = n && n < 4 ? 4 : n;
+    return w;
+  };
+  // the next tile from t on that has a reduction; dW of an expert without rows is stored as zeros on the way
+  floatx4 acc[8][4];
+  auto clear = [&] {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+  };
+  auto tile_of = [&](int round) { return round * stride + (RAGGED && (round & 1) ? stride - 1 - slot : slot); };
+  auto next_work = [&](int& round) {
+    TileWork w;
+    w.steps = 0;
+    for (; round * stride < end; ++round) {
+      const int p = tile_of(round);
+      if (p >= end) continue;
+      w = work(p);
+      if (!RAGGED || w.steps) break;
+    }
+    return w;
+  };
+  if constexpr (RAGGED) {
+    clear();
+    for (int round = 0; round * stride < end; ++round) {
+      const int p = tile_of(round);
+      if (p >= end) continue;
+      const TileWork w = work(p);
+      if (!w.steps) store_big_tile<FP8, F32OUT>(a, a.out.data + (long long)w.expert * a.out_expert, w, wi, wj, lane, acc);
+    }
+  }
+
+  // ---- loads ----
+  const long long di = IC ? KS * a.I.pitch : 128, dj = JC ? KS * a.J.pitch : 128;
+  // Of this lane's first piece of a unit from the tile.  The next lies a segment's rows further with bit 6 of its byte turned over (both kinds of tile: the
+  // bit is bit 2 of the lane), the other two likewise two segments further.
+  unsigned off_i = (unsigned)SI::row(wave * 4, lane) * (unsigned)a.I.pitch + (unsigned)SI::byte(wave * 4, lane);
+  unsigned off_j = (unsigned)SJ::row(wave * 4, lane) * (unsigned)a.J.pitch + (unsigned)SJ::byte(wave * 4, lane);
+  auto walk_i = [&](const TileWork& w) {
+    Walk v;
+    v.at = a.I.data + (RAGGED ? 0 : (long long)w.expert * a.i_expert) + (IC ? (long long)w.k0 * a.I.pitch + (long long)w.i0 * BYTES : (long long)w.i0 * a.I.pitch);
+    v.bytes = IC ? (long long)(w.k_end - w.k0 - 1) * a.I.pitch + (long long)(a.ni - w.i0) * BYTES : (long long)(a.ni - w.i0 - 1) * a.I.pitch + (long long)a.nk * BYTES;
+    return v;
+  };
+  auto walk_j = [&](const TileWork& w) {
+    Walk v;
+    v.at = a.J.data + (JC ? (long long)w.k0 * a.J.pitch + (long long)w.j0 * BYTES : (long long)w.j0 * a.J.pitch);
+    v.bytes = JC ? (long long)(w.k_end - w.k0 - 1) * a.J.pitch + (long long)(w.j_end - w.j0) * BYTES
+                 : (long long)(w.j_end - w.j0 - 1) * a.J.pitch + (long long)a.nk * BYTES;
+    return v;
+  };
+  Walk li, lj, ni, nj;                                        // of the tile being loaded, and of the one after the tile being computed
+  int l_k = 0, l_steps = 0, n_k = 0, n_steps = 0;             // its k and steps left (an empty tile's: no end)
+  unsigned l_to = lds;
+  auto turn_slot = [&](unsigned& s) { s = s == lds + (kUnits - 1) * kUnit ? lds : s + kUnit; };
+  auto nothing = [](int) {};
+  // A unit of the load step, between the parts of `meanwhile` (which does what is due anyway, in four parts).
+  auto issue = [&](auto j, auto meanwhile) {
+    constexpr bool J = decltype(j)::value, C = J ? JC : IC;
+    const intx4 rsrc = (J ? lj : li).rsrc();
+    unsigned o[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+      o[s] = (J ? off_j : off_i) + (s & 1 ? 64u - ((unsigned)lane & 4) * 32 : 0u) + (unsigned)(s * (C ? 2 : 8)) * (unsigned)(J ? a.J.pitch : a.I.pitch);
+    if (!C && l_k < KS) {                                     // by rows, what is beyond the end of k lies inside the buffer
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+        if ((J ? SJ::byte(wave * 4 + s, lane) : SI::byte(wave * 4 + s, lane)) >= l_k * BYTES) o[s] = 0xffffffffu;
+    }
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      meanwhile(s);
+      __builtin_amdgcn_sched_barrier(0);
+      buffer_to_lds(rsrc, o[s], l_to + (wave * 4 + s) * 1024);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    turn_slot(l_to);
+    (J ? lj : li).move(J ? dj : di);
+    if constexpr (!J) {
+      l_k -= KS;
+      if (--l_steps == 0) {
+        li = ni;
+        lj = nj;
+        l_k = n_k;
+        l_steps = n_steps;
+      }
+    }
+  };
+
+  // ---- products ----
+  // The next step's J fragments 2 and 3 take the place of this step's as the last block is done with them (every block begins with these two); 0 and 1
+  // are held twice in bf16, and follow 2 and 3 in e4m3, whose fragments are whole octets of registers and leave no room for that.
+  Fragment fi[4], fj[PAIR][2], fj2[2];
+  unsigned bi = SI::lane_base(wi, lane), bj = SJ::lane_base(wj, lane);
+  unsigned c_j = lds, c_i = lds + kUnit;                      // the units that J and I fragments are read from
+  auto next_unit = [&](unsigned& c) {
+    turn_slot(c);
+    turn_slot(c);
+  };
+  auto read_i = [&](int i) { SI::fragment(bi, c_i, i, fi[i % 4]); };
+  auto read_j = [&](auto stage, int j) { SJ::fragment(bj, c_j, j, j < 2 ? fj[stage.value][j] : fj2[j - 2]); };
+  auto multiply = [&](auto stage, int i, int part) {          // a quarter of block i's MFMAs
+    constexpr int S = decltype(stage)::value;
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (FP8) {
+      const int j = part ^ 2;
+      acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fi[i % 4].all, (j < 2 ? fj[S][j] : fj2[j - 2]).all, acc[i][j], 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
+    } else {
+      const int j0 = part < 2 ? 2 : 0, h = part & 1;
+#pragma unroll
+      for (int j = j0; j < j0 + 2; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fi[i % 4].h[h]),
+                                                            __builtin_bit_cast(bf16x8, (j < 2 ? fj[S][j] : fj2[j - 2]).h[h]), acc[i][j], 0, 0, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  int young = 0;                                              // steps (Y to Y) for which the units waited for are older than the last tile's stores
+  auto step = [&](auto stage) {
+    constexpr int S = decltype(stage)::value;
+    constexpr auto next = std::integral_constant<int, (S + 1) % PAIR>{};
+    // (addresses are made where they are used, not kept in registers throughout)
+    asm volatile("" : "+v"(bi), "+v"(bj), "+v"(off_i), "+v"(off_j));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (i == 1) {                                           // Y
+        unit_barrier(young > 0);
+        next_unit(c_j);
+        issue(std::false_type{}, [&](int p) {
+          multiply(stage, 1, p);
+          if (p == 0) read_i(4);
+          if (!FP8 && p == 1) read_j(next, 0);
+        });
+        --young;
+      } else if (i == 5) {                                    // X
+        unit_barrier(young > 0);
+        next_unit(c_i);
+        issue(std::true_type{}, [&](int p) {
+          multiply(stage, 5, p);
+          if (p == 0) read_i(0);
+        });
+      } else {
+        read_i((i + 3) % 8);
+        if (!FP8 && i == 2) read_j(next, 1);
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          multiply(stage, i, p);
+          if (i == 7 && FP8) read_j(next, p ^ 2);
+          if (i == 7 && !FP8 && p == 1) {
+            read_j(next, 2);
+            read_j(next, 3);
+          }
+        }
+      }
+    }
+  };
+
+  int round = 0;
+  TileWork w = next_work(round);
+  if (round * stride < end) {
+    li = walk_i(w);
+    lj = walk_j(w);
+    l_k = w.k_end - w.k0;
+    l_steps = w.steps;
+    ni = nj = Walk{a.J.data, 0};
+    issue(std::true_type{}, nothing);
+    issue(std::false_type{}, nothing);
+    issue(std::true_type{}, nothing);
+    issue(std::false_type{}, nothing);
+    unit_barrier(false);
+    issue(std::true_type{}, nothing);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) read_j(std::integral_constant<int, 0>{}, j);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) read_i(i);
+    while (true) {
+      ++round;
+      const TileWork after = next_work(round);
+      const bool more = round * stride < end;
+      if (more) {
+        ni = walk_i(after);
+        nj = walk_j(after);
+        n_k = after.k_end - after.k0;
+        n_steps = after.steps;
+      } else {
+        ni = nj = Walk{a.J.data, 0};
+        n_k = 1 << 30;
+        n_steps = 0;
+      }
+      clear();
+      for (int s = 0; s < w.steps; s += PAIR) {
+        step(std::integral_constant<int, 0>{});
+        if constexpr (PAIR == 2) step(std::integral_constant<int, 1>{});
+      }
+      store_big_tile<FP8, F32OUT>(a, a.out.data + (RAGGED ? (long long)w.expert * a.out_expert : 0), w, wi, wj, lane, acc);
+      if (!more) break;
+      young = 2;
+      w = after;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // (the last loads write to this workgroup's LDS)
+  }
+  for (int q = slot; q < 4 * rest; q += stride) {
+    const TileWork v = work(end + q / 4);
+    const int i0 = v.i0 + (q & 1) * 128, j0 = v.j0 + (q >> 1 & 1) * 128;
+    if (i0 >= a.ni || j0 >= v.j_end) continue;
+    __syncthreads();
+    tile_product<FP8, IC, JC, RAGGED, F32OUT, 128, 128, 2, 4>(a, product_lds, v.expert, i0, j0, v.j_end, v.k0, v.k_end);
+  }
+}
+
+template <bool FP8, bool IC, bool JC, bool RAGGED, bool F32OUT>
+hipError_t go_stream(ProductArgs a, hipStream_t st) {
+  a.tiles_i = (a.ni + 255) / 256;
+  a.tiles_j = (a.nj + 255) / 256;
+  auto kernel = product_stream_kernel<FP8, IC, JC, RAGGED, F32OUT>;
+  static std::atomic<unsigned long long> allowed{0};
+  const hipError_t e = allow_lds((const void*)kernel, kUnits * kUnit, allowed);
+  if (e != hipSuccess) return e;
+  kernel<<<dim3(256), dim3(512), kUnits * kUnit, st>>>(a);
+  return hipGetLastError();
+}
+
+// Whole pieces, and what the loads address with 32 bits.
+template <bool IC, bool JC>
+bool whole(const ProductArgs& a, int bytes, int B) {
+  const unsigned long long low = (unsigned long long)a.I.data | (unsigned long long)a.J.data | (unsigned long long)a.I.pitch |
+                                 (unsigned long long)a.J.pitch | (unsigned long long)a.i_expert;
+  if (low & 15) return false;
+  if ((!IC || !JC) && (long long)a.nk * bytes % 16) return false;
+  if (IC && (long long)a.ni * bytes % 16) return false;
+  if (JC && (long long)a.nj * bytes % 16) return false;
+  return a.I.pitch < (1ll << 31) / B && a.J.pitch < (1ll << 31) / B;
+}
+
+template <bool FP8, bool IC, bool JC, bool RAGGED, bool F32OUT>
 hipError_t go(ProductArgs a, hipStream_t st) {
+  if (whole<IC, JC>(a, FP8 ? 1 : 2, 256)) {
+    const long long big = (RAGGED ? (long long)a.E * ((a.nj + 255) / 256) : a.rows / 256 + a.E / 2) * ((a.ni + 255) / 256);
+    const bool long_enough = RAGGED || (long long)a.nk * (FP8 ? 1 : 2) > 384;
+    if (big >= 256 && long_enough && a.ni % 4 == 0 && !(((unsigned long long)a.out.data | (unsigned long long)a.out.pitch | (unsigned long long)a.out_expert) & 15) &&
+        a.out.pitch < (1ll << 31) / 256)
+      return go_stream<FP8, IC, JC, RAGGED, F32OUT>(a, st);
+    return go_tile<FP8, IC, JC, RAGGED, F32OUT, 128, 128, 2, 2>(a, st);
+  }
   a.tiles_i = (a.ni + 127) / 128;
   a.tiles_j = (a.nj + 127) / 128;
   const long long tiles = RAGGED ? (long long)a.E * a.tiles_j : a.rows / 128 + a.E + 1;     // (each expert and the rest may have one tile that is not full)

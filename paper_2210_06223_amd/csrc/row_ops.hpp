@@ -36,6 +36,18 @@ hipError_t launch_expert_product_dw(long long rows, int E, int n, int k, RowsArg
 
 namespace {
 
+// A kernel that needs more than 64 KiB of dynamic LDS must be told so once per device.
+inline hipError_t allow_lds(const void* kernel, int bytes, std::atomic<unsigned long long>& done) {
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  const unsigned long long bit = dev < 64 ? 1ull << dev : 0ull;    // devices past 63: set every time
+  if (done.load(std::memory_order_acquire) & bit) return hipSuccess;
+  e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == hipSuccess) done.fetch_or(bit, std::memory_order_release);
+  return e;
+}
+
 // ---- pieces of 16 bytes, at any address: gfx950's global loads and stores take every alignment (one instruction either way), so
 // rows that start anywhere need no variant of their own; only the end of a row, where less than a piece is left, goes by elements.
 typedef unsigned uint4_t __attribute__((ext_vector_type(4)));

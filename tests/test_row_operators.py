@@ -303,6 +303,10 @@ PRODUCTS = [(1, 1, 1, 1, "one"), (1, 3, 16, 64, "one"), (2, 2, 130, 72, "one"), 
             (700, 5, 512, 256, "spread"), (64, 70, 96, 1024, "spread"), (40, 3, 64, 64, "none"), (515, 3, 300, 1000, "tail"), (33, 2, 1024, 4104, "one"), (1000, 130, 64, 80, "spread")]
 
 
+# enough 256 x 256 tiles for one workgroup on each CU: several a workgroup, ends inside tiles, reductions of one step and odd ones, more experts than lanes
+MANY_TILES = [(4096, 1, 4096, 72, "one"), (2000, 70, 2048, 200, "spread"), (5000, 6, 7000, 136, "tail"), (300, 4, 2048, 2056, "spread"), (1500, 62, 1024, 64, "spread"), (1100, 63, 1024, 456, "tail"), (1100, 64, 1024, 456, "tail"), (9000, 3, 2056, 2064, "tail")]
+
+
 def e4m3_rows(t):
     """Rows in 8 bits with scales, for inputs: any power of two near the row's size."""
     e = torch.ceil(torch.log2(t.abs().amax(-1).clamp(min=1e-30))) - 8
@@ -318,7 +322,7 @@ def product_ref(x, W, o):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("rows,E,n,k,kind", PRODUCTS)
+@pytest.mark.parametrize("rows,E,n,k,kind", PRODUCTS + MANY_TILES)
 def test_expert_product(rows, E, n, k, kind):
     o = groups(rows, E, kind, rows + n)
     offsets = torch.from_numpy(o.astype(np.int32)).cuda()
@@ -352,7 +356,7 @@ def test_expert_product(rows, E, n, k, kind):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("rows,E,n,k,kind", PRODUCTS + [(0, 3, 40, 24, "none"), (2500, 2, 136, 264, "spread")])
+@pytest.mark.parametrize("rows,E,n,k,kind", PRODUCTS + MANY_TILES + [(0, 3, 40, 24, "none"), (2500, 2, 136, 264, "spread"), (700, 70, 512, 520, "spread")])
 def test_expert_product_gradients(rows, E, n, k, kind):
     o = groups(rows, E, kind, rows + n)
     offsets = torch.from_numpy(o.astype(np.int32)).cuda()
