@@ -273,21 +273,53 @@ __global__ __launch_bounds__(256) void product_kernel(ProductArgs a) {
 }
 
 // ---- whole pieces: rows, widths and addresses that are multiples of 16 bytes ----
-// BI x BJ of the output by WI x WJ waves; tiles go from memory to LDS without passing registers, two stages.
-//
-// A stage is 128 bytes of k of both tiles.  A wave holds the fragments of its J blocks for the whole stage and walks its I blocks with a ring of
-// four fragments, each read three blocks ahead, over the end of the stage too: after the block third from last every read of the stage
-// has been answered, so one barrier there frees the stage for the loads of the one after next and opens the next, whose first
-// fragments are read while the last two blocks' MFMAs run.  The MFMAs of a block (NJ, or 2 NJ in bf16) are independent of each other.
+// Tiles go from memory to LDS without passing registers, through buffers that end where the operand does: rows and k beyond come back as zeros, and nothing has
+// to be clamped.  Every load is issued, those past the last step of an empty buffer, so that they can be counted.
 typedef __attribute__((address_space(3))) unsigned char lds_byte;
+typedef int intx4 __attribute__((ext_vector_type(4)));
+typedef __amdgpu_buffer_rsrc_t product_rsrc_t;
 
-__device__ __forceinline__ void load_to_lds(const unsigned char* base, unsigned off, unsigned to) {     // 64 x 16 bytes to 1 KiB
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(to) : "memory");
+__device__ __forceinline__ product_rsrc_t product_rsrc(const void* p, unsigned bytes) {
+  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)(size_t)p), hi = __builtin_amdgcn_readfirstlane((unsigned)((size_t)p >> 32));
+  return __builtin_amdgcn_make_buffer_rsrc((void*)(((unsigned long long)hi << 32) | lo), 0, (int)__builtin_amdgcn_readfirstlane(bytes), 0x00020000);
 }
-// Every load of the wave has landed and every read has been answered; then all waves' have.
-__device__ __forceinline__ void stage_barrier() {
+// Where an operand's loads are: the tile at the next step's k, and the buffer that ends with the operand (by rows: what there is of the tile's rows from there on;
+// by columns: of the step's rows of k).  Kept to a few scalar instructions a step: the waves that share a SIMD have some 30 clocks for each pair of MFMAs.
+template <bool COLS>
+struct Feed {
+  unsigned long long at;
+  unsigned size;             // by rows: bytes from `at` to the end of the last row; by columns: of a row, from the tile's first column on
+  __device__ __forceinline__ void start(const unsigned char* first, int rows, int most, long long pitch, unsigned row_bytes) {
+    const unsigned long long f = (unsigned long long)first;
+    const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)f), hi = __builtin_amdgcn_readfirstlane((unsigned)(f >> 32));
+    at = (unsigned long long)hi << 32 | lo;
+    size = __builtin_amdgcn_readfirstlane(COLS ? row_bytes : (unsigned)((rows < most ? rows : most) - 1) * (unsigned)pitch + row_bytes);
+  }
+  // k: what is left of it (none: an empty buffer)
+  __device__ __forceinline__ intx4 rsrc(int k, unsigned pitch) const {
+    unsigned n = size;
+    if constexpr (COLS) n += (unsigned)((k < 64 ? k : 64) - 1) * pitch;
+    return intx4{(int)(unsigned)at, (int)(unsigned)(at >> 32), (int)(k > 0 ? n : 0u), 0x00020000};
+  }
+  __device__ __forceinline__ void move(unsigned by) {
+    at += by;
+    if constexpr (!COLS) size -= by;
+  }
+};
+__device__ __forceinline__ void buffer_to_lds(intx4 rsrc, unsigned off, unsigned to) {                  // 64 x 16 bytes to 1 KiB
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(rsrc), "s"(to) : "memory");
+}
+// All but the youngest VM memory operations of the wave have ended (they are counted off in the order they were issued in) and every LDS read has been
+// answered; then all waves' have.  (The check build waits for all.)
+template <int VM>
+__device__ __forceinline__ void counted_barrier() {
+  static_assert(VM >= 0 && VM < 64, "vmcnt is 6 bits");
   __builtin_amdgcn_sched_barrier(0);
+#ifdef LASNET_DRAIN_AT_BARRIERS
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#else
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(VM) : "memory");
+#endif
   __builtin_amdgcn_sched_barrier(0);
 }
 
@@ -300,8 +332,6 @@ struct Stage {
   static constexpr int PITCH = COLS ? B * 2 : 128;           // of the tile's rows in LDS
   static constexpr int TURNS = B / 16 < 8 ? B / 16 - 1 : 7;
   static_assert(B % (8 * NW) == 0, "whole segments");
-  unsigned off[SEGS];        // of this lane's piece from the tile's start in memory
-
   // of the piece that a lane loads for segment seg: its row (by columns: its k) and its first byte there
   static __device__ __forceinline__ int row(int seg, int lane) { return COLS ? seg * (1024 / PITCH) + lane / (PITCH / 16) : seg * 8 + (lane >> 3); }
   static __device__ __forceinline__ int byte(int seg, int lane) {
@@ -311,32 +341,6 @@ struct Stage {
       return (((c >> 1) ^ (turn(r) & TURNS)) * 2 + (c & 1)) * 16;
     } else {
       return ((lane & 7) ^ (r >> 1 & 7)) * 16;
-    }
-  }
-  // pitch: of the operand in memory; left: rows (by rows) or bytes of a row (by columns) from the tile's start to the operand's end.  What lies beyond
-  // is loaded from the last one within: it only reaches outputs that are not stored.
-  __device__ __forceinline__ void init(int wave, int lane, unsigned pitch, int left) {
-#pragma unroll
-    for (int s = 0; s < SEGS; ++s) {
-      int r = row(wave * SEGS + s, lane), b = byte(wave * SEGS + s, lane);
-      if (COLS && b > left - 16) b = left - 16;
-      if (!COLS && r > left - 1) r = left - 1;
-      off[s] = (unsigned)r * pitch + (unsigned)b;
-    }
-  }
-  // A stage from `from` to LDS byte `to`; left: bytes of k (by rows) or k (by columns) that there are: what is beyond becomes zero.
-  __device__ __forceinline__ void load(const unsigned char* from, unsigned to, int wave, int lane, int left) const {
-    if (left >= (COLS ? 64 : 128)) {
-#pragma unroll
-      for (int s = 0; s < SEGS; ++s) load_to_lds(from, off[s], to + (wave * SEGS + s) * 1024);
-    } else {
-#pragma unroll
-      for (int s = 0; s < SEGS; ++s) {
-        if ((COLS ? row(wave * SEGS + s, lane) : byte(wave * SEGS + s, lane)) < left)
-          load_to_lds(from, off[s], to + (wave * SEGS + s) * 1024);
-        else
-          *(__attribute__((address_space(3))) uint4_t*)(size_t)(to + (wave * SEGS + s) * 1024 + lane * 16) = uint4_t{0, 0, 0, 0};
-      }
     }
   }
   // Where a lane reads block 0 of the wave's from (w0: its first row or column); block i, half h lie at this address with some bits
@@ -349,21 +353,25 @@ struct Stage {
       return (w0 + (lane & 15)) * 128 + ((lane >> 4) ^ (lane >> 1 & 7)) * 16;
     }
   }
-  // Block i (16 rows or columns) of the tile at LDS byte `tile`: 128 bytes of k for two MFMAs of 32 (bf16) or one of 128 (e4m3).
-  static __device__ __forceinline__ void fragment(unsigned base, unsigned tile, int i, Fragment& f) {
+  // Block i (16 rows or columns) of the tile: 128 bytes of k for two MFMAs of 32 (bf16) or one of 128 (e4m3).  at: lane_base() + the tile's first byte (whose low
+  // ten bits are zero, so the bits may be turned over in the sum).
+  static __device__ __forceinline__ void fragment(unsigned at, int i, Fragment& f) {
+    if constexpr (COLS) {
+      typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+      typedef __attribute__((address_space(3))) bf16x4_t* p4;
+      const lds_byte* p = (const lds_byte*)(size_t)(at ^ (i * 32));
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-      if constexpr (COLS) {
-        typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
-        typedef __attribute__((address_space(3))) bf16x4_t* p4;
-        const unsigned p = (base ^ (i * 32)) + tile + h * 32 * PITCH;
+      for (int h = 0; h < 2; ++h) {
         union { bf16x4_t h[2]; uint4_t u; } v;
-        v.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((p4)(size_t)p);
-        v.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((p4)(size_t)(p + 4 * PITCH));
+        v.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((p4)(p + h * 32 * PITCH));
+        v.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((p4)(p + (h * 32 + 4) * PITCH));
         f.h[h] = v.u;
-      } else {
-        f.h[h] = *(const __attribute__((address_space(3))) uint4_t*)(size_t)((base ^ (h * 64)) + tile + i * 2048);
       }
+    } else {
+      typedef const __attribute__((address_space(3))) uint4_t* p16;
+      f.h[0] = *(p16)((const lds_byte*)(size_t)at + i * 2048);
+      f.h[1] = *(p16)((const lds_byte*)(size_t)(at ^ 64) + i * 2048);
+    }
   }
 };
 
@@ -392,94 +400,144 @@ __device__ __forceinline__ void tile_at(int t, int ni, int nj, int& i, int& j) {
   j = 4 * g + r % n;
 }
 
-// One tile.
-template <bool FP8, bool IC, bool JC, bool RAGGED, bool F32OUT, int BI, int BJ, int WI, int WJ>
+// One tile: BI x BJ of the output by WI x WJ waves, through STAGES stages of 128 bytes of k of both operands.
+//
+// A wave holds the fragments of its J blocks for the whole step and walks its I blocks with a ring of four fragments, each read three blocks ahead, over the end of
+// the step too: before the block second from last every read of the stage has been answered, so one barrier there frees the stage for the loads of STAGES
+// steps on and opens the next, whose first fragments are read while the last two blocks' MFMAs run.  MFMAs come first behind the barrier, loads and
+// reads between them: all waves are at the same place there.  The MFMAs of a block are independent of each other.
+template <bool FP8, bool IC, bool JC, bool RAGGED, bool F32OUT, int BI, int BJ, int WI, int WJ, int STAGES>
 __device__ __forceinline__ void tile_product(const ProductArgs& a, unsigned char* product_lds, int expert, int i0, int j0, int j_end, int k0, int k_end) {
   constexpr int BYTES = FP8 ? 1 : 2, KS = 128 / BYTES, NI = BI / WI / 16, NJ = BJ / WJ / 16;
   using SI = Stage<IC, BI, WI * WJ>;
   using SJ = Stage<JC, BJ, WI * WJ>;
-  constexpr int STAGE = SI::BYTES + SJ::BYTES;
+  constexpr int STAGE = SI::BYTES + SJ::BYTES, LOADS = SI::SEGS + SJ::SEGS;
   static_assert(NI % 4 == 0, "a ring of four fragments");
   const unsigned lds = (unsigned)(size_t)(lds_byte*)product_lds;
   int lane = (int)threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   asm volatile("" : "+v"(lane));                               // (nothing of this is worked out before its time and kept)
-  // where the tiles begin in memory, and how far a stage takes them
-  const unsigned char* pi = a.I.data + (RAGGED ? 0 : (long long)(expert < a.E ? expert : 0) * a.i_expert);
-  pi += IC ? (long long)k0 * a.I.pitch + (long long)i0 * BYTES : (long long)i0 * a.I.pitch;
-  const unsigned char* pj = a.J.data + (JC ? (long long)k0 * a.J.pitch + (long long)j0 * BYTES : (long long)j0 * a.J.pitch);
-  const long long di = IC ? KS * a.I.pitch : 128, dj = JC ? KS * a.J.pitch : 128;
-  SI si;
-  SJ sj;
-  si.init(wave, lane, (unsigned)a.I.pitch, IC ? (a.ni - i0) * BYTES : a.ni - i0);
-  sj.init(wave, lane, (unsigned)a.J.pitch, JC ? (j_end - j0) * BYTES : j_end - j0);
+  // where the tiles are in memory, and how far a step takes them
+  const unsigned char* I = a.I.data + (RAGGED ? 0 : (long long)(expert < a.E ? expert : 0) * a.i_expert);
+  const unsigned pitch_i = (unsigned)a.I.pitch, pitch_j = (unsigned)a.J.pitch, kb = (unsigned)a.nk * BYTES;
+  Feed<IC> li;
+  Feed<JC> lj;
+  li.start(I + (IC ? (long long)k0 * a.I.pitch + (long long)i0 * BYTES : (long long)i0 * a.I.pitch), a.ni - i0, BI, a.I.pitch, IC ? (unsigned)(a.ni - i0) * BYTES : kb);
+  lj.start(a.J.data + (JC ? (long long)k0 * a.J.pitch + (long long)j0 * BYTES : (long long)j0 * a.J.pitch), j_end - j0, BJ, a.J.pitch,
+           JC ? (unsigned)(j_end - j0) * BYTES : kb);
+  const unsigned di = IC ? KS * pitch_i : 128, dj = JC ? KS * pitch_j : 128;
+  unsigned off_i[SI::SEGS], off_j[SJ::SEGS];                  // of this lane's pieces from the tile
+#pragma unroll
+  for (int s = 0; s < SI::SEGS; ++s) off_i[s] = (unsigned)SI::row(wave * SI::SEGS + s, lane) * pitch_i + (unsigned)SI::byte(wave * SI::SEGS + s, lane);
+#pragma unroll
+  for (int s = 0; s < SJ::SEGS; ++s) off_j[s] = (unsigned)SJ::row(wave * SJ::SEGS + s, lane) * pitch_j + (unsigned)SJ::byte(wave * SJ::SEGS + s, lane);
+  const int steps = k_end > k0 ? (k_end - k0 + KS - 1) / KS : 0;
+  int l_k = k_end - k0;                                       // what is left of k to load
+  unsigned l_to = lds;
+  // A step's loads, between the parts of `meanwhile` (which does what is due anyway, in LOADS parts).
+  const unsigned to_i = wave * SI::SEGS * 1024, to_j = SI::BYTES + wave * SJ::SEGS * 1024;
+  auto load = [&](auto meanwhile) {
+    meanwhile(0);
+    const intx4 ri = li.rsrc(l_k, pitch_i), rj = lj.rsrc(l_k, pitch_j);
+    unsigned oi[SI::SEGS], oj[SJ::SEGS];
+#pragma unroll
+    for (int s = 0; s < SI::SEGS; ++s) oi[s] = off_i[s];
+#pragma unroll
+    for (int s = 0; s < SJ::SEGS; ++s) oj[s] = off_j[s];
+    if ((!IC || !JC) && l_k < KS) {                           // by rows, what is beyond the end of k lies inside the buffer
+#pragma unroll
+      for (int s = 0; s < SI::SEGS; ++s)
+        if (!IC && SI::byte(wave * SI::SEGS + s, lane) >= l_k * BYTES) oi[s] = 0xffffffffu;
+#pragma unroll
+      for (int s = 0; s < SJ::SEGS; ++s)
+        if (!JC && SJ::byte(wave * SJ::SEGS + s, lane) >= l_k * BYTES) oj[s] = 0xffffffffu;
+    }
+#pragma unroll
+    for (int s = 0; s < LOADS; ++s) {
+      if (s) meanwhile(s);
+      __builtin_amdgcn_sched_barrier(0);
+      if (s < SI::SEGS)
+        buffer_to_lds(ri, oi[s < SI::SEGS ? s : 0], l_to + to_i + s * 1024);
+      else
+        buffer_to_lds(rj, oj[s < SI::SEGS ? 0 : s - SI::SEGS], l_to + to_j + (s - SI::SEGS) * 1024);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    l_to = l_to == lds + (STAGES - 1) * STAGE ? lds : l_to + STAGE;
+    li.move(di);
+    lj.move(dj);
+    l_k -= KS;
+  };
 
   floatx4 acc[NI][NJ] = {};
   Fragment fi[4], fj[2][NJ];
   const int wi = wave % WI * (BI / WI), wj = wave / WI * (BJ / WJ);
-  const int steps = k_end > k0 ? (k_end - k0 + KS - 1) / KS : 0;
-  auto load = [&](int step) {                                  // to stage step & 1
-    const int k = k_end - k0 - step * KS;
-    const unsigned to = lds + (step & 1) * STAGE;
-    si.load(pi, to, wave, lane, IC ? k : k * BYTES);
-    sj.load(pj, to + SI::BYTES, wave, lane, JC ? k : k * BYTES);
-    pi += di;
-    pj += dj;
-  };
-  unsigned bi = SI::lane_base(wi, lane), bj = SJ::lane_base(wj, lane);
-  auto read_i = [&](int stage, int i) { SI::fragment(bi, lds + stage * STAGE, i, fi[i % 4]); };
+  const unsigned bi = SI::lane_base(wi, lane), bj = SJ::lane_base(wj, lane) + SI::BYTES;
+  unsigned at = lds, at_i = bi + at;                          // at: the stage that is read
+  auto read_i = [&](int i) { SI::fragment(at_i, i, fi[i % 4]); };
   auto read_j = [&](auto stage) {
+    const unsigned at_j = bj + at;
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) SJ::fragment(bj, lds + stage.value * STAGE + SI::BYTES, j, fj[stage.value][j]);
+    for (int j = 0; j < NJ; ++j) SJ::fragment(at_j, j, fj[stage.value][j]);
   };
-  auto step = [&](auto stage, int s) {
+  constexpr int MFMAS = (FP8 ? 1 : 2) * NJ;                   // of a block
+  auto multiply = [&](auto stage, int i, int m0, int m1) {
     constexpr int S = decltype(stage)::value;
-    asm volatile("" : "+v"(bi), "+v"(bj));                     // (addresses are made where they are used, not kept in registers throughout)
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int m = m0; m < m1; ++m) {
+      const int j = m % NJ, h = m / NJ;
+      if constexpr (FP8)
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fi[i % 4].all, fj[S][j].all, acc[i][j], 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
+      else
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fi[i % 4].h[h]), __builtin_bit_cast(bf16x8, fj[S][j].h[h]), acc[i][j], 0, 0, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto step = [&](auto stage) {
+    constexpr int S = decltype(stage)::value;
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-      if (i + 3 < NI) read_i(S, i + 3);
+      if (i + 3 < NI) read_i(i + 3);
       if (i == NI - 2) {
-        stage_barrier();
-        if (s + 2 < steps) load(s + 2);
-        read_j(std::integral_constant<int, S ^ 1>{});
-        read_i(S ^ 1, 0);
-        read_i(S ^ 1, 1);
-      }
-      if (i == NI - 1) read_i(S ^ 1, 2);
-      __builtin_amdgcn_sched_barrier(0);
-      if constexpr (FP8) {
-#pragma unroll
-        for (int j = 0; j < NJ; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fi[i % 4].all, fj[S][j].all, acc[i][j], 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
+        counted_barrier<(STAGES - 2) * LOADS>();
+        at = at == lds + (STAGES - 1) * STAGE ? lds : at + STAGE;
+        at_i = bi + at;
+        asm volatile("" : "+v"(at_i));                         // (a sum in a register: reads add constants to it)
+        load([&](int l) {
+          multiply(stage, i, l * MFMAS / LOADS, (l + 1) * MFMAS / LOADS);
+          if (l == 0) {
+            read_j(std::integral_constant<int, S ^ 1>{});
+            read_i(0);
+            read_i(1);
+          }
+        });
       } else {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int j = 0; j < NJ; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fi[i % 4].h[h]), __builtin_bit_cast(bf16x8, fj[S][j].h[h]),
-                                                                acc[i][j], 0, 0, 0);
+        if (i == NI - 1) read_i(2);
+        multiply(stage, i, 0, MFMAS);
       }
-      __builtin_amdgcn_sched_barrier(0);
     }
   };
   if (steps) {
-    load(0);
-    stage_barrier();
-    if (steps > 1) load(1);
+    auto nothing = [](int) {};
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s) load(nothing);
+    counted_barrier<(STAGES - 2) * LOADS>();
+    load(nothing);
     read_j(std::integral_constant<int, 0>{});
-    read_i(0, 0);
-    read_i(0, 1);
-    read_i(0, 2);
+    read_i(0);
+    read_i(1);
+    read_i(2);
     for (int s = 0; s < steps; s += 2) {
-      step(std::integral_constant<int, 0>{}, s);
-      if (s + 1 < steps) step(std::integral_constant<int, 1>{}, s + 1);
+      step(std::integral_constant<int, 0>{});
+      if (s + 1 < steps) step(std::integral_constant<int, 1>{});
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // (the last loads write to this workgroup's LDS)
   }
   unsigned char* out = a.out.data + (RAGGED ? (long long)expert * a.out_expert : 0);
   store_tile<FP8, F32OUT>(a, out, expert, i0 + wi, j0 + wj, j_end, acc);
 }
 
-template <bool FP8, bool IC, bool JC, bool RAGGED, bool F32OUT, int BI, int BJ, int WI, int WJ>
+template <bool FP8, bool IC, bool JC, bool RAGGED, bool F32OUT, int BI, int BJ, int WI, int WJ, int STAGES>
 __global__ __launch_bounds__(64 * WI * WJ, 2) void product_tile_kernel(ProductArgs a) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char product_lds[];
   int expert, ti, j0, j_end, k0, k_end;
@@ -505,16 +563,16 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void product_tile_kernel(ProductAr
     k0 = 0;
     k_end = expert < a.E ? a.nk : 0;
   }
-  tile_product<FP8, IC, JC, RAGGED, F32OUT, BI, BJ, WI, WJ>(a, product_lds, expert, ti * BI, j0, j_end, k0, k_end);
+  tile_product<FP8, IC, JC, RAGGED, F32OUT, BI, BJ, WI, WJ, STAGES>(a, product_lds, expert, ti * BI, j0, j_end, k0, k_end);
 }
 
-template <bool FP8, bool IC, bool JC, bool RAGGED, bool F32OUT, int BI, int BJ, int WI, int WJ>
+template <bool FP8, bool IC, bool JC, bool RAGGED, bool F32OUT, int BI, int BJ, int WI, int WJ, int STAGES>
 hipError_t go_tile(ProductArgs a, hipStream_t st) {
   a.tiles_i = (a.ni + BI - 1) / BI;
   a.tiles_j = (a.nj + BJ - 1) / BJ;
   const long long tiles = (RAGGED ? (long long)a.E * a.tiles_j : a.rows / BJ + a.E + 1) * a.tiles_i;     // (each expert and the rest may have one that is not full)
-  constexpr int bytes = 2 * (BI + BJ) * 128;
-  auto kernel = product_tile_kernel<FP8, IC, JC, RAGGED, F32OUT, BI, BJ, WI, WJ>;
+  constexpr int bytes = STAGES * (BI + BJ) * 128;
+  auto kernel = product_tile_kernel<FP8, IC, JC, RAGGED, F32OUT, BI, BJ, WI, WJ, STAGES>;
   static std::atomic<unsigned long long> allowed{0};
   const hipError_t e = allow_lds((const void*)kernel, bytes, allowed);
   if (e != hipSuccess) return e;
@@ -530,54 +588,21 @@ hipError_t go_tile(ProductArgs a, hipStream_t st) {
 //   X, before block 5: I of s + 1 has landed, I of s and J of s + 1 have been read by all -> J of s + 3
 // so each load has a step and a half (some 2 us) to arrive.  Behind a barrier MFMAs come first, loads and reads between them: all eight waves are at the
 // same place there, and whatever came before the MFMAs would leave the matrix cores idle.
-//
-// Loads go through buffers that end where the operand does: rows and k beyond come back as zeros, and nothing has to be clamped or counted apart.  The
-// loop over a tile's steps has no branch but that at a tile's end: past the last tile the loads read an empty buffer.
+// The loop over a tile's steps has no branch but that at a tile's end.
 constexpr int kUnit = 32768, kUnits = 5;
-typedef int intx4 __attribute__((ext_vector_type(4)));
 
-__device__ __forceinline__ void buffer_to_lds(intx4 rsrc, unsigned off, unsigned to) {                  // 64 x 16 bytes to 1 KiB
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(rsrc), "s"(to) : "memory");
-}
-// All but the youngest 8 loads of the wave (two units') have landed and every read has been answered; then all waves' have.  stored: a tile's stores
-// are younger than the unit that is waited for too (memory operations are counted off in the order they were issued in).
+// The barriers X and Y: all but the youngest 8 loads of the wave, two units', have landed.  stored: a tile's stores are younger than what is waited for, too.
 constexpr int kTileStores = 32;
 __device__ __forceinline__ void unit_barrier(bool stored) {
-  __builtin_amdgcn_sched_barrier(0);
-#ifdef LASNET_DRAIN_AT_BARRIERS
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-#else
   if (stored)
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(8 + kTileStores) : "memory");
+    counted_barrier<8 + kTileStores>();
   else
-    asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-#endif
-  __builtin_amdgcn_sched_barrier(0);
-}
-
-typedef __amdgpu_buffer_rsrc_t product_rsrc_t;
-__device__ __forceinline__ product_rsrc_t product_rsrc(const void* p, unsigned bytes) {
-  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)(size_t)p), hi = __builtin_amdgcn_readfirstlane((unsigned)((size_t)p >> 32));
-  return __builtin_amdgcn_make_buffer_rsrc((void*)(((unsigned long long)hi << 32) | lo), 0, (int)__builtin_amdgcn_readfirstlane(bytes), 0x00020000);
+    counted_barrier<8>();
 }
 
 // A tile with a reduction.
 struct TileWork {
   int expert, i0, j0, j_end, k0, k_end, steps;
-};
-
-// Where an operand's loads are: the tile at the next step's k, and how many bytes of the operand there are from there on.
-struct Walk {
-  const unsigned char* at;
-  long long bytes;
-  __device__ __forceinline__ void move(long long by) {
-    at += by;
-    bytes -= by;
-  }
-  __device__ __forceinline__ intx4 rsrc() const {
-    const unsigned n = bytes <= 0 ? 0u : bytes > 0xffffffffll ? 0xffffffffu : (unsigned)bytes;
-    return intx4{(int)(unsigned)(size_t)at, (int)((size_t)at >> 32 & 0xffff), (int)n, 0x00020000};
-  }
 };
 
 // The wave's 128 x 64 of a tile: scaled, rounded, stored through a buffer that ends with the tile's last row.  Always kTileStores stores (by hand: they are
@@ -588,7 +613,8 @@ __device__ __forceinline__ void store_big_tile(const ProductArgs& a, unsigned ch
   asm volatile("" : "+v"(lane));
   const unsigned pitch = (unsigned)a.out.pitch;
   const int rows = t.j_end - t.j0 < 256 ? t.j_end - t.j0 : 256;
-  const intx4 to = Walk{out + (long long)t.j0 * a.out.pitch + (long long)t.i0 * OB, (long long)(rows - 1) * a.out.pitch + (long long)(a.ni - t.i0) * OB}.rsrc();
+  const unsigned long long first = (unsigned long long)(out + (long long)t.j0 * a.out.pitch + (long long)t.i0 * OB);
+  const intx4 to = {(int)(unsigned)first, (int)(unsigned)(first >> 32), (int)((unsigned)(rows - 1) * pitch + (unsigned)(a.ni - t.i0) * OB), 0x00020000};
   const float floor = a.relu ? 0.f : -INFINITY;               // (NaN passes)
   // the scales of the wave's 64 rows and 128 columns, one and two a lane, all asked for before the first store
   float row_scale = 1.f, col_scale[2] = {1.f, 1.f};
@@ -767,52 +793,60 @@ __global__ __launch_bounds__(512, 2) void product_stream_kernel(ProductArgs a) {
   }
 
   // ---- loads ----
-  const long long di = IC ? KS * a.I.pitch : 128, dj = JC ? KS * a.J.pitch : 128;
+  const unsigned pitch_i = (unsigned)a.I.pitch, pitch_j = (unsigned)a.J.pitch, kb = (unsigned)a.nk * BYTES;
+  const unsigned di = IC ? KS * pitch_i : 128, dj = JC ? KS * pitch_j : 128;
   // Of this lane's first piece of a unit from the tile.  The next lies a segment's rows further with bit 6 of its byte turned over (both kinds of tile: the
   // bit is bit 2 of the lane), the other two likewise two segments further.
-  unsigned off_i = (unsigned)SI::row(wave * 4, lane) * (unsigned)a.I.pitch + (unsigned)SI::byte(wave * 4, lane);
-  unsigned off_j = (unsigned)SJ::row(wave * 4, lane) * (unsigned)a.J.pitch + (unsigned)SJ::byte(wave * 4, lane);
-  auto walk_i = [&](const TileWork& w) {
-    Walk v;
-    v.at = a.I.data + (RAGGED ? 0 : (long long)w.expert * a.i_expert) + (IC ? (long long)w.k0 * a.I.pitch + (long long)w.i0 * BYTES : (long long)w.i0 * a.I.pitch);
-    v.bytes = IC ? (long long)(w.k_end - w.k0 - 1) * a.I.pitch + (long long)(a.ni - w.i0) * BYTES : (long long)(a.ni - w.i0 - 1) * a.I.pitch + (long long)a.nk * BYTES;
+  unsigned off_i = (unsigned)SI::row(wave * 4, lane) * pitch_i + (unsigned)SI::byte(wave * 4, lane);
+  unsigned off_j = (unsigned)SJ::row(wave * 4, lane) * pitch_j + (unsigned)SJ::byte(wave * 4, lane);
+  auto feed_i = [&](const TileWork& w) {
+    Feed<IC> v;
+    v.start(a.I.data + (RAGGED ? 0 : (long long)w.expert * a.i_expert) + (IC ? (long long)w.k0 * a.I.pitch + (long long)w.i0 * BYTES : (long long)w.i0 * a.I.pitch),
+            a.ni - w.i0, 256, a.I.pitch, IC ? (unsigned)(a.ni - w.i0) * BYTES : kb);
     return v;
   };
-  auto walk_j = [&](const TileWork& w) {
-    Walk v;
-    v.at = a.J.data + (JC ? (long long)w.k0 * a.J.pitch + (long long)w.j0 * BYTES : (long long)w.j0 * a.J.pitch);
-    v.bytes = JC ? (long long)(w.k_end - w.k0 - 1) * a.J.pitch + (long long)(w.j_end - w.j0) * BYTES
-                 : (long long)(w.j_end - w.j0 - 1) * a.J.pitch + (long long)a.nk * BYTES;
+  auto feed_j = [&](const TileWork& w) {
+    Feed<JC> v;
+    v.start(a.J.data + (JC ? (long long)w.k0 * a.J.pitch + (long long)w.j0 * BYTES : (long long)w.j0 * a.J.pitch), w.j_end - w.j0, 256, a.J.pitch,
+            JC ? (unsigned)(w.j_end - w.j0) * BYTES : kb);
     return v;
   };
-  Walk li, lj, ni, nj;                                        // of the tile being loaded, and of the one after the tile being computed
-  int l_k = 0, l_steps = 0, n_k = 0, n_steps = 0;             // its k and steps left (an empty tile's: no end)
+  Feed<IC> li, ni;                                            // of the tile being loaded, and of the one after the tile being computed
+  Feed<JC> lj, nj;
+  int l_k = 0, l_steps = 0, n_k = 0, n_steps = 0;             // its k and steps left (past the last tile: no k)
   unsigned l_to = lds;
-  auto turn_slot = [&](unsigned& s) { s = s == lds + (kUnits - 1) * kUnit ? lds : s + kUnit; };
+  const unsigned mine = lds + (kUnits - 1) * kUnit;           // the last unit
+  auto turn_slot = [&](unsigned& s) { s = s == mine ? lds : s + kUnit; };
   auto nothing = [](int) {};
   // A unit of the load step, between the parts of `meanwhile` (which does what is due anyway, in four parts).
   auto issue = [&](auto j, auto meanwhile) {
     constexpr bool J = decltype(j)::value, C = J ? JC : IC;
-    const intx4 rsrc = (J ? lj : li).rsrc();
+    meanwhile(0);
+    intx4 rsrc;
+    if constexpr (J) rsrc = lj.rsrc(l_k, pitch_j);
+    else rsrc = li.rsrc(l_k, pitch_i);
     unsigned o[4];
 #pragma unroll
     for (int s = 0; s < 4; ++s)
-      o[s] = (J ? off_j : off_i) + (s & 1 ? 64u - ((unsigned)lane & 4) * 32 : 0u) + (unsigned)(s * (C ? 2 : 8)) * (unsigned)(J ? a.J.pitch : a.I.pitch);
-    if (!C && l_k < KS) {                                     // by rows, what is beyond the end of k lies inside the buffer
+      o[s] = (J ? off_j : off_i) + (s & 1 ? 64u - ((unsigned)lane & 4) * 32 : 0u) + (unsigned)(s * (C ? 2 : 8)) * (J ? pitch_j : pitch_i);
+    if (!FP8 && !C && l_k < KS) {                             // by rows, what is beyond the end of k lies inside the buffer (e4m3: whole steps only, registers lack for more)
 #pragma unroll
       for (int s = 0; s < 4; ++s)
         if ((J ? SJ::byte(wave * 4 + s, lane) : SI::byte(wave * 4 + s, lane)) >= l_k * BYTES) o[s] = 0xffffffffu;
     }
+    const unsigned to = l_to + wave * 4096;
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-      meanwhile(s);
+      if (s) meanwhile(s);
       __builtin_amdgcn_sched_barrier(0);
-      buffer_to_lds(rsrc, o[s], l_to + (wave * 4 + s) * 1024);
+      buffer_to_lds(rsrc, o[s], to + s * 1024);
       __builtin_amdgcn_sched_barrier(0);
     }
     turn_slot(l_to);
-    (J ? lj : li).move(J ? dj : di);
-    if constexpr (!J) {
+    if constexpr (J) {
+      lj.move(dj);
+    } else {
+      li.move(di);
       l_k -= KS;
       if (--l_steps == 0) {
         li = ni;
@@ -827,14 +861,12 @@ __global__ __launch_bounds__(512, 2) void product_stream_kernel(ProductArgs a) {
   // The next step's J fragments 2 and 3 take the place of this step's as the last block is done with them (every block begins with these two); 0 and 1
   // are held twice in bf16, and follow 2 and 3 in e4m3, whose fragments are whole octets of registers and leave no room for that.
   Fragment fi[4], fj[PAIR][2], fj2[2];
-  unsigned bi = SI::lane_base(wi, lane), bj = SJ::lane_base(wj, lane);
+  const unsigned bi = SI::lane_base(wi, lane), bj = SJ::lane_base(wj, lane);
   unsigned c_j = lds, c_i = lds + kUnit;                      // the units that J and I fragments are read from
-  auto next_unit = [&](unsigned& c) {
-    turn_slot(c);
-    turn_slot(c);
-  };
-  auto read_i = [&](int i) { SI::fragment(bi, c_i, i, fi[i % 4]); };
-  auto read_j = [&](auto stage, int j) { SJ::fragment(bj, c_j, j, j < 2 ? fj[stage.value][j] : fj2[j - 2]); };
+  unsigned at_i = bi + c_i;
+  auto next_unit = [&](unsigned& c) { c = c >= mine - kUnit ? c - 3 * kUnit : c + 2 * kUnit; };
+  auto read_i = [&](int i) { SI::fragment(at_i, i, fi[i % 4]); };
+  auto read_j = [&](auto stage, int j) { SJ::fragment(bj + c_j, j, j < 2 ? fj[stage.value][j] : fj2[j - 2]); };
   auto multiply = [&](auto stage, int i, int part) {          // a quarter of block i's MFMAs
     constexpr int S = decltype(stage)::value;
     __builtin_amdgcn_sched_barrier(0);
@@ -854,8 +886,7 @@ __global__ __launch_bounds__(512, 2) void product_stream_kernel(ProductArgs a) {
   auto step = [&](auto stage) {
     constexpr int S = decltype(stage)::value;
     constexpr auto next = std::integral_constant<int, (S + 1) % PAIR>{};
-    // (addresses are made where they are used, not kept in registers throughout)
-    asm volatile("" : "+v"(bi), "+v"(bj), "+v"(off_i), "+v"(off_j));
+    asm volatile("" : "+v"(off_i), "+v"(off_j));               // (what follows from them is made where it is used, not kept in registers throughout)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       if (i == 1) {                                           // Y
@@ -870,6 +901,8 @@ __global__ __launch_bounds__(512, 2) void product_stream_kernel(ProductArgs a) {
       } else if (i == 5) {                                    // X
         unit_barrier(young > 0);
         next_unit(c_i);
+        at_i = bi + c_i;
+        asm volatile("" : "+v"(at_i));                         // (a sum in a register: reads add constants to it)
         issue(std::true_type{}, [&](int p) {
           multiply(stage, 5, p);
           if (p == 0) read_i(0);
@@ -893,11 +926,12 @@ __global__ __launch_bounds__(512, 2) void product_stream_kernel(ProductArgs a) {
   int round = 0;
   TileWork w = next_work(round);
   if (round * stride < end) {
-    li = walk_i(w);
-    lj = walk_j(w);
+    li = feed_i(w);
+    lj = feed_j(w);
     l_k = w.k_end - w.k0;
     l_steps = w.steps;
-    ni = nj = Walk{a.J.data, 0};
+    ni = li;
+    nj = lj;
     issue(std::true_type{}, nothing);
     issue(std::false_type{}, nothing);
     issue(std::true_type{}, nothing);
@@ -913,13 +947,12 @@ __global__ __launch_bounds__(512, 2) void product_stream_kernel(ProductArgs a) {
       const TileWork after = next_work(round);
       const bool more = round * stride < end;
       if (more) {
-        ni = walk_i(after);
-        nj = walk_j(after);
+        ni = feed_i(after);
+        nj = feed_j(after);
         n_k = after.k_end - after.k0;
         n_steps = after.steps;
       } else {
-        ni = nj = Walk{a.J.data, 0};
-        n_k = 1 << 30;
+        n_k = 0;
         n_steps = 0;
       }
       clear();
@@ -939,7 +972,7 @@ __global__ __launch_bounds__(512, 2) void product_stream_kernel(ProductArgs a) {
     const int i0 = v.i0 + (q & 1) * 128, j0 = v.j0 + (q >> 1 & 1) * 128;
     if (i0 >= a.ni || j0 >= v.j_end) continue;
     __syncthreads();
-    tile_product<FP8, IC, JC, RAGGED, F32OUT, 128, 128, 2, 4>(a, product_lds, v.expert, i0, j0, v.j_end, v.k0, v.k_end);
+    tile_product<FP8, IC, JC, RAGGED, F32OUT, 128, 128, 2, 4, 4>(a, product_lds, v.expert, i0, j0, v.j_end, v.k0, v.k_end);
   }
 }
 
@@ -952,6 +985,80 @@ hipError_t go_stream(ProductArgs a, hipStream_t st) {
   const hipError_t e = allow_lds((const void*)kernel, kUnits * kUnit, allowed);
   if (e != hipSuccess) return e;
   kernel<<<dim3(256), dim3(512), kUnits * kUnit, st>>>(a);
+  return hipGetLastError();
+}
+
+// ---- few rows an expert: bound by reading the weights once ----
+// A workgroup takes 16 columns and up to 16 NJ rows of an expert.  Its four waves share the reduction, each a quarter of it, and read their weights straight into
+// registers (nothing is used twice), DEPTH steps of 128 bytes ahead; the quarters' sums are added in order through LDS.
+template <bool FP8, int NJ>
+__global__ __launch_bounds__(256) void product_few_kernel(ProductArgs a) {
+  constexpr int BYTES = FP8 ? 1 : 2, DEPTH = NJ == 1 ? 8 : NJ == 2 ? 4 : 2;
+  constexpr unsigned NONE = 0xffffffffu;
+  __shared__ floatx4 sums[3][NJ][64];
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int ti = (int)(blockIdx.x % a.tiles_i), i0 = ti * 16;
+  int expert, j0, j_end;
+  if (!find_rows<16 * NJ>(a, (int)(blockIdx.x / a.tiles_i), expert, j0, j_end)) return;
+  expert = __builtin_amdgcn_readfirstlane(expert);
+  j0 = __builtin_amdgcn_readfirstlane(j0);
+  j_end = __builtin_amdgcn_readfirstlane(j_end);
+  floatx4 acc[NJ] = {};
+  if (expert < a.E) {
+    const unsigned kb = (unsigned)a.nk * BYTES;
+    const int rows = j_end - j0 < 16 * NJ ? j_end - j0 : 16 * NJ, cols = a.ni - i0 < 16 ? a.ni - i0 : 16;
+    const product_rsrc_t I = product_rsrc(a.I.data + (long long)expert * a.i_expert + (long long)i0 * a.I.pitch, (unsigned)(cols - 1) * (unsigned)a.I.pitch + kb);
+    const product_rsrc_t J = product_rsrc(a.J.data + (long long)j0 * a.J.pitch, (unsigned)(rows - 1) * (unsigned)a.J.pitch + kb);
+    const int steps = (int)((kb + 127) / 128), mine = (steps + 3) / 4;
+    unsigned k = (unsigned)(wave * mine) * 128 + (lane >> 4) * 32;            // this lane's 32 bytes of a step
+    const unsigned k_end = (unsigned)(wave + 1) * mine * 128 < kb ? (unsigned)(wave + 1) * mine * 128 : kb;
+    // (rows and columns beyond the last lie beyond the buffers: zeros)
+    const unsigned at_i = (unsigned)(lane & 15) * (unsigned)a.I.pitch, at_j = (unsigned)(lane & 15) * (unsigned)a.J.pitch;
+    Fragment fi[DEPTH], fj[DEPTH][NJ];
+    auto fetch = [&](int d) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const bool there = k + h * 16 < k_end;
+        fi[d].h[h] = __builtin_bit_cast(uint4_t, __builtin_amdgcn_raw_buffer_load_b128(I, (int)(there ? at_i + k + h * 16 : NONE), 0, 0));
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+          fj[d][j].h[h] = __builtin_bit_cast(uint4_t, __builtin_amdgcn_raw_buffer_load_b128(
+                                                          J, (int)(there ? at_j + (unsigned)(16 * j) * (unsigned)a.J.pitch + k + h * 16 : NONE), 0, 0));
+      }
+      k += 128;
+    };
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) fetch(d);
+    for (int s = 0; s < mine; s += DEPTH)
+#pragma unroll
+      for (int d = 0; d < DEPTH; ++d) {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+          if constexpr (FP8)
+            acc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fi[d].all, fj[d][j].all, acc[j], 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
+          else
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fi[d].h[h]), __builtin_bit_cast(bf16x8, fj[d][j].h[h]), acc[j], 0, 0, 0);
+        fetch(d);
+      }
+  }
+  if (wave)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) sums[wave - 1][j][lane] = acc[j];
+  __syncthreads();
+  if (wave) return;
+  floatx4 whole[1][NJ];
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) whole[0][j] = ((acc[j] + sums[0][j][lane]) + sums[1][j][lane]) + sums[2][j][lane];
+  store_tile<FP8, false>(a, a.out.data, expert, i0, j0, j_end, whole);
+}
+
+template <bool FP8, int NJ>
+hipError_t go_few(ProductArgs a, hipStream_t st) {
+  a.tiles_i = (a.ni + 15) / 16;
+  const long long groups = a.rows / (16 * NJ) + (a.rows < a.E ? a.rows : a.E) + 1;       // (experts with rows, one that is not full each, and the rest)
+  product_few_kernel<FP8, NJ><<<dim3((unsigned)(groups * a.tiles_i)), dim3(256), 0, st>>>(a);
   return hipGetLastError();
 }
 
@@ -970,12 +1077,24 @@ bool whole(const ProductArgs& a, int bytes, int B) {
 template <bool FP8, bool IC, bool JC, bool RAGGED, bool F32OUT>
 hipError_t go(ProductArgs a, hipStream_t st) {
   if (whole<IC, JC>(a, FP8 ? 1 : 2, 256)) {
-    const long long big = (RAGGED ? (long long)a.E * ((a.nj + 255) / 256) : a.rows / 256 + a.E / 2) * ((a.ni + 255) / 256);
-    const bool long_enough = RAGGED || (long long)a.nk * (FP8 ? 1 : 2) > 384;
+    if constexpr (!IC && !RAGGED) {
+      if (a.rows <= 64) {
+        const long long each = a.rows / a.E;
+        return a.rows <= 16 || each <= 8 ? go_few<FP8, 1>(a, st) : a.rows <= 32 || each <= 16 ? go_few<FP8, 2>(a, st) : go_few<FP8, 4>(a, st);
+      }
+    }
+    const long long wide = (a.ni + 255) / 256, groups = a.rows < a.E ? a.rows : a.E;
+    const long long big = (RAGGED ? (long long)a.E * ((a.nj + 255) / 256) : a.rows / 256 + groups / 2) * wide;
+    const bool long_enough = RAGGED || (FP8 ? a.nk > 384 && a.nk % 128 == 0 : a.nk > 192);
     if (big >= 256 && long_enough && a.ni % 4 == 0 && !(((unsigned long long)a.out.data | (unsigned long long)a.out.pitch | (unsigned long long)a.out_expert) & 15) &&
         a.out.pitch < (1ll << 31) / 256)
       return go_stream<FP8, IC, JC, RAGGED, F32OUT>(a, st);
-    return go_tile<FP8, IC, JC, RAGGED, F32OUT, 128, 128, 2, 2>(a, st);
+#ifndef FOUR
+#define FOUR 256
+#endif
+    const long long tiles = (RAGGED ? (long long)a.E * ((a.nj + 127) / 128) : a.rows / 128 + groups / 2) * ((a.ni + 127) / 128);
+    if (tiles <= FOUR) return go_tile<FP8, IC, JC, RAGGED, F32OUT, 128, 128, 2, 4, 4>(a, st);
+    return go_tile<FP8, IC, JC, RAGGED, F32OUT, 128, 128, 2, 2, 2>(a, st);
   }
   a.tiles_i = (a.ni + 127) / 128;
   a.tiles_j = (a.nj + 127) / 128;
