@@ -37,6 +37,11 @@ EXPORTS = (
 )
 
 
+# the calls on rows that _marshal takes
+_ROW_CALLS = ("norm_rows", "norm_rows_backward", "route", "dispatch_rows", "combine_rows", "combine_rows_backward", "expert_product",
+              "expert_product_dx", "expert_product_dw")
+
+
 class LasnetError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -122,12 +127,16 @@ def load_library(path: str) -> ctypes.CDLL:
         ctypes.cast(f, vp).value for f in (L.lasnet_masker_ex, L.lasnet_sparse_bottleneck_ex, L.lasnet_dense_bottleneck,
                                            L.lasnet_sparse_bottleneck_packed, L.lasnet_sparse_bottleneck_planned,
                                            L.lasnet_packed_weights_bytes))
+    for name in _ROW_CALLS:
+        setattr(L, "at_" + name, ctypes.cast(getattr(L, "lasnet_" + name), vp).value)
     return L
 
 
 class _AllThroughCtypes:
     """In place of the native marshalling where it does not load: no call is of its form."""
     masker_ex = block_ex = block_dense = block_packed = block_planned = staticmethod(lambda *args: None)
+    norm_rows = norm_rows_backward = route = dispatch_rows = combine_rows = combine_rows_backward = masker_ex
+    expert_product = expert_product_dx = expert_product_dw = masker_ex
 
 
 def _load_marshal() -> None:
@@ -536,6 +545,13 @@ def lasnet_norm_rows(x: torch.Tensor, weight: torch.Tensor, eps: float, residual
                      out_dtype: Optional[torch.dtype] = None, stream=None):
     """(out, scale, sum_out): out = s / rms(s) * weight with s = x + residual.  out_dtype (where out is not given): x's, or
     torch.float8_e4m3fn; scale: of 8-bit rows, else None.  sum_out = s, made where there is a residual.  rstd [rows] float32: written where given."""
+    if (stream is None and out is not None and out_dtype is None and (sum_out is not None or residual is None)
+            and (scale is not None or out.dtype != torch.float8_e4m3fn)):
+        L = lib()
+        st = _marshal.norm_rows(L.at_norm_rows, x, weight, eps, residual, out, scale, sum_out, rstd)
+        if st is not None:
+            _check(st, "lasnet_norm_rows")
+            return out, scale, sum_out
     d = _rows(x, "x")
     if out is None:
         out = torch.empty(x.shape, dtype=out_dtype or x.dtype, device=x.device)
@@ -556,6 +572,14 @@ def lasnet_norm_rows_backward(dy: torch.Tensor, s: torch.Tensor, weight: torch.T
                               dsum: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None,
                               dweight: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
     """(dx, dweight) from the gradient dy of lasnet_norm_rows' out and dsum of its sum; s, rstd: as the forward call wrote them."""
+    if stream is None and dx is not None and dweight is not None:
+        L = lib()
+        cols = s.shape[-1]
+        need = L.lasnet_norm_rows_backward_workspace_bytes(s.numel() // cols, cols) if cols and workspace is None else 0
+        st = _marshal.norm_rows_backward(L.at_norm_rows_backward, dy, s, weight, rstd, dsum, dx, dweight, _workspace(workspace, need, s.device, None)[2])
+        if st is not None:
+            _check(st, "lasnet_norm_rows_backward")
+            return dx, dweight
     y, d, g = _rows(dy, "dy"), _rows(s, "s"), _rows(dsum, "dsum")
     if dx is None:
         dx = torch.empty(s.shape, dtype=s.dtype, device=s.device)
@@ -573,6 +597,13 @@ def lasnet_norm_rows_backward(dy: torch.Tensor, s: torch.Tensor, weight: torch.T
 def lasnet_route(experts: torch.Tensor, E: int, offsets: Optional[torch.Tensor] = None, order: Optional[torch.Tensor] = None,
                  position: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
     """(offsets [E+1], order [tokens*k], position [tokens,k]), int32, of experts int32 [tokens,k] (outside [0,E): not sent)."""
+    if stream is None and offsets is not None and order is not None and position is not None:
+        L = lib()
+        need = L.lasnet_route_workspace_bytes(experts.shape[0], experts.shape[1], E) if workspace is None and experts.dim() == 2 else 0
+        st = _marshal.route(L.at_route, experts, E, offsets, order, position, _workspace(workspace, need, experts.device, None)[2])
+        if st is not None:
+            _check(st, "lasnet_route")
+            return offsets, order, position
     if experts.dim() != 2 or experts.dtype != torch.int32 or not experts.is_cuda or not experts.is_contiguous():
         raise ValueError("experts must be a contiguous int32 device tensor [tokens, k]")
     tokens, k = experts.shape
@@ -605,6 +636,12 @@ def _offsets(offsets: torch.Tensor) -> int:
 def lasnet_dispatch_rows(x: torch.Tensor, position: torch.Tensor, offsets: torch.Tensor, scale: Optional[torch.Tensor] = None,
                          out: Optional[torch.Tensor] = None, out_scale: Optional[torch.Tensor] = None, stream=None):
     """(out [tokens*k, cols], out_scale): out[position[t, j]] = x[t], zeros where no expert has a row; the scales of 8-bit rows go along."""
+    if stream is None and out is not None and (out_scale is not None or scale is None):
+        L = lib()
+        st = _marshal.dispatch_rows(L.at_dispatch_rows, x, position, offsets, scale, out, out_scale)
+        if st is not None:
+            _check(st, "lasnet_dispatch_rows")
+            return out, out_scale
     tokens, k = _slots(position)
     E, d = _offsets(offsets), _rows(x, "x")
     if d.rows != tokens:
@@ -623,6 +660,12 @@ def lasnet_dispatch_rows(x: torch.Tensor, position: torch.Tensor, offsets: torch
 def lasnet_combine_rows(y: torch.Tensor, position: torch.Tensor, weights: Optional[torch.Tensor] = None,
                         base: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """out[t] = base[t] + sum_j weights[t, j] * y[position[t, j]] over the slots that were sent."""
+    if stream is None and out is not None:
+        L = lib()
+        st = _marshal.combine_rows(L.at_combine_rows, y, position, weights, base, out)
+        if st is not None:
+            _check(st, "lasnet_combine_rows")
+            return out
     tokens, k = _slots(position)
     d, b = _rows(y, "y"), _rows(base, "base")
     if out is None:
@@ -640,6 +683,12 @@ def lasnet_combine_rows_backward(dout: torch.Tensor, y: torch.Tensor, position: 
                                  weights: Optional[torch.Tensor] = None, dy: Optional[torch.Tensor] = None,
                                  dweights: Optional[torch.Tensor] = None, stream=None):
     """(dy, dweights [tokens, k]) of lasnet_combine_rows; that of base is dout."""
+    if stream is None and dy is not None and dweights is not None:
+        L = lib()
+        st = _marshal.combine_rows_backward(L.at_combine_rows_backward, dout, y, position, offsets, weights, dy, dweights)
+        if st is not None:
+            _check(st, "lasnet_combine_rows_backward")
+            return dy, dweights
     tokens, k = _slots(position)
     E, d, v = _offsets(offsets), _rows(dout, "dout"), _rows(y, "y")
     if d.rows != tokens:
@@ -665,6 +714,12 @@ def _matrices(W: torch.Tensor, E: int, n: int, k: int, *dtypes) -> Optional[int]
 def lasnet_expert_product(x: torch.Tensor, offsets: torch.Tensor, W: torch.Tensor, scale: Optional[torch.Tensor] = None,
                           wscale: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, flags: int = 0, stream=None) -> torch.Tensor:
     """out[p] = W[e] x[p] for the rows p of each expert e (W [E, n, cols]); bfloat16, or e4m3 with scale [rows], wscale [E, n]."""
+    if stream is None and out is not None:
+        L = lib()
+        st = _marshal.expert_product(L.at_expert_product, x, offsets, W, scale, wscale, out, flags)
+        if st is not None:
+            _check(st, "lasnet_expert_product")
+            return out
     E, d = _offsets(offsets), _rows(x, "x")
     if W.dim() != 3:
         raise ValueError("the experts' matrices are [E, n, cols]")
@@ -683,6 +738,12 @@ def lasnet_expert_product(x: torch.Tensor, offsets: torch.Tensor, W: torch.Tenso
 
 def lasnet_expert_product_dx(dy: torch.Tensor, offsets: torch.Tensor, W: torch.Tensor, dx: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """dx[p] = W[e]^T dy[p]."""
+    if stream is None and dx is not None:
+        L = lib()
+        st = _marshal.expert_product_dx(L.at_expert_product_dx, dy, offsets, W, dx)
+        if st is not None:
+            _check(st, "lasnet_expert_product_dx")
+            return dx
     E, d = _offsets(offsets), _rows(dy, "dy")
     if W.dim() != 3:
         raise ValueError("the experts' matrices are [E, n, cols]")
@@ -697,6 +758,12 @@ def lasnet_expert_product_dx(dy: torch.Tensor, offsets: torch.Tensor, W: torch.T
 def lasnet_expert_product_dw(dy: torch.Tensor, x: torch.Tensor, offsets: torch.Tensor, dW: Optional[torch.Tensor] = None,
                              dtype: Optional[torch.dtype] = None, stream=None) -> torch.Tensor:
     """dW[e] = sum over the rows p of expert e of dy[p] x[p]^T; dW [E, n, cols] in bfloat16 (or dtype: float32)."""
+    if stream is None and dW is not None and dtype is None:
+        L = lib()
+        st = _marshal.expert_product_dw(L.at_expert_product_dw, dy, x, offsets, dW)
+        if st is not None:
+            _check(st, "lasnet_expert_product_dw")
+            return dW
     E, d, v = _offsets(offsets), _rows(dy, "dy"), _rows(x, "x")
     if dW is None:
         dW = torch.empty((E, d.cols, v.cols), dtype=dtype or x.dtype, device=x.device)

@@ -69,6 +69,66 @@ struct Plain {                                       // false from any of these:
     if (PyFloat_CheckExact(o)) return (float)PyFloat_AS_DOUBLE(o);
     return (float)integer(o);
   }
+  // rows: dense in two dimensions, apart or not; of more dimensions contiguous
+  void rows(PyObject* o, lasnet_rows& d) {
+    const at::Tensor* t = tensor(o);
+    if (!need(t && t->defined() && t->dim() >= 2 && t->is_cuda())) return;
+    const auto ty = t->scalar_type();
+    if (!need(ty == at::kFloat || ty == at::kBFloat16 || ty == at::ScalarType::Float8_e4m3fn)) return;
+    const int64_t cols = t->size(-1);
+    if (!need(cols > 0 && cols <= INT32_MAX)) return;
+    d.rows = t->numel() / cols;
+    d.cols = (int32_t)cols;
+    d.stride = cols;
+    if (!t->is_contiguous()) {
+      if (!need(t->dim() == 2 && (cols == 1 || t->stride(1) == 1))) return;
+      if (d.rows > 1) {
+        d.stride = t->stride(0);
+        need(d.stride >= cols);
+      }
+    }
+    d.data = t->data_ptr();
+    d.dtype = ty == at::kFloat ? LASNET_F32 : ty == at::kBFloat16 ? LASNET_BF16 : LASNET_E4M3;
+  }
+  const lasnet_rows* rows_or_none(PyObject* o, lasnet_rows& d) {
+    if (o == Py_None) return nullptr;
+    rows(o, d);
+    return &d;
+  }
+  // a dense tensor of so many elements, or None
+  template <class T>
+  T* dense(PyObject* o, at::ScalarType ty, int64_t n) {
+    if (o == Py_None || !ok) return nullptr;
+    T* t = of_type<T>(o, ty);
+    return ok && need(tensor(o)->numel() == n) ? t : nullptr;
+  }
+  template <class T>
+  T* scale(PyObject* o, int64_t n) {
+    if (o == Py_None || !ok) return nullptr;
+    const at::Tensor* t = tensor(o);
+    if (!need(t && t->defined())) return nullptr;
+    return dense<T>(o, t->scalar_type() == at::kByte ? at::kByte : at::ScalarType::Float8_e8m0fnu, n);
+  }
+  // [tokens, k]
+  const int32_t* slots(PyObject* o, int64_t& tokens, int& k) {
+    const int32_t* p = of_type<const int32_t>(o, at::kInt);
+    if (!ok || !need(tensor(o)->dim() == 2 && tensor(o)->size(1) <= INT32_MAX)) return nullptr;
+    tokens = tensor(o)->size(0);
+    k = (int)tensor(o)->size(1);
+    return p;
+  }
+  // [E + 1]
+  const int32_t* offsets(PyObject* o, int& E) {
+    const int32_t* p = of_type<const int32_t>(o, at::kInt);
+    if (!ok || !need(tensor(o)->dim() == 1 && tensor(o)->numel() >= 2 && tensor(o)->numel() <= INT32_MAX)) return nullptr;
+    E = (int)tensor(o)->numel() - 1;
+    return p;
+  }
+  void* matrices(PyObject* o, int64_t E, int64_t n, int64_t k, at::ScalarType ty) {
+    const at::Tensor* t = tensor(o);
+    const int64_t shape[3] = {E, n, k};
+    return need(t && t->defined() && t->scalar_type() == ty && t->is_cuda() && t->is_contiguous() && t->sizes() == at::IntArrayRef(shape, 3)) ? t->data_ptr() : nullptr;
+  }
   // the list: storage for every cell of the map (the kernels may read entries past the count)
   void list(PyObject* idx, PyObject* count, const lasnet_tensor& x, int S, const int32_t*& i, const int32_t*& c) {
     i = c = nullptr;
@@ -227,7 +287,188 @@ PyObject* block_dense(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// (x, weight, eps, residual, out, scale, sum_out, rstd)
+PyObject* norm_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 9, [&](Plain& p) {
+    lasnet_rows x, res, out, sum;
+    p.rows(a[1], x);
+    if (!p.ok) return 0;
+    const float* weight = p.dense<const float>(a[2], at::kFloat, x.cols);
+    const float eps = p.real(a[3]);
+    const lasnet_rows *r = p.rows_or_none(a[4], res), *s = p.rows_or_none(a[7], sum);
+    p.rows(a[5], out);
+    uint8_t* scale = p.scale<uint8_t>(a[6], x.rows);
+    float* rstd = p.dense<float>(a[8], at::kFloat, x.rows);
+    if (!p.ok) return 0;
+    auto* f = entry<decltype(lasnet_norm_rows)>(a[0]);
+    ENQUEUE(f(&x, r, weight, eps, s, &out, scale, rstd, st));
+  });
+}
+
+// (dy, s, weight, rstd, dsum, dx, dweight, workspace)
+PyObject* norm_rows_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 9, [&](Plain& p) {
+    lasnet_rows dy, s, sum, dx;
+    p.rows(a[1], dy);
+    p.rows(a[2], s);
+    if (!p.ok) return 0;
+    const float* weight = p.dense<const float>(a[3], at::kFloat, s.cols);
+    const float* rstd = p.dense<const float>(a[4], at::kFloat, s.rows);
+    const lasnet_rows* dsum = p.rows_or_none(a[5], sum);
+    p.rows(a[6], dx);
+    float* dweight = p.dense<float>(a[7], at::kFloat, s.cols);
+    void* workspace = a[8] == Py_None ? nullptr : p.any<void>(a[8]);
+    if (!p.ok) return 0;
+    const size_t bytes = a[8] == Py_None ? 0 : tensor(a[8])->nbytes();
+    auto* f = entry<decltype(lasnet_norm_rows_backward)>(a[0]);
+    ENQUEUE(f(&dy, &s, weight, rstd, dsum, &dx, dweight, workspace, bytes, st));
+  });
+}
+
+// (experts, E, offsets, order, position, workspace)
+PyObject* route(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 7, [&](Plain& p) {
+    int64_t tokens;
+    int k;
+    const int32_t* experts = p.slots(a[1], tokens, k);
+    const int E = p.integer(a[2]);
+    if (!p.ok) return 0;
+    int32_t* offsets = p.dense<int32_t>(a[3], at::kInt, (int64_t)E + 1);
+    int32_t* order = p.dense<int32_t>(a[4], at::kInt, tokens * k);
+    int32_t* position = p.dense<int32_t>(a[5], at::kInt, tokens * k);
+    void* workspace = a[6] == Py_None ? nullptr : p.any<void>(a[6]);
+    if (!p.ok) return 0;
+    const size_t bytes = a[6] == Py_None ? 0 : tensor(a[6])->nbytes();
+    auto* f = entry<decltype(lasnet_route)>(a[0]);
+    ENQUEUE(f(experts, tokens, k, E, offsets, order, position, workspace, bytes, st));
+  });
+}
+
+// (x, position, offsets, scale, out, out_scale)
+PyObject* dispatch_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 7, [&](Plain& p) {
+    lasnet_rows x, out;
+    int64_t tokens;
+    int k, E;
+    p.rows(a[1], x);
+    const int32_t* position = p.slots(a[2], tokens, k);
+    const int32_t* offsets = p.offsets(a[3], E);
+    p.rows(a[5], out);
+    if (!p.ok || !p.need(x.rows == tokens)) return 0;
+    const uint8_t* scale = p.scale<const uint8_t>(a[4], tokens);
+    uint8_t* out_scale = p.scale<uint8_t>(a[6], tokens * k);
+    if (!p.ok) return 0;
+    auto* f = entry<decltype(lasnet_dispatch_rows)>(a[0]);
+    ENQUEUE(f(&x, scale, position, offsets, k, E, &out, out_scale, st));
+  });
+}
+
+// (y, position, weights, base, out)
+PyObject* combine_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 6, [&](Plain& p) {
+    lasnet_rows y, b, out;
+    int64_t tokens;
+    int k;
+    p.rows(a[1], y);
+    const int32_t* position = p.slots(a[2], tokens, k);
+    const lasnet_rows* base = p.rows_or_none(a[4], b);
+    p.rows(a[5], out);
+    if (!p.ok || !p.need(out.rows == tokens)) return 0;
+    const float* weights = p.dense<const float>(a[3], at::kFloat, tokens * k);
+    if (!p.ok) return 0;
+    auto* f = entry<decltype(lasnet_combine_rows)>(a[0]);
+    ENQUEUE(f(&y, weights, position, k, base, &out, st));
+  });
+}
+
+// (dout, y, position, offsets, weights, dy, dweights)
+PyObject* combine_rows_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 8, [&](Plain& p) {
+    lasnet_rows dout, y, dy;
+    int64_t tokens;
+    int k, E;
+    p.rows(a[1], dout);
+    p.rows(a[2], y);
+    const int32_t* position = p.slots(a[3], tokens, k);
+    const int32_t* offsets = p.offsets(a[4], E);
+    p.rows(a[6], dy);
+    if (!p.ok || !p.need(dout.rows == tokens)) return 0;
+    const float* weights = p.dense<const float>(a[5], at::kFloat, tokens * k);
+    float* dweights = p.dense<float>(a[7], at::kFloat, tokens * k);
+    if (!p.ok) return 0;
+    auto* f = entry<decltype(lasnet_combine_rows_backward)>(a[0]);
+    ENQUEUE(f(&dout, &y, weights, position, offsets, k, E, &dy, dweights, st));
+  });
+}
+
+inline at::ScalarType row_type(int dtype) {
+  return dtype == LASNET_F32 ? at::kFloat : dtype == LASNET_BF16 ? at::kBFloat16 : at::ScalarType::Float8_e4m3fn;
+}
+
+// (x, offsets, W, scale, wscale, out, flags)
+PyObject* expert_product(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 8, [&](Plain& p) {
+    lasnet_rows x, out;
+    int E;
+    p.rows(a[1], x);
+    const int32_t* offsets = p.offsets(a[2], E);
+    p.rows(a[6], out);
+    const int flags = p.integer(a[7]);
+    if (!p.ok) return 0;
+    const void* W = p.matrices(a[3], E, out.cols, x.cols, row_type(x.dtype));
+    const uint8_t* scale = p.scale<const uint8_t>(a[4], x.rows);
+    const float* wscale = p.dense<const float>(a[5], at::kFloat, (int64_t)E * out.cols);
+    if (!p.ok) return 0;
+    auto* f = entry<decltype(lasnet_expert_product)>(a[0]);
+    ENQUEUE(f(&x, scale, offsets, E, W, wscale, &out, (uint32_t)flags, st));
+  });
+}
+
+// (dy, offsets, W, dx)
+PyObject* expert_product_dx(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 5, [&](Plain& p) {
+    lasnet_rows dy, dx;
+    int E;
+    p.rows(a[1], dy);
+    const int32_t* offsets = p.offsets(a[2], E);
+    p.rows(a[4], dx);
+    if (!p.ok) return 0;
+    const void* W = p.matrices(a[3], E, dy.cols, dx.cols, row_type(dy.dtype));
+    if (!p.ok) return 0;
+    auto* f = entry<decltype(lasnet_expert_product_dx)>(a[0]);
+    ENQUEUE(f(&dy, offsets, E, W, &dx, st));
+  });
+}
+
+// (dy, x, offsets, dW)
+PyObject* expert_product_dw(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 5, [&](Plain& p) {
+    lasnet_rows dy, x;
+    int E;
+    p.rows(a[1], dy);
+    p.rows(a[2], x);
+    const int32_t* offsets = p.offsets(a[3], E);
+    const at::Tensor* dW = tensor(a[4]);
+    if (!p.ok || !p.need(dW && dW->defined())) return 0;
+    const auto ty = dW->scalar_type();
+    p.need(ty == at::kFloat || ty == at::kBFloat16);
+    void* to = p.matrices(a[4], E, dy.cols, x.cols, ty);
+    if (!p.ok) return 0;
+    auto* f = entry<decltype(lasnet_expert_product_dw)>(a[0]);
+    ENQUEUE(f(&dy, &x, offsets, E, to, ty == at::kFloat ? LASNET_F32 : LASNET_BF16, st));
+  });
+}
+
 PyMethodDef methods[] = {
+    {"norm_rows", (PyCFunction)(void*)norm_rows, METH_FASTCALL, nullptr},
+    {"norm_rows_backward", (PyCFunction)(void*)norm_rows_backward, METH_FASTCALL, nullptr},
+    {"route", (PyCFunction)(void*)route, METH_FASTCALL, nullptr},
+    {"dispatch_rows", (PyCFunction)(void*)dispatch_rows, METH_FASTCALL, nullptr},
+    {"combine_rows", (PyCFunction)(void*)combine_rows, METH_FASTCALL, nullptr},
+    {"combine_rows_backward", (PyCFunction)(void*)combine_rows_backward, METH_FASTCALL, nullptr},
+    {"expert_product", (PyCFunction)(void*)expert_product, METH_FASTCALL, nullptr},
+    {"expert_product_dx", (PyCFunction)(void*)expert_product_dx, METH_FASTCALL, nullptr},
+    {"expert_product_dw", (PyCFunction)(void*)expert_product_dw, METH_FASTCALL, nullptr},
     {"masker_ex", (PyCFunction)(void*)masker_ex, METH_FASTCALL, nullptr},
     {"block_packed", (PyCFunction)(void*)block_packed, METH_FASTCALL, nullptr},
     {"block_planned", (PyCFunction)(void*)block_planned, METH_FASTCALL, nullptr},

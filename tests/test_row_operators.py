@@ -474,6 +474,80 @@ def test_captured_in_a_graph():
             assert torch.equal(a, b), i
 
 
+@pytest.mark.gpu
+def test_native_marshalling_takes_whole_calls(monkeypatch):
+    """A call that brings its outputs goes through the native marshalling, with the results of the Python path (a given stream: never native)."""
+    g = gen(13)
+    tokens, k, E, C, n = 40, 3, 5, 96, 64
+    B.lib()
+    real, taken = B._marshal, []
+
+    class Spy:
+        def __getattr__(self, name):
+            def f(*a):
+                r = getattr(real, name)(*a)
+                taken.append((name, r))
+                return r
+            return f
+
+    x, res, w = rand(g, tokens, C, dtype=BF16, pad=8), rand(g, tokens, C, dtype=BF16), rand(g, C)
+    e = torch.randint(-1, E, (tokens, k), generator=g, dtype=torch.int32).cuda()
+    W, W8 = rand(g, E, n, C, dtype=BF16), rand(g, E, n, C).to(E4M3)
+    wt, dy, rstd = rand(g, tokens, k), rand(g, tokens, C, dtype=BF16), torch.rsqrt(x.float().square().mean(-1))
+
+    def calls(given):
+        stream = None if given else torch.cuda.current_stream()
+        out = lambda *shape, dtype=BF16: torch.zeros(*shape, dtype=dtype, device="cuda") if given else None
+        q, scale, total = B.lasnet_norm_rows(x, w, 1e-6, residual=res, out=out(tokens, C, dtype=E4M3), scale=out(tokens, dtype=torch.uint8), sum_out=out(tokens, C),
+                                             out_dtype=None if given else E4M3, stream=stream)
+        dx, dw = B.lasnet_norm_rows_backward(dy, x, w, rstd, dsum=res, dx=out(tokens, C), dweight=out(C, dtype=F32), stream=stream)
+        offsets, order, position = B.lasnet_route(e, E, offsets=out(E + 1, dtype=torch.int32), order=out(tokens * k, dtype=torch.int32),
+                                                  position=out(tokens, k, dtype=torch.int32), stream=stream)
+        rows, rs = B.lasnet_dispatch_rows(q, position, offsets, scale=scale, out=out(tokens * k, C, dtype=E4M3), out_scale=out(tokens * k, dtype=torch.uint8), stream=stream)
+        p8 = B.lasnet_expert_product(rows, offsets, W8, scale=rs, out=out(tokens * k, n), stream=stream)
+        back = B.lasnet_combine_rows(p8, position, weights=wt, out=out(tokens, n), stream=stream)
+        dp, dwt = B.lasnet_combine_rows_backward(back, p8, position, offsets, weights=wt, dy=out(tokens * k, n), dweights=out(tokens, k, dtype=F32), stream=stream)
+        dr = B.lasnet_expert_product_dx(dp, offsets, W, dx=out(tokens * k, C), stream=stream)
+        dW = B.lasnet_expert_product_dw(dp, dr, offsets, dW=out(E, n, C, dtype=F32), dtype=None if given else F32, stream=stream)
+        return [t.contiguous().view(torch.uint8) for t in (q, scale, total, dx, dw, offsets, order, position, rows, rs, p8, back, dp, dwt, dr, dW)]
+
+    want = calls(False)
+    monkeypatch.setattr(B, "_marshal", Spy())
+    got = calls(True)
+    assert [t[0] for t in taken] == ["norm_rows", "norm_rows_backward", "route", "dispatch_rows", "expert_product", "combine_rows", "combine_rows_backward",
+                                     "expert_product_dx", "expert_product_dw"] and all(t[1] == 0 for t in taken), taken
+    for i, (a, b) in enumerate(zip(want, got)):
+        assert torch.equal(a.reshape(-1), b.reshape(-1)), i
+    # what is not of the plain form is left to the Python path and its messages
+    with pytest.raises(ValueError, match="weight"):
+        B.lasnet_norm_rows(x, w[:5], 1e-6, out=torch.empty_like(x))
+    with pytest.raises(ValueError, match="as many tokens"):
+        B.lasnet_combine_rows(torch.zeros(tokens * k, n, device="cuda"), torch.zeros(tokens, k, dtype=torch.int32, device="cuda"), out=torch.zeros(tokens + 1, n, device="cuda"))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,E,n,k,kind", MANY_TILES + [(515, 3, 300, 1000, "tail"), (700, 70, 512, 520, "spread")])
+def test_products_are_those_of_the_drained_build(rows, E, n, k, kind):
+    """The check build, in which every barrier waits for all memory operations, gives the same bits: no counted wait is short."""
+    from paper_2210_06223_amd import build
+    o = groups(rows, E, kind, rows + n)
+    offsets = torch.from_numpy(o.astype(np.int32)).cuda()
+    g = gen(rows)
+    x, dy, W = rand(g, rows, k, dtype=BF16), rand(g, rows, n, dtype=BF16), rand(g, E, n, k, dtype=BF16)
+    q, V = rand(g, rows, k).to(E4M3), rand(g, E, n, k).to(E4M3)
+    f = lambda: [B.lasnet_expert_product(x, offsets, W), B.lasnet_expert_product(q, offsets, V), B.lasnet_expert_product_dx(dy, offsets, W),
+                 B.lasnet_expert_product_dw(dy, x, offsets), B.lasnet_expert_product_dw(dy, x, offsets, dtype=F32)]
+    got = f()
+    mine = B._lib
+    try:
+        B._lib = B.load_library(build.LIB_CHECK)
+        want = f()
+    finally:
+        B._lib = mine
+    for i, (a, b) in enumerate(zip(got, want)):
+        assert torch.equal(a, b), i
+
+
 # ---------------------------------------------------------------- refusals (no GPU: nothing is enqueued)
 
 def R(rows=8, cols=16, dtype=B.LASNET_BF16, data=0x1000, stride=0):
