@@ -37,6 +37,13 @@ __device__ __forceinline__ int bound(const ProductArgs& a, int e) {
   return v < 0 ? 0 : (long long)v < a.rows ? v : (int)a.rows;
 }
 
+typedef __amdgpu_buffer_rsrc_t product_rsrc_t;
+
+__device__ __forceinline__ product_rsrc_t product_rsrc(const void* p, unsigned bytes) {
+  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)(size_t)p), hi = __builtin_amdgcn_readfirstlane((unsigned)((size_t)p >> 32));
+  return __builtin_amdgcn_make_buffer_rsrc((void*)(((unsigned long long)hi << 32) | lo), 0, (int)__builtin_amdgcn_readfirstlane(bytes), 0x00020000);
+}
+
 // Row tile t of all experts' (BJ rows each, the last of an expert may have fewer) -> its expert, first row and end.  Expert E: the rows that no
 // expert has.  false: no such tile.  Every wave of a workgroup finds the same.
 template <int BJ>
@@ -122,10 +129,11 @@ __device__ __forceinline__ uint4_t load_some(const unsigned char* p, int n) {
   return v;
 }
 
-// The wave's NI x NJ blocks of 16 x 16, from column oi0 and row oj0 of the output on, scaled, rounded and stored.
+// The wave's NI x NJ blocks of 16 x 16, from column oi0 and row oj0 of the output on, scaled, rounded and stored.  Outputs whose columns and pitch are whole
+// multiples of 4 elements go through a buffer that ends with row j_end, without a branch for each; others (and rows too far apart) element by element.
 template <bool FP8, bool F32OUT, int NI, int NJ>
-__device__ __forceinline__ void store_tile(const ProductArgs& a, unsigned char* out, int expert, int oi0, int oj0, int j_end,
-                                           const floatx4 (&acc)[NI][NJ]) {
+__device__ __forceinline__ void store_tile(const ProductArgs& a, unsigned char* out, int expert, int oi0, int oj0, int j_end, const floatx4 (&acc)[NI][NJ]) {
+  constexpr int OB = F32OUT ? 4 : 2;
   const int lane = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));      // (made anew: no register holds it through the loop)
   const float floor = a.relu ? 0.f : -INFINITY;               // (NaN passes)
   float up[NJ];
@@ -137,24 +145,44 @@ __device__ __forceinline__ void store_tile(const ProductArgs& a, unsigned char* 
       if (a.scale && expert < a.E && oj < j_end) up[j] = scale_value(a.scale[oj]);
     }
   }
+  if (oj0 >= j_end || oi0 >= a.ni) return;
+  const bool fours = !((a.ni | (int)(a.out.pitch / OB)) & 3) && !((size_t)out & 3) && a.out.pitch < (1 << 22);
+  const int rows = j_end - oj0 < 16 * NJ ? j_end - oj0 : 16 * NJ;
+  const product_rsrc_t to = product_rsrc(out + (long long)oj0 * a.out.pitch + (long long)oi0 * OB,
+                                         fours ? (unsigned)(rows - 1) * (unsigned)a.out.pitch + (unsigned)(a.ni - oi0) * OB : 0u);
+  auto each = [&](auto store) {
 #pragma unroll
-  for (int i = 0; i < NI; ++i) {
-    const int oi = oi0 + 16 * i + (lane >> 4) * 4;
-    float w[4] = {1.0f, 1.0f, 1.0f, 1.0f};
-    if constexpr (FP8)
-      if (a.wscale && expert < a.E) Elem<float>::widen(load_piece<float>((const unsigned char*)(a.wscale + (size_t)expert * a.ni + oi), a.ni - oi), w);
+    for (int i = 0; i < NI; ++i) {
+      const int oi = oi0 + 16 * i + (lane >> 4) * 4;
+      float w[4] = {1.0f, 1.0f, 1.0f, 1.0f};
+      if constexpr (FP8)
+        if (a.wscale && expert < a.E) Elem<float>::widen(load_piece<float>((const unsigned char*)(a.wscale + (size_t)expert * a.ni + oi), a.ni - oi), w);
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      const int oj = oj0 + 16 * j + (lane & 15);
-      if (oj >= j_end) continue;
-      float v[4];
+      for (int j = 0; j < NJ; ++j) {
+        float v[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        v[r] = acc[i][j][r];
-        if constexpr (FP8) v[r] *= w[r] * up[j];
-        v[r] = v[r] < floor ? floor : v[r];
+        for (int r = 0; r < 4; ++r) {
+          v[r] = acc[i][j][r];
+          if constexpr (FP8) v[r] *= w[r] * up[j];
+          v[r] = v[r] < floor ? floor : v[r];
+        }
+        store(i, j, oi, v);
       }
-      unsigned char* o = out + (long long)oj * a.out.pitch + (long long)oi * (F32OUT ? 4 : 2);
+    }
+  };
+  if (fours) {
+    each([&](int i, int j, int oi, const float (&v)[4]) {
+      const int o = oi < a.ni ? (16 * j + (lane & 15)) * (int)a.out.pitch + (16 * i + (lane >> 4) * 4) * OB : -1;
+      if constexpr (F32OUT)
+        __builtin_amdgcn_raw_buffer_store_b128(Elem<float>::narrow(v), to, o, 0, 0);
+      else
+        __builtin_amdgcn_raw_buffer_store_b64(uint2_t{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])}, to, o, 0, 0);
+    });
+  } else {
+    each([&](int, int j, int oi, const float (&v)[4]) {
+      const int oj = oj0 + 16 * j + (lane & 15);
+      if (oj >= j_end) return;
+      unsigned char* o = out + (long long)oj * a.out.pitch + (long long)oi * OB;
       if constexpr (F32OUT) {
         store_piece<float>(o, a.ni - oi, Elem<float>::narrow(v));
       } else if (oi + 4 <= a.ni) {
@@ -164,7 +192,7 @@ __device__ __forceinline__ void store_tile(const ProductArgs& a, unsigned char* 
         for (int r = 0; r < 4; ++r)
           if (oi + r < a.ni) Elem<__bf16>::put(o + 2 * r, bf16_pair(v[r], 0.f));
       }
-    }
+    });
   }
 }
 
@@ -277,12 +305,6 @@ __global__ __launch_bounds__(256) void product_kernel(ProductArgs a) {
 // to be clamped.  Every load is issued, those past the last step of an empty buffer, so that they can be counted.
 typedef __attribute__((address_space(3))) unsigned char lds_byte;
 typedef int intx4 __attribute__((ext_vector_type(4)));
-typedef __amdgpu_buffer_rsrc_t product_rsrc_t;
-
-__device__ __forceinline__ product_rsrc_t product_rsrc(const void* p, unsigned bytes) {
-  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)(size_t)p), hi = __builtin_amdgcn_readfirstlane((unsigned)((size_t)p >> 32));
-  return __builtin_amdgcn_make_buffer_rsrc((void*)(((unsigned long long)hi << 32) | lo), 0, (int)__builtin_amdgcn_readfirstlane(bytes), 0x00020000);
-}
 // Where an operand's loads are: the tile at the next step's k, and the buffer that ends with the operand (by rows: what there is of the tile's rows from there on;
 // by columns: of the step's rows of k).  Kept to a few scalar instructions a step: the waves that share a SIMD have some 30 clocks for each pair of MFMAs.
 template <bool COLS>
@@ -615,7 +637,6 @@ __device__ __forceinline__ void store_big_tile(const ProductArgs& a, unsigned ch
   const int rows = t.j_end - t.j0 < 256 ? t.j_end - t.j0 : 256;
   const unsigned long long first = (unsigned long long)(out + (long long)t.j0 * a.out.pitch + (long long)t.i0 * OB);
   const intx4 to = {(int)(unsigned)first, (int)(unsigned)(first >> 32), (int)((unsigned)(rows - 1) * pitch + (unsigned)(a.ni - t.i0) * OB), 0x00020000};
-  const float floor = a.relu ? 0.f : -INFINITY;               // (NaN passes)
   // the scales of the wave's 64 rows and 128 columns, one and two a lane, all asked for before the first store
   float row_scale = 1.f, col_scale[2] = {1.f, 1.f};
   if constexpr (FP8) {
@@ -632,32 +653,38 @@ __device__ __forceinline__ void store_big_tile(const ProductArgs& a, unsigned ch
   if constexpr (FP8)
 #pragma unroll
     for (int j = 0; j < 4; ++j) up[j] = __shfl(row_scale, 16 * j + (lane & 15));
+  auto each = [&](auto relu) {
+    const intx4 buffer = to;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int oi = wi + 16 * i + (lane >> 4) * 4;
-    float w[4] = {1.f, 1.f, 1.f, 1.f};
-    if constexpr (FP8)
+    for (int i = 0; i < 8; ++i) {
+      const int oi = wi + 16 * i + (lane >> 4) * 4;
+      float w[4] = {1.f, 1.f, 1.f, 1.f};
+      if constexpr (FP8)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) w[r] = __shfl(col_scale[i / 4], 16 * (i % 4) + (lane >> 4) * 4 + r);
-    // (ni is a multiple of 4: a lane's four are stored or not)
-    unsigned off = t.i0 + oi < a.ni ? (unsigned)(wj + (lane & 15)) * pitch + (unsigned)oi * OB : 0xffffffffu;
+        for (int r = 0; r < 4; ++r) w[r] = __shfl(col_scale[i / 4], 16 * (i % 4) + (lane >> 4) * 4 + r);
+      // (ni is a multiple of 4: a lane's four are stored or, beyond the buffer's 2^31 bytes, not)
+      unsigned o = t.i0 + oi < a.ni ? (unsigned)(wj + (lane & 15)) * pitch + (unsigned)oi * OB : 0x80000000u;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float v[4];
+      for (int j = 0; j < 4; ++j, o += 16 * pitch) {
+        float v[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        v[r] = acc[i][j][r];
-        if constexpr (FP8) v[r] *= w[r] * up[j];
-        v[r] = v[r] < floor ? floor : v[r];
+        for (int r = 0; r < 4; ++r) {
+          v[r] = acc[i][j][r];
+          if constexpr (FP8) v[r] *= w[r] * up[j];
+          if constexpr (decltype(relu)::value) v[r] = v[r] < 0.f ? 0.f : v[r];              // (NaN passes)
+        }
+        // (s_nop: the registers of a store of more than 8 bytes may not be written by the very next instruction)
+        if constexpr (F32OUT)
+          asm volatile("buffer_store_dwordx4 %0, %1, %2, 0 offen\n\ts_nop 1" ::"v"(Elem<float>::narrow(v)), "v"(o), "s"(buffer) : "memory");
+        else
+          asm volatile("buffer_store_dwordx2 %0, %1, %2, 0 offen" ::"v"(uint2_t{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])}), "v"(o), "s"(buffer) : "memory");
       }
-      const unsigned o = off == 0xffffffffu ? off : off + (unsigned)j * 16 * pitch;
-      // (s_nop: the registers of a store of more than 8 bytes may not be written by the very next instruction)
-      if constexpr (F32OUT)
-        asm volatile("buffer_store_dwordx4 %0, %1, %2, 0 offen\n\ts_nop 1" ::"v"(Elem<float>::narrow(v)), "v"(o), "s"(to) : "memory");
-      else
-        asm volatile("buffer_store_dwordx2 %0, %1, %2, 0 offen" ::"v"(uint2_t{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])}), "v"(o), "s"(to) : "memory");
     }
-  }
+  };
+  if (a.relu)
+    each(std::true_type{});
+  else
+    each(std::false_type{});
 }
 
 template <bool FP8, bool IC, bool JC, bool RAGGED, bool F32OUT>
@@ -993,7 +1020,7 @@ hipError_t go_stream(ProductArgs a, hipStream_t st) {
 // registers (nothing is used twice), DEPTH steps of 128 bytes ahead; the quarters' sums are added in order through LDS.
 template <bool FP8, int NJ>
 __global__ __launch_bounds__(256) void product_few_kernel(ProductArgs a) {
-  constexpr int BYTES = FP8 ? 1 : 2, DEPTH = NJ == 1 ? 8 : NJ == 2 ? 4 : 2;
+  constexpr int BYTES = FP8 ? 1 : 2, DEPTH = NJ == 1 ? 8 : 4;
   constexpr unsigned NONE = 0xffffffffu;
   __shared__ floatx4 sums[3][NJ][64];
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -1077,11 +1104,12 @@ bool whole(const ProductArgs& a, int bytes, int B) {
 template <bool FP8, bool IC, bool JC, bool RAGGED, bool F32OUT>
 hipError_t go(ProductArgs a, hipStream_t st) {
   if (whole<IC, JC>(a, FP8 ? 1 : 2, 256)) {
+    // Up to 32 rows, and no more than some four workgroups a CU: rows go straight to registers.
+    // 16 and 32 rows, one expert 1024 x 2048 7.3 and 9.1 us, tiles 14; 16 experts 12.8 and 14.3, tiles 14.7 and 14.9; 64 rows, 16 experts 18, tiles 15; 32 rows,
+    // 8 experts 4096 x 4096 47, tiles 35 (in bf16, whole calls).
     if constexpr (!IC && !RAGGED) {
-      if (a.rows <= 64) {
-        const long long each = a.rows / a.E;
-        return a.rows <= 16 || each <= 8 ? go_few<FP8, 1>(a, st) : a.rows <= 32 || each <= 16 ? go_few<FP8, 2>(a, st) : go_few<FP8, 4>(a, st);
-      }
+      const long long units = (a.rows / 16 + (a.rows < a.E ? a.rows : a.E)) * ((a.ni + 15) / 16);
+      if (a.rows <= 32 && units <= 1200) return a.rows <= 16 || a.rows / a.E <= 8 ? go_few<FP8, 1>(a, st) : go_few<FP8, 2>(a, st);
     }
     const long long wide = (a.ni + 255) / 256, groups = a.rows < a.E ? a.rows : a.E;
     const long long big = (RAGGED ? (long long)a.E * ((a.nj + 255) / 256) : a.rows / 256 + groups / 2) * wide;
@@ -1089,11 +1117,12 @@ hipError_t go(ProductArgs a, hipStream_t st) {
     if (big >= 256 && long_enough && a.ni % 4 == 0 && !(((unsigned long long)a.out.data | (unsigned long long)a.out.pitch | (unsigned long long)a.out_expert) & 15) &&
         a.out.pitch < (1ll << 31) / 256)
       return go_stream<FP8, IC, JC, RAGGED, F32OUT>(a, st);
-#ifndef FOUR
-#define FOUR 256
-#endif
-    const long long tiles = (RAGGED ? (long long)a.E * ((a.nj + 127) / 128) : a.rows / 128 + groups / 2) * ((a.ni + 127) / 128);
-    if (tiles <= FOUR) return go_tile<FP8, IC, JC, RAGGED, F32OUT, 128, 128, 2, 4, 4>(a, st);
+    const long long i128 = (a.ni + 127) / 128;
+    const long long tiles128 = (RAGGED ? (long long)a.E * ((a.nj + 127) / 128) : a.rows / 128 + groups / 2) * i128;
+    const long long tiles64 = (RAGGED ? (long long)a.E * ((a.nj + 63) / 64) : a.rows / 64 + groups / 2) * i128;
+    if (tiles64 <= 256) return go_tile<FP8, IC, JC, RAGGED, F32OUT, 128, 64, 2, 2, 3>(a, st);
+    if (tiles128 <= 240) return go_tile<FP8, IC, JC, RAGGED, F32OUT, 128, 128, 2, 4, 4>(a, st);
+    if (tiles64 <= 512) return go_tile<FP8, IC, JC, RAGGED, F32OUT, 128, 64, 2, 2, 3>(a, st);
     return go_tile<FP8, IC, JC, RAGGED, F32OUT, 128, 128, 2, 2, 2>(a, st);
   }
   a.tiles_i = (a.ni + 127) / 128;

@@ -167,11 +167,13 @@ hipError_t pick(const NormArgs& a, hipStream_t st) {
 }
 
 // ---- the gradients ----
+__host__ __device__ inline int part_pitch(int cols) { return (cols + 3) / 4 * 4; }     // floats of a workgroup's part: whole pieces
+
 struct NormGradArgs {
   RowsArg dy, s, dsum, dx;
   const float* weight;
   const float* rstd;
-  float* part;                     // [workgroups][cols]
+  float* part;                     // [workgroups][part_pitch(cols)]
   long long rows;
   int cols;
 };
@@ -242,30 +244,43 @@ __global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void norm_grad_kernel(NormGra
     }
     if (sub) return;
   }
-  float* part = a.part + (size_t)blockIdx.x * a.cols;
+  float* part = a.part + (size_t)blockIdx.x * part_pitch(a.cols);
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const int c = (i * 64 * W + lane) * E::PER;
 #pragma unroll
     for (int j = 0; j < E::PER; ++j)
-      if (c + j < a.cols) part[c + j] = dg[i][j];
+      if (c + j < part_pitch(a.cols)) part[c + j] = dg[i][j];
   }
 }
 
-// dweight[c] = sum of the workgroups' parts, 16 waves a column block of 64, each its share of the workgroups in order.
-__global__ __launch_bounds__(1024) void norm_grad_join_kernel(const float* part, int groups, int cols, float* dweight) {
-  __shared__ float sum[16][64];
-  const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
-  const int c = (int)blockIdx.x * 64 + lane;
-  float v = 0.f;
+// dweight[c] = sum of the workgroups' parts: a workgroup has 16 columns, four a thread, and 64 threads share the parts, each every 64th in order; then the 64 sums in
+// order of a tree.  (One thread a column, 16 a workgroup, took 20 us for 1024 parts of 1024 columns: few loads in flight.)
+__global__ __launch_bounds__(256) void norm_grad_join_kernel(const float* part, int groups, int pitch, int cols, float* dweight) {
+  __shared__ float sum[64][20];
+  const int four = (int)threadIdx.x & 3, share = (int)threadIdx.x >> 2;
+  const int c = (int)blockIdx.x * 16 + four * 4;
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
   if (c < cols)
-    for (int b = wave; b < groups; b += 16) v += part[(size_t)b * cols + c];
-  sum[wave][lane] = v;
-  __syncthreads();
-  if (wave || c >= cols) return;
+#pragma unroll 8
+    for (int b = share; b < groups; b += 64) {
+      float f[4];
+      Elem<float>::widen(load16((const unsigned char*)(part + (size_t)b * pitch + c)), f);
 #pragma unroll
-  for (int i = 1; i < 16; ++i) v += sum[i][lane];
-  dweight[c] = v;
+      for (int i = 0; i < 4; ++i) v[i] += f[i];
+    }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sum[share][four * 4 + i] = v[i];
+  for (int d = 32; d >= 1; d >>= 1) {
+    __syncthreads();
+    if (share < d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum[share][four * 4 + i] += sum[share + d][four * 4 + i];
+  }
+  if (share == 0)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (c + i < cols) dweight[c + i] = sum[0][four * 4 + i];
 }
 
 // Workgroups of the backward pass: as many as the chip runs at once, so that the parts stay few.
@@ -280,7 +295,7 @@ hipError_t go_grad(const NormGradArgs& a, int groups, float* dweight, hipStream_
   norm_grad_kernel<T, W, N><<<dim3((unsigned)groups), dim3(W < 4 ? 256 : 64 * W), 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  norm_grad_join_kernel<<<dim3((unsigned)((a.cols + 63) / 64)), dim3(1024), 0, st>>>(a.part, groups, a.cols, dweight);
+  norm_grad_join_kernel<<<dim3((unsigned)((a.cols + 15) / 16)), dim3(256), 0, st>>>(a.part, groups, part_pitch(a.cols), a.cols, dweight);
   return hipGetLastError();
 }
 
@@ -305,14 +320,14 @@ hipError_t launch_norm_rows(int dtype, int out_dtype, long long rows, int cols, 
   return q ? pick<__bf16, true>(a, st) : pick<__bf16, false>(a, st);
 }
 
-size_t norm_backward_workspace_bytes(long long rows, int cols) { return (size_t)grad_groups(rows, cols) * cols * sizeof(float); }
+size_t norm_backward_workspace_bytes(long long rows, int cols) { return (size_t)grad_groups(rows, cols) * part_pitch(cols) * sizeof(float); }
 
 hipError_t launch_norm_rows_backward(int dtype, long long rows, int cols, RowsArg dy, RowsArg s, const float* weight, const float* rstd,
                                      RowsArg dsum, RowsArg dx, float* dweight, void* workspace, hipStream_t st) {
   const NormGradArgs a{dy, s, dsum, dx, weight, rstd, (float*)workspace, rows, cols};
   const int groups = grad_groups(rows, cols);
   if (rows == 0) {                                             // no rows, no parts: dweight = 0
-    norm_grad_join_kernel<<<dim3((unsigned)((cols + 63) / 64)), dim3(1024), 0, st>>>(nullptr, 0, cols, dweight);
+    norm_grad_join_kernel<<<dim3((unsigned)((cols + 15) / 16)), dim3(256), 0, st>>>(nullptr, 0, 0, cols, dweight);
     return hipGetLastError();
   }
   return dtype == LASNET_F32 ? pick_grad<float>(a, groups, dweight, st) : pick_grad<__bf16>(a, groups, dweight, st);

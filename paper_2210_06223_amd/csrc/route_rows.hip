@@ -17,9 +17,9 @@ struct RouteArgs {
   int32_t* offsets;
   int32_t* order;
   int32_t* position;
-  int32_t* counts;                 // [runs][E], several workgroups: a run's slots for each expert, then those of the runs before it
-  int32_t* totals;                 // [E]
+  int32_t* counts;                 // [runs][E], several workgroups: a run's slots for each expert
   int runs;
+  long long run;                   // slots of a run
 };
 
 // Lanes whose key is this lane's (valid lanes only).
@@ -34,29 +34,49 @@ __device__ __forceinline__ unsigned long long same_key(int key, bool valid, int 
 }
 __device__ __forceinline__ unsigned long long lanes_before(int lane) { return (1ull << lane) - 1; }
 
+// Keys of 256 slots from s on, four a lane, all requested at once.
+struct Keys { int of[4]; };
+__device__ __forceinline__ Keys load_keys(const RouteArgs& a, long long s, long long end) {
+  const int lane = (int)threadIdx.x & 63;
+  Keys k;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) k.of[r] = s + 64 * r + lane < end ? a.experts[s + 64 * r + lane] : -1;
+  return k;
+}
 // Counts of one wave's slots [first, end) into its table.
 __device__ __forceinline__ void count_slots(const RouteArgs& a, long long first, long long end, int* table) {
   const int lane = (int)threadIdx.x & 63;
-  for (long long s = first; s < end; s += 64) {
-    const int key = s + lane < end ? a.experts[s + lane] : -1;
-    const bool valid = (unsigned)key < (unsigned)a.E;
-    const unsigned long long m = same_key(key, valid, a.bits);
-    if (valid && !(m & lanes_before(lane))) atomicAdd(&table[key], __popcll(m));
+  for (long long s = first; s < end; s += 256) {
+    const Keys k = load_keys(a, s, end);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      if (s + 64 * r >= end) break;
+      const int key = k.of[r];
+      const bool valid = (unsigned)key < (unsigned)a.E;
+      const unsigned long long m = same_key(key, valid, a.bits);
+      if (valid && !(m & lanes_before(lane))) atomicAdd(&table[key], __popcll(m));
+    }
   }
 }
 // ... and their places, from the table of the first free row of each expert.
 __device__ __forceinline__ void place_slots(const RouteArgs& a, long long first, long long end, int* table) {
   const int lane = (int)threadIdx.x & 63;
-  for (long long s = first; s < end; s += 64) {
-    const int key = s + lane < end ? a.experts[s + lane] : -1;
-    const bool valid = (unsigned)key < (unsigned)a.E;
-    const unsigned long long m = same_key(key, valid, a.bits);
-    const int ahead = __popcll(m & lanes_before(lane));
-    int at = 0;
-    if (valid && !ahead) at = atomicAdd(&table[key], __popcll(m));
-    at = __shfl(at, valid ? __ffsll((long long)m) - 1 : lane) + ahead;
-    if (s + lane < end) a.position[s + lane] = valid ? at : -1;
-    if (valid && a.order) a.order[at] = (int32_t)(s + lane);
+  for (long long s = first; s < end; s += 256) {
+    const Keys k = load_keys(a, s, end);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const long long slot = s + 64 * r + lane;
+      if (s + 64 * r >= end) break;
+      const int key = k.of[r];
+      const bool valid = (unsigned)key < (unsigned)a.E;
+      const unsigned long long m = same_key(key, valid, a.bits);
+      const int ahead = __popcll(m & lanes_before(lane));
+      int at = 0;
+      if (valid && !ahead) at = atomicAdd(&table[key], __popcll(m));
+      at = __shfl(at, valid ? __ffsll((long long)m) - 1 : lane) + ahead;
+      if (slot < end) a.position[slot] = valid ? at : -1;
+      if (valid && a.order) a.order[at] = (int32_t)slot;
+    }
   }
 }
 
@@ -82,72 +102,107 @@ __device__ __forceinline__ int wave_scan(int n, F f, G g) {
 constexpr int kRouteTable = 8192;          // entries of LDS tables in a workgroup
 __host__ __device__ inline int route_waves(int E) { return E <= kRouteTable / 16 ? 16 : kRouteTable / E; }      // E up to 4096: at least 2
 
-// Few slots: one workgroup does it all, a table for each wave.
+// Places of a workgroup's slots [first, end): its waves' runs are counted, the counts summed over the waves before each, and the rows before the
+// workgroup's first of each expert added: between() makes the tables' columns exclusive sums from there.
+template <class Between>
+__device__ __forceinline__ void place_run(const RouteArgs& a, long long first, long long end, int* table, Between between) {
+  const int nw = (int)blockDim.x >> 6, wave = (int)threadIdx.x >> 6;
+  const long long per = (end - first + 64 * nw - 1) / (64 * nw) * 64;
+  const long long mine = first + per * wave, mine_end = mine + per < end ? mine + per : end;
+  for (int i = (int)threadIdx.x; i < nw * a.E; i += blockDim.x) table[i] = 0;
+  __syncthreads();
+  count_slots(a, mine, mine_end, table + wave * a.E);
+  __syncthreads();
+  between();
+  __syncthreads();
+  place_slots(a, mine, mine_end, table + wave * a.E);
+}
+// Column e of the waves' tables, exclusively summed from `sum` on; returns the sum behind the last.
+__device__ __forceinline__ int stack_column(const RouteArgs& a, int* table, int e, int sum) {
+  const int nw = (int)blockDim.x >> 6;
+  for (int w = 0; w < nw; ++w) {
+    const int v = table[w * a.E + e];
+    table[w * a.E + e] = sum;
+    sum += v;
+  }
+  return sum;
+}
+// starts[e] <- the sum of starts before e, by wave 0; offsets too where `write`, and order beyond the last row.
+__device__ __forceinline__ int scan_starts(const RouteArgs& a, int* starts, bool write) {
+  const int sent = wave_scan(a.E, [&](int e) { return starts[e]; }, [&](int e, int v) {
+    starts[e] = v;
+    if (write) a.offsets[e] = v;
+  });
+  if (write && threadIdx.x == 0) a.offsets[a.E] = sent;
+  return sent;
+}
+
+// Few slots: one workgroup does it all.
 __global__ __launch_bounds__(1024) void route_one_kernel(RouteArgs a) {
   __shared__ int table[kRouteTable];
   __shared__ int starts[4096];
-  const int nw = (int)blockDim.x >> 6, wave = (int)threadIdx.x >> 6, tid = (int)threadIdx.x;
-  const long long per = (a.slots + 64 * nw - 1) / (64 * nw) * 64;
-  const long long first = per * wave, end = first + per < a.slots ? first + per : a.slots;
-  for (int i = tid; i < nw * a.E; i += blockDim.x) table[i] = 0;
-  __syncthreads();
-  count_slots(a, first, end, table + wave * a.E);
-  __syncthreads();
-  for (int e = tid; e < a.E; e += blockDim.x) {
-    int sum = 0;
-    for (int w = 0; w < nw; ++w) {
-      const int v = table[w * a.E + e];
-      table[w * a.E + e] = sum;
-      sum += v;
+  const int nw = (int)blockDim.x >> 6, tid = (int)threadIdx.x;
+  place_run(a, 0, a.slots, table, [&] {
+    for (int e = tid; e < a.E; e += blockDim.x) starts[e] = stack_column(a, table, e, 0);
+    __syncthreads();
+    if (tid < 64) {
+      const int sent = scan_starts(a, starts, true);
+      if (a.order)
+        for (long long p = sent + tid; p < a.slots; p += 64) a.order[p] = -1;
     }
-    starts[e] = sum;
-  }
-  __syncthreads();
-  if (wave == 0) {
-    const int sent = wave_scan(a.E, [&](int e) { return starts[e]; }, [&](int e, int v) { starts[e] = v; a.offsets[e] = v; });
-    if (tid == 0) a.offsets[a.E] = sent;
-    if (a.order)
-      for (long long p = sent + tid; p < a.slots; p += 64) a.order[p] = -1;
-  }
-  __syncthreads();
-  for (int i = tid; i < nw * a.E; i += blockDim.x) table[i] += starts[i % a.E];
-  __syncthreads();
-  place_slots(a, first, end, table + wave * a.E);
+    __syncthreads();
+    for (int i = tid; i < nw * a.E; i += blockDim.x) table[i] += starts[i % a.E];
+  });
 }
 
-// Many slots: a run of kRouteRun slots for each wave (= workgroup); counts, their scan for each expert over the runs, places.
-constexpr int kRouteRun = 256;
-__global__ __launch_bounds__(64) void route_count_kernel(RouteArgs a) {
+// Many slots: a run of them for each workgroup.  Its counts first; then every workgroup adds up the counts of the runs before its own (and of all, for the
+// offsets) and places its slots.  At most kRouteRuns runs, so that this sum stays short.
+constexpr int kRouteRuns = 256;
+__global__ __launch_bounds__(256) void route_count_kernel(RouteArgs a) {
   __shared__ int table[4096];
-  const int lane = (int)threadIdx.x;
-  for (int e = lane; e < a.E; e += 64) table[e] = 0;
+  for (int e = (int)threadIdx.x; e < a.E; e += 256) table[e] = 0;
   __syncthreads();
-  const long long first = (long long)blockIdx.x * kRouteRun;
-  count_slots(a, first, first + kRouteRun < a.slots ? first + kRouteRun : a.slots, table);
+  const long long first = a.run * blockIdx.x, end = first + a.run < a.slots ? first + a.run : a.slots;
+  const long long per = (end - first + 255) / 256 * 64, mine = first + per * ((int)threadIdx.x >> 6);
+  count_slots(a, mine, mine + per < end ? mine + per : end, table);
   __syncthreads();
-  for (int e = lane; e < a.E; e += 64) a.counts[(size_t)e * a.runs + blockIdx.x] = table[e];
+  for (int e = (int)threadIdx.x; e < a.E; e += 256) a.counts[(size_t)blockIdx.x * a.E + e] = table[e];
 }
-__global__ __launch_bounds__(64) void route_scan_kernel(RouteArgs a) {
-  int32_t* c = a.counts + (size_t)blockIdx.x * a.runs;
-  const int total = wave_scan(a.runs, [&](int i) { return c[i]; }, [&](int i, int v) { c[i] = v; });
-  if (threadIdx.x == 0) a.totals[blockIdx.x] = total;
-}
-__global__ __launch_bounds__(64) void route_place_kernel(RouteArgs a) {
-  __shared__ int table[4096];
-  const int lane = (int)threadIdx.x;
-  const int sent = wave_scan(a.E, [&](int e) { return a.totals[e]; }, [&](int e, int v) {
-    table[e] = v + a.counts[(size_t)e * a.runs + blockIdx.x];
-    if (blockIdx.x == 0) a.offsets[e] = v;
+__global__ __launch_bounds__(256) void route_place_kernel(RouteArgs a) {
+  __shared__ int table[kRouteTable];
+  __shared__ int starts[4096], before[4096];                  // rows of each expert: of all runs, of those before this one
+  const int tid = (int)threadIdx.x, nw = (int)blockDim.x >> 6, run = (int)blockIdx.x;
+  const long long first = a.run * run, end = first + a.run < a.slots ? first + a.run : a.slots;
+  for (int e = tid; e < a.E; e += blockDim.x) starts[e] = before[e] = 0;
+  place_run(a, first, end, table, [&] {
+    const int share = (a.runs + nw - 1) / nw, r0 = (tid >> 6) * share, r1 = r0 + share < a.runs ? r0 + share : a.runs;
+    for (int e = tid & 63; e < a.E; e += 64) {
+      int here = 0, all = 0;
+#pragma unroll 16
+      for (int r = r0; r < r1; ++r) {
+        const int v = a.counts[(size_t)r * a.E + e];
+        here += r < run ? v : 0;
+        all += v;
+      }
+      atomicAdd(&starts[e], all);
+      atomicAdd(&before[e], here);
+    }
+    __syncthreads();
+    if (tid < 64) {
+      const int sent = scan_starts(a, starts, run == 0);
+      if (a.order)
+        for (long long p = first + tid; p < end; p += 64)
+          if (p >= sent) a.order[p] = -1;
+    }
+    __syncthreads();
+    for (int e = tid; e < a.E; e += blockDim.x) stack_column(a, table, e, before[e] + starts[e]);
   });
-  if (blockIdx.x == 0 && lane == 0) a.offsets[a.E] = sent;
-  __syncthreads();
-  const long long first = (long long)blockIdx.x * kRouteRun, end = first + kRouteRun < a.slots ? first + kRouteRun : a.slots;
-  place_slots(a, first, end, table);
-  if (a.order)
-    for (long long p = first + lane; p < end; p += 64)
-      if (p >= sent) a.order[p] = -1;
 }
 constexpr long long kRouteOne = 8192;      // up to so many slots one workgroup sorts
+long long route_run(long long slots) {     // slots of a workgroup: whole waves of 64
+  const long long least = 1024, run = (slots + kRouteRuns - 1) / kRouteRuns;
+  return run < least ? least : (run + 255) / 256 * 256;
+}
 
 // ---- rows ----
 // A group of `width` threads (a power of two from 16 to 256) takes a token; the groups of all workgroups go through the tokens.
@@ -361,26 +416,24 @@ hipError_t go_combine_grad(const CombineGradArgs& a, hipStream_t st) {
 
 size_t route_workspace_bytes(long long slots, int E) {
   if (slots <= kRouteOne) return 0;
-  return ((size_t)((slots + kRouteRun - 1) / kRouteRun) * E + E) * sizeof(int32_t);
+  return (size_t)((slots + route_run(slots) - 1) / route_run(slots)) * E * sizeof(int32_t);
 }
 
 hipError_t launch_route(const int32_t* experts, long long slots, int E, int32_t* offsets, int32_t* order, int32_t* position, void* workspace,
                         hipStream_t st) {
-  RouteArgs a{experts, slots, E, 0, offsets, order, position, nullptr, nullptr, 0};
+  RouteArgs a{experts, slots, E, 0, offsets, order, position, (int32_t*)workspace, 0, 0};
   while ((1 << a.bits) < E) ++a.bits;
+  const int most = route_waves(E);
   if (slots <= kRouteOne) {
     const long long waves = (slots + 63) / 64;
-    const int most = route_waves(E);
     const int nw = waves < 1 ? 1 : waves < most ? (int)waves : most;
     route_one_kernel<<<dim3(1), dim3((unsigned)(64 * nw)), 0, st>>>(a);
     return hipGetLastError();
   }
-  a.runs = (int)((slots + kRouteRun - 1) / kRouteRun);
-  a.totals = (int32_t*)workspace;
-  a.counts = a.totals + E;
-  route_count_kernel<<<dim3((unsigned)a.runs), dim3(64), 0, st>>>(a);
-  route_scan_kernel<<<dim3((unsigned)E), dim3(64), 0, st>>>(a);
-  route_place_kernel<<<dim3((unsigned)a.runs), dim3(64), 0, st>>>(a);
+  a.run = route_run(slots);
+  a.runs = (int)((slots + a.run - 1) / a.run);
+  route_count_kernel<<<dim3((unsigned)a.runs), dim3(256), 0, st>>>(a);
+  route_place_kernel<<<dim3((unsigned)a.runs), dim3((unsigned)(64 * (most < 4 ? most : 4))), 0, st>>>(a);
   return hipGetLastError();
 }
 
