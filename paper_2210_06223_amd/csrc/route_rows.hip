@@ -237,6 +237,7 @@ struct DispatchArgs {
   Groups g;
 };
 
+template <bool PAST>
 __global__ __launch_bounds__(256) void dispatch_kernel(DispatchArgs a) {
   const int lane = (int)threadIdx.x % a.g.width;
   const long long slots = a.tokens * a.k, stride = group_count(a.g.width);
@@ -250,7 +251,7 @@ __global__ __launch_bounds__(256) void dispatch_kernel(DispatchArgs a) {
         const uint4_t v = load16(x + at);
         for (int j = 0; j < a.k; ++j) {
           const long long p = to[j];
-          if (p >= 0 && p < slots) store16(a.out.data + p * a.out.pitch + at, v);
+          if (p >= 0 && p < slots) store16<PAST>(a.out.data + p * a.out.pitch + at, v);
         }
       } else {
         for (int j = 0; j < a.k; ++j) {
@@ -287,7 +288,7 @@ struct CombineArgs {
   Groups g;
 };
 
-template <class T>
+template <class T, bool PAST>
 __global__ __launch_bounds__(256) void combine_kernel(CombineArgs a) {
   using E = Elem<T>;
   const int lane = (int)threadIdx.x % a.g.width;
@@ -320,7 +321,7 @@ __global__ __launch_bounds__(256) void combine_kernel(CombineArgs a) {
             for (int i = 0; i < E::PER; ++i) sum[i] += w[j] * f[i];
           }
       }
-      store_piece<T>(a.out.data + t * a.out.pitch + (size_t)c * 16, left, E::narrow(sum));
+      store_piece<T, PAST>(a.out.data + t * a.out.pitch + (size_t)c * 16, left, E::narrow(sum));
     }
   }
 }
@@ -336,7 +337,7 @@ struct CombineGradArgs {
 };
 
 // W waves a token.  Four slots at a time: their rows are read, multiplied by dout for the weights' gradient, and written over.
-template <class T, int W>
+template <class T, int W, bool PAST>
 __global__ __launch_bounds__(256) void combine_grad_kernel(CombineGradArgs a) {
   using E = Elem<T>;
   constexpr int GROUPS = 4 / W;
@@ -371,7 +372,7 @@ __global__ __launch_bounds__(256) void combine_grad_kernel(CombineGradArgs a) {
             float o[E::PER];
 #pragma unroll
             for (int i = 0; i < E::PER; ++i) o[i] = w[j] * g[i];
-            store_piece<T>(a.dy.data + p[j] * a.dy.pitch + (size_t)c * 16, left, E::narrow(o));
+            store_piece<T, PAST>(a.dy.data + p[j] * a.dy.pitch + (size_t)c * 16, left, E::narrow(o));
             if (a.dweights) {
               float f[E::PER];
               E::widen(v[j], f);
@@ -403,12 +404,22 @@ __global__ __launch_bounds__(256) void combine_grad_kernel(CombineGradArgs a) {
       store_piece<T>(a.dy.data + r * a.dy.pitch + (size_t)c * 16, a.cols - c * E::PER, uint4_t{0, 0, 0, 0});
 }
 
-template <class T>
+template <class T, bool PAST>
 hipError_t go_combine_grad(const CombineGradArgs& a, hipStream_t st) {
   if (a.pieces <= 64)
-    combine_grad_kernel<T, 1><<<dim3(group_blocks(a.tokens, 64)), dim3(256), 0, st>>>(a);
+    combine_grad_kernel<T, 1, PAST><<<dim3(group_blocks(a.tokens, 64)), dim3(256), 0, st>>>(a);
   else
-    combine_grad_kernel<T, 4><<<dim3(group_blocks(a.tokens, 256)), dim3(256), 0, st>>>(a);
+    combine_grad_kernel<T, 4, PAST><<<dim3(group_blocks(a.tokens, 256)), dim3(256), 0, st>>>(a);
+  return hipGetLastError();
+}
+template <class T, bool PAST>
+hipError_t go_combine(const CombineArgs& a, hipStream_t st) {
+  combine_kernel<T, PAST><<<dim3(group_blocks(a.tokens, a.g.width)), dim3(256), 0, st>>>(a);
+  return hipGetLastError();
+}
+template <bool PAST>
+hipError_t go_dispatch(const DispatchArgs& a, hipStream_t st) {
+  dispatch_kernel<PAST><<<dim3(group_blocks(a.tokens, a.g.width)), dim3(256), 0, st>>>(a);
   return hipGetLastError();
 }
 
@@ -440,26 +451,23 @@ hipError_t launch_route(const int32_t* experts, long long slots, int E, int32_t*
 hipError_t launch_dispatch(long long tokens, int k, int E, int row_bytes, RowsArg x, const uint8_t* scale, const int32_t* position,
                            const int32_t* offsets, RowsArg out, uint8_t* out_scale, hipStream_t st) {
   const DispatchArgs a{x, out, scale, position, offsets, out_scale, tokens, k, E, row_bytes, groups_for(row_bytes, 16)};
-  dispatch_kernel<<<dim3(group_blocks(tokens, a.g.width)), dim3(256), 0, st>>>(a);
-  return hipGetLastError();
+  return writes_past(tokens * k * row_bytes) ? go_dispatch<true>(a, st) : go_dispatch<false>(a, st);
 }
 
 hipError_t launch_combine(int dtype, long long tokens, int k, int cols, RowsArg y, const float* weights, const int32_t* position, RowsArg base,
                           RowsArg out, hipStream_t st) {
-  const CombineArgs a{y, base, out, weights, position, tokens, k, cols, groups_for(cols * (dtype == LASNET_F32 ? 4 : 2), 16)};
-  const dim3 grid(group_blocks(tokens, a.g.width));
-  if (dtype == LASNET_F32)
-    combine_kernel<float><<<grid, dim3(256), 0, st>>>(a);
-  else
-    combine_kernel<__bf16><<<grid, dim3(256), 0, st>>>(a);
-  return hipGetLastError();
+  const int row_bytes = cols * (dtype == LASNET_F32 ? 4 : 2);
+  const CombineArgs a{y, base, out, weights, position, tokens, k, cols, groups_for(row_bytes, 16)};
+  if (writes_past(tokens * row_bytes)) return dtype == LASNET_F32 ? go_combine<float, true>(a, st) : go_combine<__bf16, true>(a, st);
+  return dtype == LASNET_F32 ? go_combine<float, false>(a, st) : go_combine<__bf16, false>(a, st);
 }
 
 hipError_t launch_combine_backward(int dtype, long long tokens, int k, int E, int cols, RowsArg dout, RowsArg y, const float* weights,
                                    const int32_t* position, const int32_t* offsets, RowsArg dy, float* dweights, hipStream_t st) {
   const int per = dtype == LASNET_F32 ? 4 : 8;
   const CombineGradArgs a{dout, y, dy, weights, position, offsets, dweights, tokens, k, E, cols, (cols + per - 1) / per};
-  return dtype == LASNET_F32 ? go_combine_grad<float>(a, st) : go_combine_grad<__bf16>(a, st);
+  if (writes_past(tokens * k * cols * (16 / per))) return dtype == LASNET_F32 ? go_combine_grad<float, true>(a, st) : go_combine_grad<__bf16, true>(a, st);
+  return dtype == LASNET_F32 ? go_combine_grad<float, false>(a, st) : go_combine_grad<__bf16, false>(a, st);
 }
 
 }  // namespace lasnet

@@ -34,6 +34,10 @@ hipError_t launch_expert_product_dx(long long rows, int E, int n, int k, RowsArg
 hipError_t launch_expert_product_dw(long long rows, int E, int n, int k, RowsArg dy, RowsArg x, const int32_t* offsets, void* dW, bool f32,
                                     hipStream_t st);
 
+// Whether a call that writes so many bytes writes them past the caches: more than the 256 MB Infinity Cache would still hold when the next kernel reads them.
+// Dispatch of 268 MB and the sum that reads it: 156 us with ordinary stores, 116 past the caches; of 134 MB 56 and 61, of 67 MB 31 and 33.
+inline bool writes_past(long long bytes) { return bytes > (192ll << 20); }
+
 namespace {
 
 // A kernel that needs more than 64 KiB of dynamic LDS must be told so once per device.
@@ -56,7 +60,14 @@ typedef float floatx8 __attribute__((ext_vector_type(8)));
 
 struct Piece { uint4_t v; };
 __device__ __forceinline__ uint4_t load16(const unsigned char* p) { return *(const uint4_any*)p; }
-__device__ __forceinline__ void store16(unsigned char* p, uint4_t v) { *(uint4_any*)p = v; }
+// PAST: past the caches (see writes_past)
+template <bool PAST = false>
+__device__ __forceinline__ void store16(unsigned char* p, uint4_t v) {
+  if constexpr (PAST)
+    __builtin_nontemporal_store(v, (uint4_any*)p);
+  else
+    *(uint4_any*)p = v;
+}
 
 __device__ __forceinline__ float bf16_lo(unsigned u) { return __uint_as_float(u << 16); }
 __device__ __forceinline__ float bf16_hi(unsigned u) { return __uint_as_float(u & 0xffff0000u); }
@@ -109,11 +120,11 @@ __device__ __forceinline__ uint4_t load_piece(const unsigned char* p, int n) {
     if (i < n) v[i * E::BYTES / 4] |= E::bits(p + i * E::BYTES) << (8 * (i * E::BYTES % 4));
   return v;
 }
-template <class T>
+template <class T, bool PAST = false>
 __device__ __forceinline__ void store_piece(unsigned char* p, int n, uint4_t v) {
   using E = Elem<T>;
   if (n >= E::PER) {
-    store16(p, v);
+    store16<PAST>(p, v);
     return;
   }
 #pragma unroll

@@ -285,6 +285,32 @@ def test_the_gradient_of_dispatch_is_combine():
     assert float((out.double() * a.double()).sum()) == float((x.double() * B.lasnet_combine_rows(a, position).double()).sum())
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_outputs_larger_than_the_caches(dtype):
+    """Outputs that are written past the caches (more than 192 MiB), in an order of their own: rows are copied or multiplied by powers of two, so exactly."""
+    tokens, k, E, cols = 7001, 4 if dtype == BF16 else 2, 3, 4104
+    g = gen(6)
+    e = torch.randint(-1, E, (tokens, k), generator=g, dtype=torch.int32).cuda()
+    offsets, order, position = B.lasnet_route(e, E)
+    x = torch.randn(tokens, cols, device="cuda").to(dtype)
+    print("large", dtype, flush=True)
+    rows, _ = B.lasnet_dispatch_rows(x, position, offsets)
+    n = int(offsets[-1])
+    assert rows.numel() * rows.element_size() > 192 << 20
+    assert torch.equal(rows[:n], x[order[:n].long() // k]) and not rows[n:].any()
+    w = torch.exp2(torch.randint(-3, 3, (tokens, k), generator=g).float()).cuda()
+    dy, dw = B.lasnet_combine_rows_backward(x, rows, position, offsets, weights=w)
+    flat = w.reshape(-1)[order[:n].long()]
+    assert torch.equal(dy[:n].float(), rows[:n].float() * flat[:, None]) and not dy[n:].any()
+    assert (dw[position < 0] == 0).all() and torch.isfinite(dw).all()
+    del rows, dy
+    one = torch.randperm(14003, generator=g).to(torch.int32).cuda()[:, None]        # one slot a token: the sum is the row
+    y = torch.randn(14003, cols * 4 // x.element_size(), device="cuda").to(dtype)
+    out = B.lasnet_combine_rows(y, one)
+    assert out.numel() * out.element_size() > 192 << 20 and torch.equal(out, y[one[:, 0].long()])
+
+
 # ---------------------------------------------------------------- the experts' products
 
 def groups(rows, E, kind, seed):
