@@ -574,14 +574,31 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void product_tile_kernel(ProductAr
     k0 = __builtin_amdgcn_readfirstlane(bound(a, expert));
     k_end = __builtin_amdgcn_readfirstlane(bound(a, expert + 1));
   } else {
-    const int tiles = row_tiles<BJ>(a), t = xcd_tile(tiles * a.tiles_i);
     int tj;
-    if (t < 0) return;
-    tile_at(t, a.tiles_i, tiles, ti, tj);
-    if (!find_rows<BJ>(a, tj, expert, j0, j_end)) return;
-    expert = __builtin_amdgcn_readfirstlane(expert);
-    j0 = __builtin_amdgcn_readfirstlane(j0);
-    j_end = __builtin_amdgcn_readfirstlane(j_end);
+    if (a.E <= 62) {                                          // an expert (and the rows without one, and their end) for each lane: looked up once
+      const int lane = (int)threadIdx.x & 63;
+      const int lo = lane <= a.E ? bound(a, lane) : (int)a.rows, hi = __shfl(lo, lane < 63 ? lane + 1 : 63);
+      int upto = hi > lo ? (hi - lo + BJ - 1) / BJ : 0;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const int u = __shfl_up(upto, d);
+        if (lane >= d) upto += u;
+      }
+      const int tiles = __builtin_amdgcn_readlane(upto, 63), t = xcd_tile(tiles * a.tiles_i);
+      if (t < 0) return;
+      tile_at(t, a.tiles_i, tiles, ti, tj);
+      expert = __ffsll((long long)__ballot(tj < upto)) - 1;
+      j0 = __builtin_amdgcn_readlane(lo, expert) + (tj - (expert ? __builtin_amdgcn_readlane(upto, expert - 1) : 0)) * BJ;
+      j_end = __builtin_amdgcn_readlane(lo, expert + 1);
+    } else {
+      const int tiles = row_tiles<BJ>(a), t = xcd_tile(tiles * a.tiles_i);
+      if (t < 0) return;
+      tile_at(t, a.tiles_i, tiles, ti, tj);
+      if (!find_rows<BJ>(a, tj, expert, j0, j_end)) return;
+      expert = __builtin_amdgcn_readfirstlane(expert);
+      j0 = __builtin_amdgcn_readfirstlane(j0);
+      j_end = __builtin_amdgcn_readfirstlane(j_end);
+    }
     k0 = 0;
     k_end = expert < a.E ? a.nk : 0;
   }

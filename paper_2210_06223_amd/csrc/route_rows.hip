@@ -241,6 +241,7 @@ template <bool PAST>
 __global__ __launch_bounds__(256) void dispatch_kernel(DispatchArgs a) {
   const int lane = (int)threadIdx.x % a.g.width;
   const long long slots = a.tokens * a.k, stride = group_count(a.g.width);
+  const long long sent = rows_sent(a.offsets, a.E, slots);
   for (long long t = first_group(a.g.width); t < a.tokens; t += stride) {
     const int32_t* to = a.position + t * a.k;
     const unsigned char* x = a.x.data + t * a.x.pitch;
@@ -249,9 +250,13 @@ __global__ __launch_bounds__(256) void dispatch_kernel(DispatchArgs a) {
         // the last piece ends with the row: it may overlap the one before, which writes the same bytes
         const int at = c * 16 <= a.row_bytes - 16 ? c * 16 : a.row_bytes - 16;
         const uint4_t v = load16(x + at);
-        for (int j = 0; j < a.k; ++j) {
-          const long long p = to[j];
-          if (p >= 0 && p < slots) store16<PAST>(a.out.data + p * a.out.pitch + at, v);
+        for (int j0 = 0; j0 < a.k; j0 += 4) {                 // (four places requested at once)
+          int p[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) p[j] = j0 + j < a.k ? to[j0 + j] : -1;
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (p[j] >= 0 && p[j] < slots) store16<PAST>(a.out.data + p[j] * a.out.pitch + at, v);
         }
       } else {
         for (int j = 0; j < a.k; ++j) {
@@ -267,7 +272,7 @@ __global__ __launch_bounds__(256) void dispatch_kernel(DispatchArgs a) {
         if (p >= 0 && p < slots) a.out_scale[p] = a.scale[t];
       }
   }
-  for (long long p = rows_sent(a.offsets, a.E, slots) + first_group(a.g.width); p < slots; p += stride) {
+  for (long long p = sent + first_group(a.g.width); p < slots; p += stride) {
     for (int c = lane; c < a.g.pieces; c += a.g.width) {
       unsigned char* o = a.out.data + p * a.out.pitch;
       if (a.row_bytes >= 16)
