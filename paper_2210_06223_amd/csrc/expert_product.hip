@@ -118,15 +118,30 @@ __device__ __forceinline__ float scale_value(unsigned b) {
   return __uint_as_float(b == 255 ? 0x7fc00000u : b ? b << 23 : 0x00400000u);
 }
 
-template <int BYTES>
-__device__ __forceinline__ uint4_t load_some(const unsigned char* p, int n) {
-  if constexpr (BYTES == 2) return load_piece<__bf16>(p, n);
-  if (n >= 16) return load16(p);
+// The 16 bytes of a row of `size` from byte b on, without a branch where every row has 16 bytes (WIDE): they may begin earlier, so as to end with the row
+// (see cut_piece; what is before a shorter row is not kept, whatever it is).
+template <bool WIDE>
+__device__ __forceinline__ uint4_t row_piece(const unsigned char* row, int b, int size) {
+  if (WIDE || size >= 16) return load16(row + (b < size - 16 ? b : size - 16));
   uint4_t v = {0, 0, 0, 0};
 #pragma unroll
-  for (int i = 0; i < 16; ++i)
-    if (i < n) v[i / 4] |= (unsigned)p[i] << (8 * (i % 4));
+  for (int i = 0; i < 16; ++i) v[i / 4] |= (unsigned)row[i > 16 - size ? i - (16 - size) : 0] << (8 * (i % 4));
   return v;
+}
+// ... of which n were left: moved to the front, zeros behind them.
+__device__ __forceinline__ uint4_t cut_piece(uint4_t v, int n) {
+  const int s = n <= 0 ? 16 : n < 16 ? 16 - n : 0;            // bytes to drop
+#pragma unroll
+  for (int w = 1; w <= 4; w *= 2) {
+    uint4_t u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = i + w < 4 ? v[i + w] : 0u;
+    if (s & 4 * w) v = u;
+  }
+  uint4_t u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) u[i] = __builtin_amdgcn_alignbyte(i < 3 ? v[i + 1] : 0u, v[i], s & 3);
+  return u;
 }
 
 // The wave's NI x NJ blocks of 16 x 16, from column oi0 and row oj0 of the output on, scaled, rounded and stored.  Outputs whose columns and pitch are whole
@@ -197,8 +212,8 @@ __device__ __forceinline__ void store_tile(const ProductArgs& a, unsigned char* 
 }
 
 // 128 x 128 of the output by 4 waves, 64 x 64 each; rows and weights through registers into two LDS stages.
-// FP8: e4m3, else bf16.  IC, JC: held by columns.  RAGGED: the reduction runs over an expert's rows (dW).
-template <bool FP8, bool IC, bool JC, bool RAGGED, bool F32OUT>
+// FP8: e4m3, else bf16.  IC, JC: held by columns.  RAGGED: the reduction runs over an expert's rows (dW).  WIDE: see row_piece.
+template <bool FP8, bool IC, bool JC, bool RAGGED, bool F32OUT, bool WIDE>
 __global__ __launch_bounds__(256) void product_kernel(ProductArgs a) {
   constexpr int BYTES = FP8 ? 1 : 2, KS = 128 / BYTES;
   __shared__ __attribute__((aligned(128))) unsigned char lds[2][2][16384];
@@ -222,30 +237,42 @@ __global__ __launch_bounds__(256) void product_kernel(ProductArgs a) {
 
   floatx4 acc[4][4] = {};
   uint4_t ri[4], rj[4];
+  // Rows beyond the last are read as the last: of i or j, what comes of them is not stored; of k they are cut to nothing.
+  const int row_i = (IC ? a.ni : a.nk) * BYTES, row_j = (JC ? a.nj : a.nk) * BYTES;
+  const unsigned char *pi[4], *pj[4];                         // by rows: the rows of a thread's pieces
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int q = u * 256 + tid, i = i0 + Tile<IC>::row(q), j = j0 + Tile<JC>::row(q);
+    pi[u] = I + (IC ? 0 : (long long)(i < a.ni ? i : a.ni - 1) * a.I.pitch);
+    pj[u] = a.J.data + (JC ? 0 : (long long)(j < j_end ? j : j_end - 1) * a.J.pitch);
+  }
   auto fetch = [&](int k) {
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const int q = u * 256 + tid;
-      if constexpr (IC) {
-        const int kk = k + Tile<true>::row(q), i = i0 + Tile<true>::byte(q) / BYTES;
-        ri[u] = load_some<BYTES>(I + (long long)kk * a.I.pitch + (long long)i * BYTES, kk < k_end ? a.ni - i : 0);
-      } else {
-        const int i = i0 + Tile<false>::row(q), kk = k + Tile<false>::byte(q) / BYTES;
-        ri[u] = load_some<BYTES>(I + (long long)i * a.I.pitch + (long long)kk * BYTES, i < a.ni ? k_end - kk : 0);
-      }
-      if constexpr (JC) {
-        const int kk = k + Tile<true>::row(q), j = j0 + Tile<true>::byte(q) / BYTES;
-        rj[u] = load_some<BYTES>(a.J.data + (long long)kk * a.J.pitch + (long long)j * BYTES, kk < k_end ? j_end - j : 0);
-      } else {
-        const int j = j0 + Tile<false>::row(q), kk = k + Tile<false>::byte(q) / BYTES;
-        rj[u] = load_some<BYTES>(a.J.data + (long long)j * a.J.pitch + (long long)kk * BYTES, j < j_end ? k_end - kk : 0);
-      }
+      const int q = u * 256 + tid, r = k + Tile<IC>::row(q);
+      const unsigned char* row = IC ? I + (long long)(r < k_end ? r : k_end - 1) * a.I.pitch : pi[u];
+      ri[u] = row_piece<WIDE>(row, (IC ? i0 : k) * BYTES + Tile<IC>::byte(q), row_i);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int q = u * 256 + tid, r = k + Tile<JC>::row(q);
+      const unsigned char* row = JC ? a.J.data + (long long)(r < k_end ? r : k_end - 1) * a.J.pitch : pj[u];
+      rj[u] = row_piece<WIDE>(row, (JC ? j0 : k) * BYTES + Tile<JC>::byte(q), row_j);
     }
   };
-  auto stage = [&](int s) {
+  auto stage = [&](int s, int k) {
+    const bool whole_i = k + KS <= k_end && (!IC || i0 + 128 <= a.ni), whole_j = k + KS <= k_end && (!JC || j0 + 128 <= j_end);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int q = u * 256 + tid;
+      if (!whole_i) {
+        const int left = k_end - k, b = Tile<IC>::byte(q);
+        ri[u] = cut_piece(ri[u], IC ? Tile<IC>::row(q) < left ? (a.ni - i0) * BYTES - b : 0 : left * BYTES - b);
+      }
+      if (!whole_j) {
+        const int left = k_end - k, b = Tile<JC>::byte(q);
+        rj[u] = cut_piece(rj[u], JC ? Tile<JC>::row(q) < left ? (j_end - j0) * BYTES - b : 0 : left * BYTES - b);
+      }
       *(uint4_t*)(lds[s][0] + Tile<IC>::place(q)) = ri[u];
       *(uint4_t*)(lds[s][1] + Tile<JC>::place(q)) = rj[u];
     }
@@ -254,7 +281,7 @@ __global__ __launch_bounds__(256) void product_kernel(ProductArgs a) {
   int s = 0;
   if (k0 < k_end) {
     fetch(k0);
-    stage(0);
+    stage(0, k0);
   }
   __syncthreads();
   for (int k = k0; k < k_end; k += KS, s ^= 1) {
@@ -292,7 +319,7 @@ __global__ __launch_bounds__(256) void product_kernel(ProductArgs a) {
           for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fi[i].v, fj[j].v, acc[i][j], 0, 0, 0);
       }
     }
-    if (k + KS < k_end) stage(s ^ 1);
+    if (k + KS < k_end) stage(s ^ 1, k + KS);
     __syncthreads();
   }
 
@@ -428,32 +455,42 @@ __device__ __forceinline__ void tile_at(int t, int ni, int nj, int& i, int& j) {
 // the step too: before the block second from last every read of the stage has been answered, so one barrier there frees the stage for the loads of STAGES
 // steps on and opens the next, whose first fragments are read while the last two blocks' MFMAs run.  MFMAs come first behind the barrier, loads and
 // reads between them: all waves are at the same place there.  The MFMAs of a block are independent of each other.
-template <bool FP8, bool IC, bool JC, bool RAGGED, bool F32OUT, int BI, int BJ, int WI, int WJ, int STAGES>
+//
+// WK > 1: so many groups of WI x WJ waves share the reduction, each a run of its steps through stages of its own; their sums are added in order.
+template <bool FP8, bool IC, bool JC, bool RAGGED, bool F32OUT, int BI, int BJ, int WI, int WJ, int STAGES, int WK = 1>
 __device__ __forceinline__ void tile_product(const ProductArgs& a, unsigned char* product_lds, int expert, int i0, int j0, int j_end, int k0, int k_end) {
   constexpr int BYTES = FP8 ? 1 : 2, KS = 128 / BYTES, NI = BI / WI / 16, NJ = BJ / WJ / 16;
   using SI = Stage<IC, BI, WI * WJ>;
   using SJ = Stage<JC, BJ, WI * WJ>;
   constexpr int STAGE = SI::BYTES + SJ::BYTES, LOADS = SI::SEGS + SJ::SEGS;
   static_assert(NI % 4 == 0, "a ring of four fragments");
-  const unsigned lds = (unsigned)(size_t)(lds_byte*)product_lds;
   int lane = (int)threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) % (WI * WJ);
+  const int group = WK > 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) / (WI * WJ) : 0;
+  const unsigned lds = (unsigned)(size_t)(lds_byte*)product_lds + group * STAGES * STAGE;
   asm volatile("" : "+v"(lane));                               // (nothing of this is worked out before its time and kept)
+  const int steps = k_end > k0 ? (k_end - k0 + WK * KS - 1) / (WK * KS) : 0;
+  if constexpr (WK > 1) {                                      // (a group whose run begins at the end or beyond loads nothing)
+    k0 += group * steps * KS;
+    if (k0 > k_end) k0 = k_end;
+    if (k_end > k0 + steps * KS) k_end = k0 + steps * KS;
+  }
   // where the tiles are in memory, and how far a step takes them
   const unsigned char* I = a.I.data + (RAGGED ? 0 : (long long)(expert < a.E ? expert : 0) * a.i_expert);
   const unsigned pitch_i = (unsigned)a.I.pitch, pitch_j = (unsigned)a.J.pitch, kb = (unsigned)a.nk * BYTES;
   Feed<IC> li;
   Feed<JC> lj;
-  li.start(I + (IC ? (long long)k0 * a.I.pitch + (long long)i0 * BYTES : (long long)i0 * a.I.pitch), a.ni - i0, BI, a.I.pitch, IC ? (unsigned)(a.ni - i0) * BYTES : kb);
-  lj.start(a.J.data + (JC ? (long long)k0 * a.J.pitch + (long long)j0 * BYTES : (long long)j0 * a.J.pitch), j_end - j0, BJ, a.J.pitch,
-           JC ? (unsigned)(j_end - j0) * BYTES : kb);
+  const unsigned skip = RAGGED ? 0 : (unsigned)k0 * BYTES;     // (by rows k0 is a place in the rows)
+  li.start(I + (IC ? (long long)k0 * a.I.pitch + (long long)i0 * BYTES : (long long)i0 * a.I.pitch + skip), a.ni - i0, BI, a.I.pitch,
+           IC ? (unsigned)(a.ni - i0) * BYTES : kb - skip);
+  lj.start(a.J.data + (JC ? (long long)k0 * a.J.pitch + (long long)j0 * BYTES : (long long)j0 * a.J.pitch + skip), j_end - j0, BJ, a.J.pitch,
+           JC ? (unsigned)(j_end - j0) * BYTES : kb - skip);
   const unsigned di = IC ? KS * pitch_i : 128, dj = JC ? KS * pitch_j : 128;
   unsigned off_i[SI::SEGS], off_j[SJ::SEGS];                  // of this lane's pieces from the tile
 #pragma unroll
   for (int s = 0; s < SI::SEGS; ++s) off_i[s] = (unsigned)SI::row(wave * SI::SEGS + s, lane) * pitch_i + (unsigned)SI::byte(wave * SI::SEGS + s, lane);
 #pragma unroll
   for (int s = 0; s < SJ::SEGS; ++s) off_j[s] = (unsigned)SJ::row(wave * SJ::SEGS + s, lane) * pitch_j + (unsigned)SJ::byte(wave * SJ::SEGS + s, lane);
-  const int steps = k_end > k0 ? (k_end - k0 + KS - 1) / KS : 0;
   int l_k = k_end - k0;                                       // what is left of k to load
   unsigned l_to = lds;
   // A step's loads, between the parts of `meanwhile` (which does what is due anyway, in LOADS parts).
@@ -555,12 +592,28 @@ __device__ __forceinline__ void tile_product(const ProductArgs& a, unsigned char
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // (the last loads write to this workgroup's LDS)
   }
+  if constexpr (WK > 1) {
+    floatx4* sums = (floatx4*)product_lds + wave * NI * NJ * 64 + lane;        // [group - 1][wave][block][lane]
+    constexpr int GROUP = WI * WJ * NI * NJ * 64;
+    static_assert((WK - 1) * GROUP * 16 <= WK * STAGES * STAGE, "room for the sums");
+    __syncthreads();
+    if (group) {
+#pragma unroll
+      for (int b = 0; b < NI * NJ; ++b) sums[(group - 1) * GROUP + b * 64] = acc[b / NJ][b % NJ];
+    }
+    __syncthreads();
+    if (group) return;
+#pragma unroll
+    for (int g = 0; g < WK - 1; ++g)
+#pragma unroll
+      for (int b = 0; b < NI * NJ; ++b) acc[b / NJ][b % NJ] += sums[g * GROUP + b * 64];
+  }
   unsigned char* out = a.out.data + (RAGGED ? (long long)expert * a.out_expert : 0);
   store_tile<FP8, F32OUT>(a, out, expert, i0 + wi, j0 + wj, j_end, acc);
 }
 
-template <bool FP8, bool IC, bool JC, bool RAGGED, bool F32OUT, int BI, int BJ, int WI, int WJ, int STAGES>
-__global__ __launch_bounds__(64 * WI * WJ, 2) void product_tile_kernel(ProductArgs a) {
+template <bool FP8, bool IC, bool JC, bool RAGGED, bool F32OUT, int BI, int BJ, int WI, int WJ, int STAGES, int WK = 1>
+__global__ __launch_bounds__(64 * WI * WJ * WK, 2) void product_tile_kernel(ProductArgs a) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char product_lds[];
   int expert, ti, j0, j_end, k0, k_end;
   if constexpr (RAGGED) {
@@ -602,20 +655,20 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void product_tile_kernel(ProductAr
     k0 = 0;
     k_end = expert < a.E ? a.nk : 0;
   }
-  tile_product<FP8, IC, JC, RAGGED, F32OUT, BI, BJ, WI, WJ, STAGES>(a, product_lds, expert, ti * BI, j0, j_end, k0, k_end);
+  tile_product<FP8, IC, JC, RAGGED, F32OUT, BI, BJ, WI, WJ, STAGES, WK>(a, product_lds, expert, ti * BI, j0, j_end, k0, k_end);
 }
 
-template <bool FP8, bool IC, bool JC, bool RAGGED, bool F32OUT, int BI, int BJ, int WI, int WJ, int STAGES>
+template <bool FP8, bool IC, bool JC, bool RAGGED, bool F32OUT, int BI, int BJ, int WI, int WJ, int STAGES, int WK = 1>
 hipError_t go_tile(ProductArgs a, hipStream_t st) {
   a.tiles_i = (a.ni + BI - 1) / BI;
   a.tiles_j = (a.nj + BJ - 1) / BJ;
   const long long tiles = (RAGGED ? (long long)a.E * a.tiles_j : a.rows / BJ + a.E + 1) * a.tiles_i;     // (each expert and the rest may have one that is not full)
-  constexpr int bytes = STAGES * (BI + BJ) * 128;
-  auto kernel = product_tile_kernel<FP8, IC, JC, RAGGED, F32OUT, BI, BJ, WI, WJ, STAGES>;
+  constexpr int bytes = WK * STAGES * (BI + BJ) * 128;
+  auto kernel = product_tile_kernel<FP8, IC, JC, RAGGED, F32OUT, BI, BJ, WI, WJ, STAGES, WK>;
   static std::atomic<unsigned long long> allowed{0};
   const hipError_t e = allow_lds((const void*)kernel, bytes, allowed);
   if (e != hipSuccess) return e;
-  kernel<<<dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(64 * WI * WJ), bytes, st>>>(a);
+  kernel<<<dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(64 * WI * WJ * WK), bytes, st>>>(a);
   return hipGetLastError();
 }
 
@@ -1121,31 +1174,36 @@ bool whole(const ProductArgs& a, int bytes, int B) {
 template <bool FP8, bool IC, bool JC, bool RAGGED, bool F32OUT>
 hipError_t go(ProductArgs a, hipStream_t st) {
   if (whole<IC, JC>(a, FP8 ? 1 : 2, 256)) {
-    // Up to 32 rows, and no more than some four workgroups a CU: rows go straight to registers.
-    // 16 and 32 rows, one expert 1024 x 2048 7.3 and 9.1 us, tiles 14; 16 experts 12.8 and 14.3, tiles 14.7 and 14.9; 64 rows, 16 experts 18, tiles 15; 32 rows,
-    // 8 experts 4096 x 4096 47, tiles 35 (in bf16, whole calls).
+    // Few rows, and not much more than one workgroup a CU: rows go straight to registers.
     if constexpr (!IC && !RAGGED) {
-      const long long units = (a.rows / 16 + (a.rows < a.E ? a.rows : a.E)) * ((a.ni + 15) / 16);
-      if (a.rows <= 32 && units <= 1200) return a.rows <= 16 || a.rows / a.E <= 8 ? go_few<FP8, 1>(a, st) : go_few<FP8, 2>(a, st);
+      const long long blocks = a.E < a.rows ? a.E : a.rows, units = (blocks > (a.rows + 15) / 16 ? blocks : (a.rows + 15) / 16) * ((a.ni + 15) / 16);
+      if (a.rows <= 64 && units <= 384 && (FP8 || a.rows / a.E <= 16 || a.nk <= 1024))
+        return a.rows <= 16 || a.rows / a.E <= 8 ? go_few<FP8, 1>(a, st) : go_few<FP8, 2>(a, st);
     }
-    const long long wide = (a.ni + 255) / 256, groups = a.rows < a.E ? a.rows : a.E;
-    const long long big = (RAGGED ? (long long)a.E * ((a.nj + 255) / 256) : a.rows / 256 + groups / 2) * wide;
-    const bool long_enough = RAGGED || (FP8 ? a.nk > 384 && a.nk % 128 == 0 : a.nk > 192);
-    if (big >= 256 && long_enough && a.ni % 4 == 0 && !(((unsigned long long)a.out.data | (unsigned long long)a.out.pitch | (unsigned long long)a.out_expert) & 15) &&
-        a.out.pitch < (1ll << 31) / 256)
+    // Tiles of BI x BJ, about (how the rows are spread is not known here).
+    const long long groups = a.E < a.rows ? a.E : a.rows;
+    auto tiles = [&](int BI, int BJ) {
+      const long long mean = a.rows / BJ + groups / 2, rows = mean > groups ? mean : groups;
+      return (RAGGED ? (long long)a.E * ((a.nj + BJ - 1) / BJ) : rows) * ((a.ni + BI - 1) / BI);
+    };
+    const bool long_enough = RAGGED || (FP8 ? a.nk >= 256 && a.nk % 128 == 0 : a.nk >= 128);
+    if ((RAGGED ? tiles(256, 256) >= (a.rows / a.E >= 4096 ? 128 : 256) : (a.rows / 256 + groups / 2) * ((a.ni + 255) / 256) >= 200) && long_enough && a.ni % 4 == 0 &&
+        !(((unsigned long long)a.out.data | (unsigned long long)a.out.pitch | (unsigned long long)a.out_expert) & 15) && a.out.pitch < (1ll << 31) / 256)
       return go_stream<FP8, IC, JC, RAGGED, F32OUT>(a, st);
-    const long long i128 = (a.ni + 127) / 128;
-    const long long tiles128 = (RAGGED ? (long long)a.E * ((a.nj + 127) / 128) : a.rows / 128 + groups / 2) * i128;
-    const long long tiles64 = (RAGGED ? (long long)a.E * ((a.nj + 63) / 64) : a.rows / 64 + groups / 2) * i128;
-    if (tiles64 <= 256) return go_tile<FP8, IC, JC, RAGGED, F32OUT, 128, 64, 2, 2, 3>(a, st);
-    if (tiles128 <= 240) return go_tile<FP8, IC, JC, RAGGED, F32OUT, 128, 128, 2, 4, 4>(a, st);
-    if (tiles64 <= 512) return go_tile<FP8, IC, JC, RAGGED, F32OUT, 128, 64, 2, 2, 3>(a, st);
+    const long long steps = (RAGGED ? a.rows / a.E : a.nk) / (FP8 ? 128 : 64);
+    if (steps >= 12 && tiles(64, 32) <= 256) return go_tile<FP8, IC, JC, RAGGED, F32OUT, 64, 32, 1, 2, 3, 4>(a, st);
+    if (steps >= 6 && tiles(64, 64) <= 256) return go_tile<FP8, IC, JC, RAGGED, F32OUT, 64, 64, 1, 4, 4, 2>(a, st);
+    if (tiles(128, 64) <= 256) return go_tile<FP8, IC, JC, RAGGED, F32OUT, 128, 64, 2, 2, 3>(a, st);
+    if (tiles(128, 128) <= 240) return go_tile<FP8, IC, JC, RAGGED, F32OUT, 128, 128, 2, 4, 4>(a, st);
+    if (tiles(128, 64) <= 512) return go_tile<FP8, IC, JC, RAGGED, F32OUT, 128, 64, 2, 2, 3>(a, st);
     return go_tile<FP8, IC, JC, RAGGED, F32OUT, 128, 128, 2, 2, 2>(a, st);
   }
   a.tiles_i = (a.ni + 127) / 128;
   a.tiles_j = (a.nj + 127) / 128;
   const long long tiles = RAGGED ? (long long)a.E * a.tiles_j : a.rows / 128 + a.E + 1;     // (each expert and the rest may have one tile that is not full)
-  product_kernel<FP8, IC, JC, RAGGED, F32OUT><<<dim3((unsigned)(tiles * a.tiles_i)), dim3(256), 0, st>>>(a);
+  const bool wide = (IC ? a.ni : a.nk) >= (FP8 ? 16 : 8) && (JC ? a.nj : a.nk) >= (FP8 ? 16 : 8);
+  auto kernel = wide ? product_kernel<FP8, IC, JC, RAGGED, F32OUT, true> : product_kernel<FP8, IC, JC, RAGGED, F32OUT, false>;
+  kernel<<<dim3((unsigned)(tiles * a.tiles_i)), dim3(256), 0, st>>>(a);
   return hipGetLastError();
 }
 

@@ -3,7 +3,13 @@
 //   s = x + r;  rstd = (mean s^2 + eps)^-1/2;  y = s rstd g;  in 8 bits q = e4m3(y / 2^e), 2^e least with max|y| <= 448 2^e
 //
 // Bound by memory: a row is read once into the registers of W waves (1, 4 or 16), N pieces of 16 bytes a lane, and everything follows from
-// there: the sum of squares and, for 8 bits, the maximum are two reductions over lanes.
+// there: the sum of squares and, for 8 bits, the maximum are two reductions over lanes.  Sums, s and y stay in 32 bits; s is rounded where it is
+// stored (and y follows from what was not), y once, to its own type.
+//
+//   16384 x 4096 bf16 with a residual, out in e4m3 (470 MB): 84 us, 5.6 TB/s, where a large copy reaches 5.0.  4 rows of it: 3.7 us, a launch and one
+//   row's chain of loads and reductions.  Gradients of 25088 x 1024 bf16 (206 MB): 45.7 us, 4.5 TB/s, of which joining the parts of g's takes some 3.
+#include <type_traits>
+
 #include "row_ops.hpp"
 
 namespace lasnet {
@@ -250,8 +256,8 @@ __global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void norm_grad_kernel(NormGra
   for (int i = 0; i < N; ++i) {
     const int c = (i * 64 * W + lane) * E::PER;
 #pragma unroll
-    for (int j = 0; j < E::PER; ++j)
-      if (c + j < part_pitch(a.cols)) part[c + j] = dg[i][j];
+    for (int j = 0; j < E::PER; j += 4)
+      if (c + j < part_pitch(a.cols)) store16((unsigned char*)(part + c + j), Elem<float>::narrow({dg[i][j], dg[i][j + 1], dg[i][j + 2], dg[i][j + 3]}));
   }
 }
 
@@ -284,10 +290,11 @@ __global__ __launch_bounds__(256) void norm_grad_join_kernel(const float* part, 
       if (c + i < cols) dweight[c + i] = sum[0][four * 4 + i];
 }
 
-// Workgroups of the backward pass: as many as the chip runs at once, so that the parts stay few.
+// Workgroups of the backward pass: as many as the chip runs at once, so that the parts stay few (25088 x 1024: 45.7 us a call; 512 of them
+// 49.0, 2048 49.9), and of many rows at least two for each wave that has one at a time (1024 x 4096 15.5 us, one each 19.2; 4 x 4096 6.9, two each 8.2).
 int grad_groups(long long rows, int cols) {
-  const long long most = 1024;
-  const long long need = cols <= 1024 ? (rows + 3) / 4 : rows;
+  const long long most = 1024, each = rows < (cols <= 1024 ? 2048 : 256) ? 1 : 2, at_once = cols <= 1024 ? 4 : 1;
+  const long long need = (rows + at_once * each - 1) / (at_once * each);
   return (int)(need < most ? need : most);
 }
 
@@ -305,7 +312,11 @@ hipError_t pick_grad(const NormGradArgs& a, int groups, float* dweight, hipStrea
   const int pieces = (a.cols + Elem<T>::PER - 1) / Elem<T>::PER;
   if (pieces <= 64) return go_grad<T, 1, 1>(a, groups, dweight, st);
   if (pieces <= 128) return go_grad<T, 1, 2>(a, groups, dweight, st);
-  if (pieces <= 256) return go_grad<T, 4, 1>(a, groups, dweight, st);
+  if (pieces <= 256) {
+    // (32 bits: 16384 x 1001 40.4 us a call by one wave a row, four 45.1; bf16, twice as many elements for a lane: 16384 x 2048 45.4 and 41.9)
+    if constexpr (std::is_same_v<T, float>) return go_grad<T, 1, 4>(a, groups, dweight, st);
+    return go_grad<T, 4, 1>(a, groups, dweight, st);
+  }
   if (pieces <= 512) return go_grad<T, 4, 2>(a, groups, dweight, st);
   if (pieces <= 1024) return go_grad<T, 4, 4>(a, groups, dweight, st);
   return go_grad<T, 16, kNormCols / 1024 / Elem<T>::PER>(a, groups, dweight, st);

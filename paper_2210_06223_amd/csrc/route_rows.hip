@@ -156,8 +156,7 @@ __global__ __launch_bounds__(1024) void route_one_kernel(RouteArgs a) {
 }
 
 // Many slots: a run of them for each workgroup.  Its counts first; then every workgroup adds up the counts of the runs before its own (and of all, for the
-// offsets) and places its slots.  At most kRouteRuns runs, so that this sum stays short.
-constexpr int kRouteRuns = 256;
+// offsets) and places its slots.  See route_run for how many there are.
 __global__ __launch_bounds__(256) void route_count_kernel(RouteArgs a) {
   __shared__ int table[4096];
   for (int e = (int)threadIdx.x; e < a.E; e += 256) table[e] = 0;
@@ -199,8 +198,11 @@ __global__ __launch_bounds__(256) void route_place_kernel(RouteArgs a) {
   });
 }
 constexpr long long kRouteOne = 8192;      // up to so many slots one workgroup sorts
-long long route_run(long long slots) {     // slots of a workgroup: whole waves of 64
-  const long long least = 1024, run = (slots + kRouteRuns - 1) / kRouteRuns;
+// Slots of a workgroup: whole waves of 64.  Every workgroup adds up runs * E counts, so of many experts there are fewer runs: 4 Mi slots of 8 experts 57.8 us in
+// 1024 runs, 71.7 in 256; of 256 experts 136.5 and 114.3 (64 runs 390).
+long long route_run(long long slots, int E) {
+  const long long most = E <= 64 ? 1024 : E <= 1024 ? 256 : 128;
+  const long long least = 1024, run = (slots + most - 1) / most;
   return run < least ? least : (run + 255) / 256 * 256;
 }
 
@@ -411,7 +413,8 @@ __global__ __launch_bounds__(256) void combine_grad_kernel(CombineGradArgs a) {
 
 template <class T, bool PAST>
 hipError_t go_combine_grad(const CombineGradArgs& a, hipStream_t st) {
-  if (a.pieces <= 64)
+  // (16384 x 1024 bf16, four each: one wave a token 49.5 us, four 70.8; 16384 x 2048 122.6 and 109; 8 x 1024 4.3 and 3.6)
+  if (a.pieces <= 64 || (a.pieces <= 128 && a.tokens >= 1024))
     combine_grad_kernel<T, 1, PAST><<<dim3(group_blocks(a.tokens, 64)), dim3(256), 0, st>>>(a);
   else
     combine_grad_kernel<T, 4, PAST><<<dim3(group_blocks(a.tokens, 256)), dim3(256), 0, st>>>(a);
@@ -432,7 +435,7 @@ hipError_t go_dispatch(const DispatchArgs& a, hipStream_t st) {
 
 size_t route_workspace_bytes(long long slots, int E) {
   if (slots <= kRouteOne) return 0;
-  return (size_t)((slots + route_run(slots) - 1) / route_run(slots)) * E * sizeof(int32_t);
+  return (size_t)((slots + route_run(slots, E) - 1) / route_run(slots, E)) * E * sizeof(int32_t);
 }
 
 hipError_t launch_route(const int32_t* experts, long long slots, int E, int32_t* offsets, int32_t* order, int32_t* position, void* workspace,
@@ -446,7 +449,7 @@ hipError_t launch_route(const int32_t* experts, long long slots, int E, int32_t*
     route_one_kernel<<<dim3(1), dim3((unsigned)(64 * nw)), 0, st>>>(a);
     return hipGetLastError();
   }
-  a.run = route_run(slots);
+  a.run = route_run(slots, E);
   a.runs = (int)((slots + a.run - 1) / a.run);
   route_count_kernel<<<dim3((unsigned)a.runs), dim3(256), 0, st>>>(a);
   route_place_kernel<<<dim3((unsigned)a.runs), dim3((unsigned)(64 * (most < 4 ? most : 4))), 0, st>>>(a);

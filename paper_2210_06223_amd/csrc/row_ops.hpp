@@ -56,9 +56,7 @@ inline hipError_t allow_lds(const void* kernel, int bytes, std::atomic<unsigned 
 // rows that start anywhere need no variant of their own; only the end of a row, where less than a piece is left, goes by elements.
 typedef unsigned uint4_t __attribute__((ext_vector_type(4)));
 typedef uint4_t uint4_any __attribute__((aligned(1)));
-typedef float floatx8 __attribute__((ext_vector_type(8)));
 
-struct Piece { uint4_t v; };
 __device__ __forceinline__ uint4_t load16(const unsigned char* p) { return *(const uint4_any*)p; }
 // PAST: past the caches (see writes_past)
 template <bool PAST = false>

@@ -681,3 +681,54 @@ def test_binding_refusals_on_the_device():
         B.lasnet_expert_product(x.bfloat16(), torch.zeros(3, dtype=torch.int32, device="cuda"), torch.zeros(2, 5, 9, dtype=BF16, device="cuda"))
     with pytest.raises(B.LasnetError):
         B.lasnet_norm_rows_backward(x, x, w, torch.zeros(4, device="cuda"), workspace=torch.zeros(4, dtype=torch.uint8, device="cuda"))
+
+
+# few tiles with long reductions, which groups of waves share (with a last group that has less, or nothing), reductions of two to four steps in many tiles, up to 64
+# rows, and rows of less than 16 bytes or that end inside a piece
+FEW_TILES = [(70, 3, 136, 1616, "tail"), (96, 2, 200, 1544, "spread"), (40, 1, 64, 2048, "one"), (50, 2, 1000, 72, "spread"), (3300, 2, 200, 136, "spread"),
+             (5000, 3, 64, 96, "tail"), (2000, 2, 72, 40, "one"), (900, 3, 600, 784, "spread"), (1000, 4, 512, 456, "spread"), (50, 3, 256, 512, "spread"), (64, 2, 128, 1040, "tail"),
+             (3300, 2, 4200, 136, "spread"), (3300, 2, 4200, 256, "tail"), (40, 3, 5, 7, "spread"), (33, 2, 64, 6, "spread"), (20, 2, 3, 100, "tail"), (300, 2, 130, 1001, "spread"),
+             (150, 3, 1001, 130, "tail"), (1700, 2, 15, 17, "spread")]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,E,n,k,kind", FEW_TILES)
+def test_products_of_few_tiles_and_odd_rows(rows, E, n, k, kind):
+    test_expert_product(rows, E, n, k, kind)
+    test_expert_product_gradients(rows, E, n, k, kind)
+    test_products_are_those_of_the_drained_build(rows, E, n, k, kind)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens,k,E", [(6144, 1, 9), (6145, 1, 9), (70000, 2, 8), (300000, 4, 64), (40000, 1, 65), (40000, 2, 1025)])
+def test_route_runs(tokens, k, E):
+    """Sorts by one workgroup and by many, with the counts of few and of many runs."""
+    g = gen(tokens + E)
+    e = torch.randint(-1, E + 1, (tokens, k), generator=g, dtype=torch.int32)                 # (-1 and E: no expert)
+    offsets, order, position = (t.cpu() for t in B.lasnet_route(e.cuda(), E))
+    key = torch.where((e < 0) | (e >= E), E, e).reshape(-1).long()
+    want = torch.argsort(key, stable=True)
+    sent = int((key < E).sum())
+    assert torch.equal(offsets.long(), torch.searchsorted(key[want], torch.arange(E + 1))) and int(offsets[E]) == sent
+    assert torch.equal(order[:sent].long(), want[:sent]) and (order[sent:] == -1).all()
+    where = torch.full((tokens * k,), -1, dtype=torch.int64)
+    where[want[:sent]] = torch.arange(sent)
+    assert torch.equal(position.reshape(-1).long(), where)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,cols,dtype", [(255, 1100, BF16), (256, 1100, BF16), (2049, 1000, F32), (2051, 777, BF16), (1500, 2050, F32), (3000, 4097, BF16)])
+def test_norm_gradient_of_more_rows(rows, cols, dtype):
+    """More rows than workgroups at work, two rows for each."""
+    g = gen(rows)
+    s, dy, dsum, w = rand(g, rows, cols, dtype=dtype), rand(g, rows, cols, dtype=dtype), rand(g, rows, cols, dtype=dtype), rand(g, cols)
+    rstd = torch.rsqrt(s.float().square().mean(-1) + 1e-6)
+    dx, dw = B.lasnet_norm_rows_backward(dy, s, w, rstd, dsum=dsum)
+    S, Y, D, G, R = f64(s), f64(dy), f64(dsum), f64(w), f64(rstd)[:, None]
+    h = Y * G
+    dot, size = (h * S).mean(-1, keepdim=True), (h * S).abs().mean(-1, keepdim=True)
+    ref = D + R * (h - S * R * R * dot)
+    mag = D.abs() + R * (h.abs() + S.abs() * R * R * size)
+    close(dx, ref, HALF[dtype] * ref.abs() + (cols + 8) * U * mag + 1e-40, "dx")
+    terms = (Y * S * R).abs().sum(0)
+    close(dw, (Y * S * R).sum(0), (rows + 4) * U * terms + 1e-40, "dweight")
