@@ -405,11 +405,17 @@ LASNET_API int lasnet_expert_product(const lasnet_rows* x, const uint8_t* scale,
  *   dx[p][c]    = sum_i dy[p][i] * W[e][i][c]                        rows from offsets[E] on are set to zero
  *   dW[e][i][c] = sum over the rows p of expert e of dy[p][i] * x[p][c]        zero for an expert without rows
  * dW: [E][dy.cols][x.cols], dense, dw_dtype F32 or BF16; written, not added to.
+ * _ex with a workspace of lasnet_expert_product_dw_workspace_bytes(rows, E, dy.cols, x.cols) bytes (0: it makes no difference; NULL: the plain call): where
+ * few tiles of dW are sums over many rows, parts of the rows are summed at once and joined in a fixed order (another than the plain call's).
  */
 LASNET_API int lasnet_expert_product_dx(const lasnet_rows* dy, const int32_t* offsets, int E, const void* W,
                                         const lasnet_rows* dx, void* hip_stream);
 LASNET_API int lasnet_expert_product_dw(const lasnet_rows* dy, const lasnet_rows* x, const int32_t* offsets, int E,
                                         void* dW, int dw_dtype, void* hip_stream);
+LASNET_API size_t lasnet_expert_product_dw_workspace_bytes(int64_t rows, int E, int n, int k);
+LASNET_API int lasnet_expert_product_dw_ex(const lasnet_rows* dy, const lasnet_rows* x, const int32_t* offsets, int E,
+                                           void* dW, int dw_dtype, void* workspace, size_t workspace_bytes,
+                                           void* hip_stream);
 
 /*
  * Microbenchmarks for the measurement harness (what this GPU sustains, beside the data-sheet peaks the

@@ -34,12 +34,13 @@ EXPORTS = (
     "lasnet_norm_rows", "lasnet_norm_rows_backward", "lasnet_norm_rows_backward_workspace_bytes",
     "lasnet_route", "lasnet_route_workspace_bytes", "lasnet_dispatch_rows", "lasnet_combine_rows",
     "lasnet_combine_rows_backward", "lasnet_expert_product", "lasnet_expert_product_dx", "lasnet_expert_product_dw",
+    "lasnet_expert_product_dw_ex", "lasnet_expert_product_dw_workspace_bytes",
 )
 
 
 # the calls on rows that _marshal takes
 _ROW_CALLS = ("norm_rows", "norm_rows_backward", "route", "dispatch_rows", "combine_rows", "combine_rows_backward", "expert_product",
-              "expert_product_dx", "expert_product_dw")
+              "expert_product_dx", "expert_product_dw_ex")
 
 
 class LasnetError(RuntimeError):
@@ -119,7 +120,9 @@ def load_library(path: str) -> ctypes.CDLL:
             ("combine_rows_backward", ip, [rp, rp, vp, vp, vp, ip, ip, rp, vp, vp]),
             ("expert_product", ip, [rp, vp, vp, ip, vp, vp, rp, ctypes.c_uint32, vp]),
             ("expert_product_dx", ip, [rp, vp, ip, vp, rp, vp]),
-            ("expert_product_dw", ip, [rp, rp, vp, ip, vp, ip, vp])):
+            ("expert_product_dw", ip, [rp, rp, vp, ip, vp, ip, vp]),
+            ("expert_product_dw_workspace_bytes", sz, [i64, ip, ip, ip]),
+            ("expert_product_dw_ex", ip, [rp, rp, vp, ip, vp, ip, vp, sz, vp])):
         f = getattr(L, "lasnet_" + name)
         f.restype, f.argtypes = result, args
     # the entry points that _marshal calls, by address
@@ -756,20 +759,24 @@ def lasnet_expert_product_dx(dy: torch.Tensor, offsets: torch.Tensor, W: torch.T
 
 
 def lasnet_expert_product_dw(dy: torch.Tensor, x: torch.Tensor, offsets: torch.Tensor, dW: Optional[torch.Tensor] = None,
-                             dtype: Optional[torch.dtype] = None, stream=None) -> torch.Tensor:
-    """dW[e] = sum over the rows p of expert e of dy[p] x[p]^T; dW [E, n, cols] in bfloat16 (or dtype: float32)."""
+                             dtype: Optional[torch.dtype] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """dW[e] = sum over the rows p of expert e of dy[p] x[p]^T; dW [E, n, cols] in bfloat16 (or dtype: float32).  workspace (uint8; made where not given): of
+    lasnet_expert_product_dw_workspace_bytes() bytes."""
+    L = lib()
     if stream is None and dW is not None and dtype is None:
-        L = lib()
-        st = _marshal.expert_product_dw(L.at_expert_product_dw, dy, x, offsets, dW)
+        rows = x.numel() // max(x.shape[-1], 1) if x.dim() else 0
+        need = L.lasnet_expert_product_dw_workspace_bytes(rows, *dW.shape) if workspace is None and rows >= 4096 and dW.dim() == 3 else 0
+        st = _marshal.expert_product_dw(L.at_expert_product_dw_ex, dy, x, offsets, dW, _workspace(workspace, need, x.device, None)[2])
         if st is not None:
-            _check(st, "lasnet_expert_product_dw")
+            _check(st, "lasnet_expert_product_dw_ex")
             return dW
     E, d, v = _offsets(offsets), _rows(dy, "dy"), _rows(x, "x")
     if dW is None:
         dW = torch.empty((E, d.cols, v.cols), dtype=dtype or x.dtype, device=x.device)
     elif dtype is not None and dW.dtype != dtype:
         raise ValueError("dW has another type than dtype")
-    st = lib().lasnet_expert_product_dw(ctypes.byref(d), ctypes.byref(v), _ptr(offsets), E,
-                                        _matrices(dW, E, d.cols, v.cols, torch.bfloat16, torch.float32), _ROW_DTYPES[dW.dtype], _stream(stream))
-    _check(st, "lasnet_expert_product_dw")
+    at, size, keep = _workspace(workspace, L.lasnet_expert_product_dw_workspace_bytes(v.rows, E, d.cols, v.cols), x.device, stream)
+    st = L.lasnet_expert_product_dw_ex(ctypes.byref(d), ctypes.byref(v), _ptr(offsets), E,
+                                       _matrices(dW, E, d.cols, v.cols, torch.bfloat16, torch.float32), _ROW_DTYPES[dW.dtype], at, size, _stream(stream))
+    _check(st, "lasnet_expert_product_dw_ex")
     return dW

@@ -28,6 +28,7 @@ struct ProductArgs {
   long long rows;                  // all rows
   int E, ni, nj, nk;               // output columns; output rows (dW); reduction (forward, dx)
   int tiles_i, tiles_j;            // dW: tiles of an expert's matrix
+  int part_rows, parts;            // dW in parts: rows of a part, and how many parts there may be
   bool relu;
 };
 
@@ -44,10 +45,9 @@ __device__ __forceinline__ product_rsrc_t product_rsrc(const void* p, unsigned b
   return __builtin_amdgcn_make_buffer_rsrc((void*)(((unsigned long long)hi << 32) | lo), 0, (int)__builtin_amdgcn_readfirstlane(bytes), 0x00020000);
 }
 
-// Row tile t of all experts' (BJ rows each, the last of an expert may have fewer) -> its expert, first row and end.  Expert E: the rows that no
+// Row tile t of all experts' (BJ rows each, the last of an expert may have fewer) -> its expert, first row and the expert's end.  Expert E: the rows that no
 // expert has.  false: no such tile.  Every wave of a workgroup finds the same.
-template <int BJ>
-__device__ __forceinline__ bool find_rows(const ProductArgs& a, int t, int& expert, int& first, int& end) {
+__device__ __forceinline__ bool find_rows(const ProductArgs& a, int BJ, int t, int& expert, int& first, int& end) {
   const int lane = (int)threadIdx.x & 63;
   int before = 0;
   for (int e0 = 0; e0 <= a.E; e0 += 64) {
@@ -228,7 +228,7 @@ __global__ __launch_bounds__(256) void product_kernel(ProductArgs a) {
     k0 = bound(a, expert);
     k_end = bound(a, expert + 1);
   } else {
-    if (!find_rows<128>(a, (int)(blockIdx.x / a.tiles_i), expert, j0, j_end)) return;
+    if (!find_rows(a, 128, (int)(blockIdx.x / a.tiles_i), expert, j0, j_end)) return;
     k0 = 0;
     k_end = expert < a.E ? a.nk : 0;                          // (no reduction: zeros)
   }
@@ -647,7 +647,7 @@ __global__ __launch_bounds__(64 * WI * WJ * WK, 2) void product_tile_kernel(Prod
       const int tiles = row_tiles<BJ>(a), t = xcd_tile(tiles * a.tiles_i);
       if (t < 0) return;
       tile_at(t, a.tiles_i, tiles, ti, tj);
-      if (!find_rows<BJ>(a, tj, expert, j0, j_end)) return;
+      if (!find_rows(a, BJ, tj, expert, j0, j_end)) return;
       expert = __builtin_amdgcn_readfirstlane(expert);
       j0 = __builtin_amdgcn_readfirstlane(j0);
       j_end = __builtin_amdgcn_readfirstlane(j_end);
@@ -845,7 +845,7 @@ __global__ __launch_bounds__(512, 2) void product_stream_kernel(ProductArgs a) {
         w.j_end = __builtin_amdgcn_readlane(lo, l + 1);
       } else {
         int e = 0, j0 = 0, j1 = 0;
-        find_rows<256>(a, tj, e, j0, j1);
+        find_rows(a, 256, tj, e, j0, j1);
         w.expert = __builtin_amdgcn_readfirstlane(e);
         w.j0 = __builtin_amdgcn_readfirstlane(j0);
         w.j_end = __builtin_amdgcn_readfirstlane(j1);
@@ -1085,6 +1085,97 @@ hipError_t go_stream(ProductArgs a, hipStream_t st) {
   return hipGetLastError();
 }
 
+// ---- dW of few tiles from many rows: parts of the rows, joined in order ----
+// An expert's rows are cut into parts of part_rows (the last may have fewer), so that all parts' tiles fill the chip once whatever the experts' shares; each part's product
+// is stored in 32 bits, and the second kernel sums an expert's parts in order.
+template <int BI, int BJ, int WI, int WJ, int STAGES, int WK>
+__global__ __launch_bounds__(64 * WI * WJ * WK, 2) void product_part_kernel(ProductArgs a) {
+  extern __shared__ __attribute__((aligned(1024))) unsigned char product_lds[];
+  const int per = a.tiles_i * a.tiles_j, t = xcd_tile(a.parts * per);
+  if (t < 0) return;
+  const int part = t / per;
+  int expert, k0, k_end, ti, tj;
+  if (!find_rows(a, a.part_rows, part, expert, k0, k_end)) return;
+  if (__builtin_amdgcn_readfirstlane(expert) == a.E) return;
+  k0 = __builtin_amdgcn_readfirstlane(k0);
+  k_end = __builtin_amdgcn_readfirstlane(k_end);
+  tile_at(t - part * per, a.tiles_i, a.tiles_j, ti, tj);
+  tile_product<false, true, true, true, true, BI, BJ, WI, WJ, STAGES, WK>(a, product_lds, part, ti * BI, tj * BJ, a.nj, k0, k0 + a.part_rows < k_end ? k0 + a.part_rows : k_end);
+}
+// a.I: the parts; four elements a thread.
+template <bool F32OUT>
+__global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a) {
+  const int lane = (int)threadIdx.x & 63, expert = (int)blockIdx.y;
+  int before = 0, mine = 0;
+  for (int e = lane; e <= expert; e += 64) {
+    const int n = bound(a, e + 1) - bound(a, e), parts = n > 0 ? (n + a.part_rows - 1) / a.part_rows : 0;
+    if (e < expert) before += parts;
+    else mine = parts;
+  }
+#pragma unroll
+  for (int d = 32; d; d >>= 1) {
+    before += __shfl_xor(before, d);
+    mine += __shfl_xor(mine, d);
+  }
+  if (before > a.parts) before = a.parts;                      // (offsets that do not ascend)
+  if (mine > a.parts - before) mine = a.parts - before;
+  const long long size = (long long)a.ni * a.nj, at = ((long long)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (at >= size) return;
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+  const unsigned char* part = a.I.data + ((long long)before * size + at) * 4;
+#pragma unroll 8
+  for (int i = 0; i < mine; ++i) {
+    float v[4];
+    Elem<float>::widen(load16(part + (long long)i * size * 4), v);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) sum[r] += v[r];
+  }
+  unsigned char* out = a.out.data + (expert * size + at) * (F32OUT ? 4 : 2);
+  if constexpr (F32OUT)
+    store16(out, Elem<float>::narrow(sum));
+  else
+    *(uint2_any*)out = uint2_t{bf16_pair(sum[0], sum[1]), bf16_pair(sum[2], sum[3])};
+}
+
+// Whether and how dW is made in parts: parts == 0, not.
+struct Parts {
+  int rows;
+  long long parts;
+  bool narrow;                     // tiles of 64 x 64
+};
+Parts parts_for(long long rows, int E, int n, int k) {
+  const bool narrow = n <= 64 || k <= 64;
+  const int B = narrow ? 64 : 128;
+  const long long per = (long long)((n + B - 1) / B) * ((k + B - 1) / B);
+  if (n % 8 || k % 8 || rows / E < 6144 || E * per > 128) return Parts{0, 0, false};
+  const long long want = 256 / per - E;                       // (2 E or more less E: every expert may have one that is not full)
+  const long long each = (rows + want - 1) / want, part = (each < 512 ? 512 : each + 63) / 64 * 64;
+  return Parts{(int)part, rows / part + E, narrow};
+}
+
+template <int BI, int BJ, int WI, int WJ, int STAGES, int WK>
+hipError_t go_parts(ProductArgs a, const Parts& p, bool f32, void* workspace, hipStream_t st) {
+  a.part_rows = p.rows;
+  a.parts = (int)p.parts;
+  a.tiles_i = (a.ni + BI - 1) / BI;
+  a.tiles_j = (a.nj + BJ - 1) / BJ;
+  ProductArgs b = a;
+  b.out = RowsArg{(unsigned char*)workspace, (long long)a.ni * 4};
+  b.out_expert = (long long)a.ni * a.nj * 4;
+  constexpr int bytes = WK * STAGES * (BI + BJ) * 128;
+  auto kernel = product_part_kernel<BI, BJ, WI, WJ, STAGES, WK>;
+  static std::atomic<unsigned long long> allowed{0};
+  hipError_t e = allow_lds((const void*)kernel, bytes, allowed);
+  if (e != hipSuccess) return e;
+  kernel<<<dim3((unsigned)((p.parts * a.tiles_i * a.tiles_j + 7) / 8 * 8)), dim3(64 * WI * WJ * WK), bytes, st>>>(b);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  a.I = b.out;
+  auto join = f32 ? product_join_kernel<true> : product_join_kernel<false>;
+  join<<<dim3((unsigned)(((long long)a.ni * a.nj + 1023) / 1024), (unsigned)a.E), dim3(256), 0, st>>>(a);
+  return hipGetLastError();
+}
+
 // ---- few rows an expert: bound by reading the weights once ----
 // A workgroup takes 16 columns and up to 16 NJ rows of an expert.  Its four waves share the reduction, each a quarter of it, and read their weights straight into
 // registers (nothing is used twice), DEPTH steps of 128 bytes ahead; the quarters' sums are added in order through LDS.
@@ -1096,7 +1187,7 @@ __global__ __launch_bounds__(256) void product_few_kernel(ProductArgs a) {
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int ti = (int)(blockIdx.x % a.tiles_i), i0 = ti * 16;
   int expert, j0, j_end;
-  if (!find_rows<16 * NJ>(a, (int)(blockIdx.x / a.tiles_i), expert, j0, j_end)) return;
+  if (!find_rows(a, 16 * NJ, (int)(blockIdx.x / a.tiles_i), expert, j0, j_end)) return;
   expert = __builtin_amdgcn_readfirstlane(expert);
   j0 = __builtin_amdgcn_readfirstlane(j0);
   j_end = __builtin_amdgcn_readfirstlane(j_end);
@@ -1212,20 +1303,25 @@ hipError_t go(ProductArgs a, hipStream_t st) {
 hipError_t launch_expert_product(int dtype, long long rows, int E, int n, int k, RowsArg x, const uint8_t* scale, const int32_t* offsets,
                                  const void* W, const float* wscale, RowsArg out, bool relu, hipStream_t st) {
   const int b = dtype == LASNET_E4M3 ? 1 : 2;
-  ProductArgs a{{(unsigned char*)W, (long long)k * b}, x, out, (long long)n * k * b, 0, offsets, scale, wscale, rows, E, n, 0, k, 0, 0, relu};
+  ProductArgs a{{(unsigned char*)W, (long long)k * b}, x, out, (long long)n * k * b, 0, offsets, scale, wscale, rows, E, n, 0, k, 0, 0, 0, 0, relu};
   return dtype == LASNET_E4M3 ? go<true, false, false, false, false>(a, st) : go<false, false, false, false, false>(a, st);
 }
 
 hipError_t launch_expert_product_dx(long long rows, int E, int n, int k, RowsArg dy, const int32_t* offsets, const void* W, RowsArg dx,
                                     hipStream_t st) {
-  ProductArgs a{{(unsigned char*)W, (long long)k * 2}, dy, dx, (long long)n * k * 2, 0, offsets, nullptr, nullptr, rows, E, k, 0, n, 0, 0, false};
+  ProductArgs a{{(unsigned char*)W, (long long)k * 2}, dy, dx, (long long)n * k * 2, 0, offsets, nullptr, nullptr, rows, E, k, 0, n, 0, 0, 0, 0, false};
   return go<false, true, false, false, false>(a, st);
 }
 
+size_t product_dw_workspace_bytes(long long rows, int E, int n, int k) { return (size_t)parts_for(rows, E, n, k).parts * n * k * sizeof(float); }
+
 hipError_t launch_expert_product_dw(long long rows, int E, int n, int k, RowsArg dy, RowsArg x, const int32_t* offsets, void* dW, bool f32,
-                                    hipStream_t st) {
+                                    void* workspace, hipStream_t st) {
   const int b = f32 ? 4 : 2;
-  ProductArgs a{x, dy, {(unsigned char*)dW, (long long)k * b}, 0, (long long)n * k * b, offsets, nullptr, nullptr, rows, E, k, n, 0, 0, 0, false};
+  ProductArgs a{x, dy, {(unsigned char*)dW, (long long)k * b}, 0, (long long)n * k * b, offsets, nullptr, nullptr, rows, E, k, n, 0, 0, 0, 0, 0, false};
+  const Parts p = parts_for(rows, E, n, k);
+  if (workspace && p.parts && whole<true, true>(a, 2, 256))
+    return p.narrow ? go_parts<64, 64, 1, 4, 4, 2>(a, p, f32, workspace, st) : go_parts<128, 128, 2, 4, 4, 1>(a, p, f32, workspace, st);
   return f32 ? go<false, true, true, true, true>(a, st) : go<false, true, true, true, false>(a, st);
 }
 

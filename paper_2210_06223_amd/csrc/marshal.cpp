@@ -440,9 +440,9 @@ PyObject* expert_product_dx(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// (dy, x, offsets, dW)
+// (dy, x, offsets, dW, workspace)
 PyObject* expert_product_dw(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return call(n, 5, [&](Plain& p) {
+  return call(n, 6, [&](Plain& p) {
     lasnet_rows dy, x;
     int E;
     p.rows(a[1], dy);
@@ -453,9 +453,11 @@ PyObject* expert_product_dw(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const auto ty = dW->scalar_type();
     p.need(ty == at::kFloat || ty == at::kBFloat16);
     void* to = p.matrices(a[4], E, dy.cols, x.cols, ty);
+    void* workspace = a[5] == Py_None ? nullptr : p.any<void>(a[5]);
     if (!p.ok) return 0;
-    auto* f = entry<decltype(lasnet_expert_product_dw)>(a[0]);
-    ENQUEUE(f(&dy, &x, offsets, E, to, ty == at::kFloat ? LASNET_F32 : LASNET_BF16, st));
+    const size_t bytes = a[5] == Py_None ? 0 : tensor(a[5])->nbytes();
+    auto* f = entry<decltype(lasnet_expert_product_dw_ex)>(a[0]);
+    ENQUEUE(f(&dy, &x, offsets, E, to, ty == at::kFloat ? LASNET_F32 : LASNET_BF16, workspace, bytes, st));
   });
 }
 

@@ -192,18 +192,29 @@ int lasnet_expert_product_dx(const lasnet_rows* dy, const int32_t* offsets, int 
   return enqueued(launch_expert_product_dx(dy->rows, E, dy->cols, dx->cols, arg(dy), offsets, W, arg(dx), (hipStream_t)hip_stream));
 }
 
-int lasnet_expert_product_dw(const lasnet_rows* dy, const lasnet_rows* x, const int32_t* offsets, int E, void* dW, int dw_dtype,
-                             void* hip_stream) {
+size_t lasnet_expert_product_dw_workspace_bytes(int64_t rows, int E, int n, int k) {
+  if (rows <= 0 || rows > kMaxRows || check_experts(1, E) != LASNET_OK || n <= 0 || k <= 0 || check_tiles(rows, E, k, n) != LASNET_OK) return 0;
+  return product_dw_workspace_bytes(rows, E, n, k);
+}
+
+int lasnet_expert_product_dw_ex(const lasnet_rows* dy, const lasnet_rows* x, const int32_t* offsets, int E, void* dW, int dw_dtype,
+                                void* workspace, size_t workspace_bytes, void* hip_stream) {
   CHECK(check_rows(dy, 1u << LASNET_BF16));
   CHECK(check_rows(x, 1u << LASNET_BF16));
   CHECK(check_experts(1, E));
   if (x->rows != dy->rows) return LASNET_ESHAPE;
   if (!offsets || !dW || (dw_dtype != LASNET_F32 && dw_dtype != LASNET_BF16)) return LASNET_EINVAL;
   CHECK(check_tiles(x->rows, E, x->cols, dy->cols));
+  if (workspace && (workspace_bytes < lasnet_expert_product_dw_workspace_bytes(x->rows, E, dy->cols, x->cols) || ((uintptr_t)workspace & 255))) return LASNET_EINVAL;
   if (dW == x->data || dW == dy->data) return LASNET_EALIAS;
   if (!device_ok()) return LASNET_EHIP;
-  return enqueued(launch_expert_product_dw(x->rows, E, dy->cols, x->cols, arg(dy), arg(x), offsets, dW, dw_dtype == LASNET_F32,
+  return enqueued(launch_expert_product_dw(x->rows, E, dy->cols, x->cols, arg(dy), arg(x), offsets, dW, dw_dtype == LASNET_F32, workspace,
                                            (hipStream_t)hip_stream));
+}
+
+int lasnet_expert_product_dw(const lasnet_rows* dy, const lasnet_rows* x, const int32_t* offsets, int E, void* dW, int dw_dtype,
+                             void* hip_stream) {
+  return lasnet_expert_product_dw_ex(dy, x, offsets, E, dW, dw_dtype, nullptr, 0, hip_stream);
 }
 
 }  // extern "C"

@@ -32,7 +32,8 @@ hipError_t launch_expert_product(int dtype, long long rows, int E, int n, int k,
 hipError_t launch_expert_product_dx(long long rows, int E, int n, int k, RowsArg dy, const int32_t* offsets, const void* W, RowsArg dx,
                                     hipStream_t st);
 hipError_t launch_expert_product_dw(long long rows, int E, int n, int k, RowsArg dy, RowsArg x, const int32_t* offsets, void* dW, bool f32,
-                                    hipStream_t st);
+                                    void* workspace, hipStream_t st);
+size_t product_dw_workspace_bytes(long long rows, int E, int n, int k);
 
 // Whether a call that writes so many bytes writes them past the caches: more than the 256 MB Infinity Cache would still hold when the next kernel reads them.
 // Dispatch of 268 MB and the sum that reads it: 156 us with ordinary stores, 116 past the caches; of 134 MB 56 and 61, of 67 MB 31 and 33.

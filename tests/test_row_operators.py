@@ -732,3 +732,50 @@ def test_norm_gradient_of_more_rows(rows, cols, dtype):
     close(dx, ref, HALF[dtype] * ref.abs() + (cols + 8) * U * mag + 1e-40, "dx")
     terms = (Y * S * R).abs().sum(0)
     close(dw, (Y * S * R).sum(0), (rows + 4) * U * terms + 1e-40, "dweight")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,E,n,k,kind", [(13000, 2, 136, 200, "spread"), (7001, 1, 64, 40, "one"), (20000, 3, 72, 520, "tail"), (6500, 1, 256, 256, "one"), (12500, 2, 64, 72, "none"),
+                                             (26000, 4, 520, 264, "spread")])
+def test_weights_gradient_in_parts(rows, E, n, k, kind):
+    """Few tiles from many rows, with a workspace and without: both right, each the same bits every time and as in the drained build."""
+    from paper_2210_06223_amd import build
+    L, g, o = B.lib(), gen(rows), groups(rows, E, kind, rows)
+    offsets = torch.from_numpy(o.astype(np.int32)).cuda()
+    x, dy = rand(g, rows, k, dtype=BF16, pad=8), rand(g, rows, n, dtype=BF16)
+    need = L.lasnet_expert_product_dw_workspace_bytes(rows, E, n, k)
+    assert need > 0
+    ref, size, terms = (torch.zeros(E, n, k, dtype=torch.float64) for _ in range(3))
+    for e in range(E):
+        s = slice(int(o[e]), int(o[e + 1]))
+        ref[e], size[e], terms[e] = f64(dy)[s].T @ f64(x)[s], f64(dy)[s].T.abs() @ f64(x)[s].abs(), s.stop - s.start
+    dyr, xr = (B._rows(t, "rows") for t in (dy, x))
+    ws = torch.full((need + 256,), 255, dtype=torch.uint8, device="cuda")                    # (NaN wherever nothing is written)
+    for dtype, code in ((BF16, B.LASNET_BF16), (F32, B.LASNET_F32)):
+        bound = HALF[dtype] * ref.abs() + (terms + 2) * U * size + 1e-40
+        plain, parts = (torch.full((E, n, k), 7.0, dtype=dtype, device="cuda") for _ in range(2))
+        st = torch.cuda.current_stream().cuda_stream
+        assert L.lasnet_expert_product_dw(ctypes.byref(dyr), ctypes.byref(xr), offsets.data_ptr(), E, plain.data_ptr(), code, st) == 0
+        assert L.lasnet_expert_product_dw_ex(ctypes.byref(dyr), ctypes.byref(xr), offsets.data_ptr(), E, parts.data_ptr(), code, ws.data_ptr(), need, st) == 0
+        assert (ws[need:] == 255).all()
+        for t in (plain, parts):
+            close(t, ref, bound, "dW")
+        assert torch.equal(parts, B.lasnet_expert_product_dw(dy, x, offsets, dtype=dtype)), "the binding makes a workspace"
+        again = torch.empty_like(parts)
+        assert torch.equal(parts, B.lasnet_expert_product_dw(dy, x, offsets, dW=again, workspace=ws[:need])), "a given workspace, natively marshalled"
+        mine = B._lib
+        try:
+            B._lib = B.load_library(build.LIB_CHECK)
+            assert torch.equal(parts, B.lasnet_expert_product_dw(dy, x, offsets, dtype=dtype)), "drained"
+        finally:
+            B._lib = mine
+        a = (ctypes.byref(dyr), ctypes.byref(xr), offsets.data_ptr(), E, parts.data_ptr(), code)
+        assert L.lasnet_expert_product_dw_ex(*a, ws.data_ptr(), need - 1, st) != 0 and L.lasnet_expert_product_dw_ex(*a, ws.data_ptr() + 8, need, st) != 0
+
+
+def test_workspace_of_the_weights_gradient():
+    """Only where few tiles are sums over many rows; 0 for what the call refuses."""
+    f = B.lib().lasnet_expert_product_dw_workspace_bytes
+    assert f(32768, 1, 1024, 256) > 0 and f(32768, 16, 4096, 2048) == 0 and f(100, 1, 64, 64) == 0 and f(32768, 1, 1023, 256) == 0
+    assert f(0, 1, 64, 64) == f(-5, 1, 64, 64) == f(32768, 0, 64, 64) == f(32768, 1, 0, 64) == f(32768, 1, 64, -8) == 0
+    assert f(1 << 30, 1, 64, 64) < 1 << 24
