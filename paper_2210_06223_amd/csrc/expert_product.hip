@@ -8,6 +8,10 @@
 // consecutive i in a lane.  An operand is held by ROWS (k is contiguous in memory: x, dy, and W in the forward product) or by COLUMNS (i or j
 // is: W for dx, both for dW).  In LDS a tile by rows lies as it is read, 128 bytes of k a row; one by columns lies as it is in memory, and
 // the transposing LDS read (ds_read_b64_tr_b16: 4 k x 16 columns for 16 lanes) turns it.
+//
+// Five kernels, from what bounds them: many tiles, the matrix cores (product_stream_kernel); fewer, the latency of a step and the loads to LDS, 64 bytes a clock
+// for a CU (product_tile_kernel; dW from many rows in parts); few rows, the weights' bytes (product_few_kernel); rows of any alignment through registers
+// (product_kernel).  go() says when which one runs.  Sums are held in 32 bits and rounded once, where they are stored.
 #include <type_traits>
 
 #include "row_ops.hpp"
@@ -211,7 +215,10 @@ __device__ __forceinline__ void store_tile(const ProductArgs& a, unsigned char* 
   }
 }
 
-// 128 x 128 of the output by 4 waves, 64 x 64 each; rows and weights through registers into two LDS stages.
+// Any alignment and width: 128 x 128 of the output by 4 waves, 64 x 64 each; rows and weights through registers into two LDS stages, the next step's loads in
+// flight while this one's products run.  Bound by those loads: pieces that begin anywhere touch two lines of the caches.  16384 rows of 8 experts, 2047 x 2049:
+// bf16 224 us, its gradients 256 and 266, 8 bits 141; a branch for each piece's end instead of row_piece: 222, 322, 421, 160, and with few columns up to five
+// times as long (28473 rows, 2103 x 226, gradient of the weights 199 and 1010).
 // FP8: e4m3, else bf16.  IC, JC: held by columns.  RAGGED: the reduction runs over an expert's rows (dW).  WIDE: see row_piece.
 template <bool FP8, bool IC, bool JC, bool RAGGED, bool F32OUT, bool WIDE>
 __global__ __launch_bounds__(256) void product_kernel(ProductArgs a) {
@@ -673,6 +680,10 @@ hipError_t go_tile(ProductArgs a, hipStream_t st) {
 }
 
 // ---- many tiles: 256 x 256 by eight waves, one workgroup a CU that goes from tile to tile without letting its loads run dry ----
+// 8192 x 8192 x 8192 bf16 810 us, 1360 TFLOP/s (the library's product 745 to 757 us), 8 bits 412 us, 2660 TFLOP/s.  Reductions of 2048 leave a tile's
+// stores more to say: 128 KiB from each of 256 CUs at once, some 9 us a round of tiles at the rate memory takes them (16384 x 2048 x 2048 128 to 137 us, 1000 to
+// 1070 TFLOP/s; 32768 x 4096 x 2048 in 8 bits 301 us, 1830 TFLOP/s).
+//
 // LDS holds five units of 32 KiB, each the 128 bytes of k of one operand's tile, loaded in the order J0 I0 J1 I1 ... of the workgroup's steps, whatever
 // tile they belong to.  In step s a wave multiplies the I fragments of its eight blocks, a ring of four read three blocks ahead, with the four J fragments it
 // holds, and reads the J fragments of step s + 1.  Two barriers a step, each of which waits for one unit, frees one and is followed by the loads of one:
@@ -1087,7 +1098,8 @@ hipError_t go_stream(ProductArgs a, hipStream_t st) {
 
 // ---- dW of few tiles from many rows: parts of the rows, joined in order ----
 // An expert's rows are cut into parts of part_rows (the last may have fewer), so that all parts' tiles fill the chip once whatever the experts' shares; each part's product
-// is stored in 32 bits, and the second kernel sums an expert's parts in order.
+// is stored in 32 bits, and the second kernel sums an expert's parts in order.  Bound by the rows' bytes and the loads to LDS, then by the parts' 16 MB: one expert,
+// 1024 x 256 from 32768 rows 32 us, 512 x 512 from 16384 rows 22 (groups of waves in one workgroup a tile: 95 and 48).
 template <int BI, int BJ, int WI, int WJ, int STAGES, int WK>
 __global__ __launch_bounds__(64 * WI * WJ * WK, 2) void product_part_kernel(ProductArgs a) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char product_lds[];
@@ -1143,6 +1155,7 @@ struct Parts {
   long long parts;
   bool narrow;                     // tiles of 64 x 64
 };
+// 6144 rows an expert: with 4096 (208 x 944) one workgroup a tile takes 17 us, two launches and the parts' way through memory are no less than 10.
 Parts parts_for(long long rows, int E, int n, int k) {
   const bool narrow = n <= 64 || k <= 64;
   const int B = narrow ? 64 : 128;
@@ -1178,7 +1191,8 @@ hipError_t go_parts(ProductArgs a, const Parts& p, bool f32, void* workspace, hi
 
 // ---- few rows an expert: bound by reading the weights once ----
 // A workgroup takes 16 columns and up to 16 NJ rows of an expert.  Its four waves share the reduction, each a quarter of it, and read their weights straight into
-// registers (nothing is used twice), DEPTH steps of 128 bytes ahead; the quarters' sums are added in order through LDS.
+// registers (nothing is used twice), DEPTH steps of 128 bytes ahead; the quarters' sums are added in order through LDS.  One row, 4096 x 4096: 8.2 us in bf16
+// (4.1 TB/s), 6.2 in 8 bits.
 template <bool FP8, int NJ>
 __global__ __launch_bounds__(256) void product_few_kernel(ProductArgs a) {
   constexpr int BYTES = FP8 ? 1 : 2, DEPTH = NJ == 1 ? 8 : 4;
@@ -1265,7 +1279,9 @@ bool whole(const ProductArgs& a, int bytes, int B) {
 template <bool FP8, bool IC, bool JC, bool RAGGED, bool F32OUT>
 hipError_t go(ProductArgs a, hipStream_t st) {
   if (whole<IC, JC>(a, FP8 ? 1 : 2, 256)) {
-    // Few rows, and not much more than one workgroup a CU: rows go straight to registers.
+    // Few rows, and not much more than one workgroup a CU: rows go straight to registers.  1 row, 1024 x 2048 5.7 us (tiles 7.8), 4096 x 4096 8.2 (11.2); 16 rows of
+    // 4 experts, 1024 x 2048 6.4 (7.8).  768 workgroups (24 rows of 2 experts, 4096 x 4096) 19.2 (14.1); in bf16 with more than 16 rows an expert and a
+    // longer reduction: 32 rows, 1024 x 2048 8.7 (7.9; 8 bits 6.2 and 6.7).
     if constexpr (!IC && !RAGGED) {
       const long long blocks = a.E < a.rows ? a.E : a.rows, units = (blocks > (a.rows + 15) / 16 ? blocks : (a.rows + 15) / 16) * ((a.ni + 15) / 16);
       if (a.rows <= 64 && units <= 384 && (FP8 || a.rows / a.E <= 16 || a.nk <= 1024))
@@ -1278,10 +1294,20 @@ hipError_t go(ProductArgs a, hipStream_t st) {
       return (RAGGED ? (long long)a.E * ((a.nj + BJ - 1) / BJ) : rows) * ((a.ni + BI - 1) / BI);
     };
     const bool long_enough = RAGGED || (FP8 ? a.nk >= 256 && a.nk % 128 == 0 : a.nk >= 128);
+    // Tiles of 256 x 256 where there are enough for the chip: 16384 rows of 4 experts, 2048 x 2048 bf16 128 us (128 x 128: 152), 8 bits 77 (99), dW of 8 experts 134
+    // (223).  With 136 of them, 8192 rows of 4 experts, 1024 x 2048, evenly spread, 38 (34), unevenly 57 (60).  dW has few of them with long reductions: 128
+    // tiles of 4096 rows 87 (125), of 2048 rows 45 (38).  Short reductions: 32768 x 2048 x 128 in bf16 66 (69), x 256 in 8 bits 70 (74); less does not
+    // fill the steps that a tile has at least.
     if ((RAGGED ? tiles(256, 256) >= (a.rows / a.E >= 4096 ? 128 : 256) : (a.rows / 256 + groups / 2) * ((a.ni + 255) / 256) >= 200) && long_enough && a.ni % 4 == 0 &&
         !(((unsigned long long)a.out.data | (unsigned long long)a.out.pitch | (unsigned long long)a.out_expert) & 15) && a.out.pitch < (1ll << 31) / 256)
       return go_stream<FP8, IC, JC, RAGGED, F32OUT>(a, st);
     const long long steps = (RAGGED ? a.rows / a.E : a.nk) / (FP8 ? 128 : 64);
+    // Tiles that all run at once, one workgroup a CU, with the reduction shared by groups of waves: a step of one wave a SIMD is 0.2 to 0.3 us of latency, whatever
+    // the depth of the loads ahead.  64 x 32 by four groups: 64 rows, 1024 x 4096 11.2 us (128 x 64 by one group 23.3), 4096 x 1024 6.4 (9.1), 9 steps (300 rows
+    // of 8 experts, 1024 x 520) 7.2 (6.9).  64 x 64 by two: 1024 x 1024 x 1024 8.0 (9.3), 2048 x 512 x 2048 10.5 (14.0), 4 steps 6.2 (5.8).
+    // Shorter or more of them: 128 x 64 in three stages, two workgroups a CU; 1024 rows of 16 experts, 1024 x 2048 16.2 (128 x 128 in four stages 21.2, in two
+    // 28.3), 8000 rows of 4, 512 x 2048 24.9 (39.7, 35.8).  128 x 128 by eight waves where one round does: 2048 rows of 16, 1024 x 2048 22.0 (25.5, 29.3).
+    // Beyond, 128 x 128 by four waves, two workgroups a CU: dW of 3000 rows, 8 experts 1024 x 1024 18.7 (128 x 64 22.7).
     if (steps >= 12 && tiles(64, 32) <= 256) return go_tile<FP8, IC, JC, RAGGED, F32OUT, 64, 32, 1, 2, 3, 4>(a, st);
     if (steps >= 6 && tiles(64, 64) <= 256) return go_tile<FP8, IC, JC, RAGGED, F32OUT, 64, 64, 1, 4, 4, 2>(a, st);
     if (tiles(128, 64) <= 256) return go_tile<FP8, IC, JC, RAGGED, F32OUT, 128, 64, 2, 2, 3>(a, st);

@@ -4,6 +4,9 @@
 // by one ballot for each bit of its number, the first of them adds their count to the wave's table in LDS, and a lane's rank is the
 // table's value before plus the lanes ahead of it.  What moves rows is bound by memory: each token's row is read once, the k copies are written
 // (or read) once, and sums run over j in order, so nothing depends on timing.
+//
+//   sort: a chain of LDS and memory accesses: 32 slots of 64 experts 3 us, 65536 10, 4 Mi 71.  Rows, at the rate of large copies: dispatch of 16384 x 2048 bf16 to
+//   four experts each (335 MB) with the sort 60 us, sum of them into the residual (386 MB) 74, its gradient (604 MB) 109.
 #include "row_ops.hpp"
 
 namespace lasnet {
@@ -197,7 +200,8 @@ __global__ __launch_bounds__(256) void route_place_kernel(RouteArgs a) {
     for (int e = tid; e < a.E; e += blockDim.x) stack_column(a, table, e, before[e] + starts[e]);
   });
 }
-constexpr long long kRouteOne = 8192;      // up to so many slots one workgroup sorts
+// Up to so many slots one workgroup sorts (of 64 experts: 4096 slots 7.3 us, by two launches 9.4; 8192 slots 11.7 and 10.2).
+constexpr long long kRouteOne = 6144;
 // Slots of a workgroup: whole waves of 64.  Every workgroup adds up runs * E counts, so of many experts there are fewer runs: 4 Mi slots of 8 experts 57.8 us in
 // 1024 runs, 71.7 in 256; of 256 experts 136.5 and 114.3 (64 runs 390).
 long long route_run(long long slots, int E) {
@@ -207,7 +211,8 @@ long long route_run(long long slots, int E) {
 }
 
 // ---- rows ----
-// A group of `width` threads (a power of two from 16 to 256) takes a token; the groups of all workgroups go through the tokens.
+// A group of `width` threads (a power of two from 16 to 256) takes a token; the groups of all workgroups go through the tokens.  16384 x 64 bf16, four each: groups
+// of 16 threads 4.0 us, of 256 15.5; 16384 x 1024: 26 either way.
 struct Groups {
   int width;                       // threads of a group
   int pieces;                      // of 16 bytes in a row, the last one may have less
@@ -306,7 +311,7 @@ __global__ __launch_bounds__(256) void combine_kernel(CombineArgs a) {
       const int left = a.cols - c * E::PER;
       float sum[E::PER] = {};
       if (a.base.data) E::widen(load_piece<T>(a.base.data + t * a.base.pitch + (size_t)c * 16, left), sum);
-      for (int j0 = 0; j0 < a.k; j0 += 4) {
+      for (int j0 = 0; j0 < a.k; j0 += 4) {                    // (four rows requested at once)
         uint4_t v[4];
         float w[4];
         bool sent[4];
