@@ -216,12 +216,19 @@ long long route_run(long long slots, int E) {
 struct Groups {
   int width;                       // threads of a group
   int pieces;                      // of 16 bytes in a row, the last one may have less
+  int part;                        // pieces of a row that a workgroup (blockIdx.y) takes
+  __device__ __forceinline__ int first() const { return (int)blockIdx.y * part; }
+  __device__ __forceinline__ int end() const { return first() + part < pieces ? first() + part : pieces; }
 };
 __device__ __forceinline__ long long first_group(int width) { return ((long long)blockIdx.x * 256 + threadIdx.x) / width; }
 __device__ __forceinline__ long long group_count(int width) { return (long long)gridDim.x * (256 / width); }
-Groups groups_for(int row_bytes, int least) {
-  Groups g{least, (row_bytes + 15) / 16};
+Groups groups_for(long long tokens, int row_bytes, int least) {
+  Groups g{least, (row_bytes + 15) / 16, 0};
   while (g.width < 256 && g.width < g.pieces) g.width *= 2;
+  // Few tokens with wide rows: workgroups share a row.  Sum for 155 tokens of four rows of 7428 floats 5.1 us (one workgroup a token 16.3), for 500 of 4096 bf16 4.6 (5.8);
+  // for 1000 of 4096 10.3 (9.6), so those are left whole.
+  g.part = g.pieces;
+  while (g.part > 256 && tokens * ((g.pieces + g.part - 1) / g.part) < 512) g.part = (g.part + 1) / 2;
   return g;
 }
 unsigned group_blocks(long long tokens, int width) {
@@ -252,7 +259,7 @@ __global__ __launch_bounds__(256) void dispatch_kernel(DispatchArgs a) {
   for (long long t = first_group(a.g.width); t < a.tokens; t += stride) {
     const int32_t* to = a.position + t * a.k;
     const unsigned char* x = a.x.data + t * a.x.pitch;
-    for (int c = lane; c < a.g.pieces; c += a.g.width) {
+    for (int c = a.g.first() + lane; c < a.g.end(); c += a.g.width) {
       if (a.row_bytes >= 16) {
         // the last piece ends with the row: it may overlap the one before, which writes the same bytes
         const int at = c * 16 <= a.row_bytes - 16 ? c * 16 : a.row_bytes - 16;
@@ -273,21 +280,21 @@ __global__ __launch_bounds__(256) void dispatch_kernel(DispatchArgs a) {
         }
       }
     }
-    if (a.scale)
+    if (a.scale && blockIdx.y == 0)
       for (int j = lane; j < a.k; j += a.g.width) {
         const long long p = to[j];
         if (p >= 0 && p < slots) a.out_scale[p] = a.scale[t];
       }
   }
   for (long long p = sent + first_group(a.g.width); p < slots; p += stride) {
-    for (int c = lane; c < a.g.pieces; c += a.g.width) {
+    for (int c = a.g.first() + lane; c < a.g.end(); c += a.g.width) {
       unsigned char* o = a.out.data + p * a.out.pitch;
       if (a.row_bytes >= 16)
         store16(o + (c * 16 <= a.row_bytes - 16 ? c * 16 : a.row_bytes - 16), uint4_t{0, 0, 0, 0});
       else
         for (int i = 0; i < a.row_bytes; ++i) o[i] = 0;
     }
-    if (a.scale && lane == 0) a.out_scale[p] = 127;
+    if (a.scale && lane == 0 && blockIdx.y == 0) a.out_scale[p] = 127;
   }
 }
 
@@ -307,7 +314,7 @@ __global__ __launch_bounds__(256) void combine_kernel(CombineArgs a) {
   const long long slots = a.tokens * a.k, stride = group_count(a.g.width);
   for (long long t = first_group(a.g.width); t < a.tokens; t += stride) {
     const int32_t* from = a.position + t * a.k;
-    for (int c = lane; c < a.g.pieces; c += a.g.width) {
+    for (int c = a.g.first() + lane; c < a.g.end(); c += a.g.width) {
       const int left = a.cols - c * E::PER;
       float sum[E::PER] = {};
       if (a.base.data) E::widen(load_piece<T>(a.base.data + t * a.base.pitch + (size_t)c * 16, left), sum);
@@ -427,12 +434,12 @@ hipError_t go_combine_grad(const CombineGradArgs& a, hipStream_t st) {
 }
 template <class T, bool PAST>
 hipError_t go_combine(const CombineArgs& a, hipStream_t st) {
-  combine_kernel<T, PAST><<<dim3(group_blocks(a.tokens, a.g.width)), dim3(256), 0, st>>>(a);
+  combine_kernel<T, PAST><<<dim3(group_blocks(a.tokens, a.g.width), (unsigned)((a.g.pieces + a.g.part - 1) / a.g.part)), dim3(256), 0, st>>>(a);
   return hipGetLastError();
 }
 template <bool PAST>
 hipError_t go_dispatch(const DispatchArgs& a, hipStream_t st) {
-  dispatch_kernel<PAST><<<dim3(group_blocks(a.tokens, a.g.width)), dim3(256), 0, st>>>(a);
+  dispatch_kernel<PAST><<<dim3(group_blocks(a.tokens, a.g.width), (unsigned)((a.g.pieces + a.g.part - 1) / a.g.part)), dim3(256), 0, st>>>(a);
   return hipGetLastError();
 }
 
@@ -463,14 +470,14 @@ hipError_t launch_route(const int32_t* experts, long long slots, int E, int32_t*
 
 hipError_t launch_dispatch(long long tokens, int k, int E, int row_bytes, RowsArg x, const uint8_t* scale, const int32_t* position,
                            const int32_t* offsets, RowsArg out, uint8_t* out_scale, hipStream_t st) {
-  const DispatchArgs a{x, out, scale, position, offsets, out_scale, tokens, k, E, row_bytes, groups_for(row_bytes, 16)};
+  const DispatchArgs a{x, out, scale, position, offsets, out_scale, tokens, k, E, row_bytes, groups_for(tokens, row_bytes, 16)};
   return writes_past(tokens * k * row_bytes) ? go_dispatch<true>(a, st) : go_dispatch<false>(a, st);
 }
 
 hipError_t launch_combine(int dtype, long long tokens, int k, int cols, RowsArg y, const float* weights, const int32_t* position, RowsArg base,
                           RowsArg out, hipStream_t st) {
   const int row_bytes = cols * (dtype == LASNET_F32 ? 4 : 2);
-  const CombineArgs a{y, base, out, weights, position, tokens, k, cols, groups_for(row_bytes, 16)};
+  const CombineArgs a{y, base, out, weights, position, tokens, k, cols, groups_for(tokens, row_bytes, 16)};
   if (writes_past(tokens * row_bytes)) return dtype == LASNET_F32 ? go_combine<float, true>(a, st) : go_combine<__bf16, true>(a, st);
   return dtype == LASNET_F32 ? go_combine<float, false>(a, st) : go_combine<__bf16, false>(a, st);
 }

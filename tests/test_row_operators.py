@@ -779,3 +779,30 @@ def test_workspace_of_the_weights_gradient():
     assert f(32768, 1, 1024, 256) > 0 and f(32768, 16, 4096, 2048) == 0 and f(100, 1, 64, 64) == 0 and f(32768, 1, 1023, 256) == 0
     assert f(0, 1, 64, 64) == f(-5, 1, 64, 64) == f(32768, 0, 64, 64) == f(32768, 1, 0, 64) == f(32768, 1, 64, -8) == 0
     assert f(1 << 30, 1, 64, 64) < 1 << 24
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens,k,cols", [(1, 1, 5000), (3, 3, 8200), (40, 2, 16381), (300, 2, 4100), (2, 5, 70001)])
+def test_few_tokens_with_wide_rows(tokens, k, cols):
+    """Rows that several workgroups share: moved bit for bit (with scales, and zeros behind the last), and summed with powers of two, which round once."""
+    g, E = gen(tokens + cols), 7
+    e = torch.randint(-1, E, (tokens, k), generator=g, dtype=torch.int32).cuda()
+    e[0, 0] = 2
+    offsets, order, position = B.lasnet_route(e, E)
+    n = int(offsets[E])
+    src = order[:n].long() // k
+    for dtype in (BF16, F32, E4M3):
+        x = (torch.randint(1, 120, (tokens, cols + 3), generator=g, dtype=torch.uint8).cuda().view(E4M3) if dtype == E4M3 else rand(g, tokens, cols + 3, dtype=dtype))[:, :cols]
+        scale = torch.randint(1, 250, (tokens,), generator=g, dtype=torch.uint8).cuda() if dtype == E4M3 else None
+        rows, rs = B.lasnet_dispatch_rows(x, position, offsets, scale=scale)
+        bits = lambda t: t.contiguous().view(torch.uint8)
+        assert torch.equal(bits(rows[:n]), bits(x[src])) and not bits(rows[n:]).any()
+        if dtype == E4M3:
+            assert torch.equal(rs[:n], scale[src]) and (rs[n:] == 127).all()
+            continue
+        w = torch.exp2(torch.randint(-3, 3, (tokens, k), generator=g).float()).cuda()
+        ref, size = f64(x), f64(x).abs()
+        for j in range(k):
+            part = torch.where((position[:, j] >= 0).cpu()[:, None], f64(x) * f64(w[:, j:j + 1]), 0.0)
+            ref, size = ref + part, size + part.abs()
+        close(B.lasnet_combine_rows(rows, position, weights=w, base=x), ref, HALF[dtype] * ref.abs() + (k + 2) * U * size + 1e-40, "sum")
