@@ -131,27 +131,29 @@ __device__ __forceinline__ void store_piece(unsigned char* p, int n, uint4_t v) 
     if (i < n) E::put(p + i * E::BYTES, v[i * E::BYTES / 4] >> (8 * (i * E::BYTES % 4)));
 }
 
+template <int L = 64>
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
-  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+  for (int d = L / 2; d; d >>= 1) v += __shfl_xor(v, d);
   return v;
 }
+template <int L = 64>
 __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
-  for (int d = 32; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
+  for (int d = L / 2; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
   return v;
 }
-// Sum (or maximum) over the W waves that share a row, the same bits in each.  at: W floats of LDS that nobody else writes before the next barrier but one.
-template <int W, bool MAX>
+// Sum (or maximum) over the L threads that share a row, the same bits in each.  at: L / 64 floats of LDS that nobody else writes before the next barrier but one.
+template <int L, bool MAX>
 __device__ __forceinline__ float row_join(float v, float* at) {
-  v = MAX ? wave_max(v) : wave_sum(v);
-  if constexpr (W == 1) return v;
-  const int wave = (int)(threadIdx.x >> 6) % W;
+  v = MAX ? wave_max<(L < 64 ? L : 64)>(v) : wave_sum<(L < 64 ? L : 64)>(v);
+  if constexpr (L <= 64) return v;
+  const int wave = (int)(threadIdx.x >> 6) % (L / 64);
   if ((threadIdx.x & 63) == 0) at[wave] = v;
   __syncthreads();
   float r = at[0];
 #pragma unroll
-  for (int i = 1; i < W; ++i) r = MAX ? fmaxf(r, at[i]) : r + at[i];
+  for (int i = 1; i < L / 64; ++i) r = MAX ? fmaxf(r, at[i]) : r + at[i];
   return r;
 }
 

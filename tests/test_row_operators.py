@@ -806,3 +806,13 @@ def test_few_tokens_with_wide_rows(tokens, k, cols):
             part = torch.where((position[:, j] >= 0).cpu()[:, None], f64(x) * f64(w[:, j:j + 1]), 0.0)
             ref, size = ref + part, size + part.abs()
         close(B.lasnet_combine_rows(rows, position, weights=w, base=x), ref, HALF[dtype] * ref.abs() + (k + 2) * U * size + 1e-40, "sum")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_norm_of_narrow_rows(dtype, monkeypatch):
+    """Rows that a part of a wave takes: as many as fit, the last of them alone or with room beside it, and the widths where the parts change."""
+    monkeypatch.setitem(globals(), "NORM_SHAPES", [(17, 128), (33, 129), (301, 200), (1030, 100), (77, 256), (64, 257), (5000, 65), (19, 64), (18, 16), (2049, 127)])
+    test_norm_rows(dtype, False)
+    test_norm_rows(dtype, True)
+    test_norm_rows_backward(dtype)
