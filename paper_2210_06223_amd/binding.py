@@ -195,6 +195,23 @@ def _as_tensor_desc(x: torch.Tensor) -> lasnet_tensor:
     return lasnet_tensor(x.data_ptr() or None, *shape, dt)
 
 
+def _empty(shape, dtype: torch.dtype, device, stream) -> torch.Tensor:
+    """What a call makes is memory of the stream that the call runs on: a block of the current stream's pool may have a last user there that has not finished,
+    and the call's kernels would not wait for it.  (A stream of another kind is known by its handle.)"""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream, device=device)):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _output(shape, dtype: torch.dtype, device, stream) -> torch.Tensor:
+    """... and an output will be used on the caller's current stream, too: freed, it is not given away before that has come so far."""
+    t = _empty(shape, dtype, device, stream)
+    if stream is not None:
+        t.record_stream(torch.cuda.current_stream(t.device))
+    return t
+
+
 def _check(status: int, where: str):
     if status != LASNET_OK:
         raise LasnetError(status, where)
@@ -490,7 +507,7 @@ def lasnet_microbench_copy(src: torch.Tensor, dst: torch.Tensor, stream=None) ->
 # ---- rows and experts ----
 # Rows are tensors of two dimensions whose rows are dense (their distance is free), or dense tensors of more, whose last dimension
 # is a row's: a feature map [N,H,W,C] is N*H*W rows.  8-bit rows are torch.float8_e4m3fn, their scales torch.float8_e8m0fnu (or uint8: the same
-# bytes).  A call without an output makes it.
+# bytes).  A call without an output makes it, as memory of its stream (`stream`, or the current one).
 
 _ROW_DTYPES = {torch.float32: LASNET_F32, torch.bfloat16: LASNET_BF16, torch.float8_e4m3fn: LASNET_E4M3}
 _SCALE_DTYPES = (torch.float8_e8m0fnu, torch.uint8)
@@ -534,11 +551,9 @@ def _dense(t: Optional[torch.Tensor], name: str, numel: int, *dtypes) -> Optiona
 
 
 def _workspace(t: Optional[torch.Tensor], need: int, device, stream):
-    """(address, bytes, tensor to keep until the call is enqueued).  What is made here belongs to the call's stream from then on."""
+    """(address, bytes, tensor to keep until the call is enqueued)."""
     if t is None and need:
-        t = torch.empty(need, dtype=torch.uint8, device=device)
-        if stream is not None:
-            t.record_stream(stream)
+        t = _empty(need, torch.uint8, device, stream)
     return (None, 0, None) if t is None else (t.data_ptr(), t.numel() * t.element_size(), t)
 
 
@@ -557,13 +572,13 @@ def lasnet_norm_rows(x: torch.Tensor, weight: torch.Tensor, eps: float, residual
             return out, scale, sum_out
     d = _rows(x, "x")
     if out is None:
-        out = torch.empty(x.shape, dtype=out_dtype or x.dtype, device=x.device)
+        out = _output(x.shape, out_dtype or x.dtype, x.device, stream)
     elif out_dtype is not None and out.dtype != out_dtype:
         raise ValueError("out has another type than out_dtype")
     if scale is None and out.dtype == torch.float8_e4m3fn:
-        scale = torch.empty(d.rows, dtype=torch.float8_e8m0fnu, device=x.device)
+        scale = _output(d.rows, torch.float8_e8m0fnu, x.device, stream)
     if sum_out is None and residual is not None:
-        sum_out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        sum_out = _output(x.shape, x.dtype, x.device, stream)
     r, s, o = _rows(residual, "residual"), _rows(sum_out, "sum_out"), _rows(out, "out")
     st = lib().lasnet_norm_rows(ctypes.byref(d), _ref(r), _dense(weight, "weight", d.cols, torch.float32), eps, _ref(s), ctypes.byref(o),
                                 _dense(scale, "scale", d.rows, *_SCALE_DTYPES), _dense(rstd, "rstd", d.rows, torch.float32), _stream(stream))
@@ -585,9 +600,9 @@ def lasnet_norm_rows_backward(dy: torch.Tensor, s: torch.Tensor, weight: torch.T
             return dx, dweight
     y, d, g = _rows(dy, "dy"), _rows(s, "s"), _rows(dsum, "dsum")
     if dx is None:
-        dx = torch.empty(s.shape, dtype=s.dtype, device=s.device)
+        dx = _output(s.shape, s.dtype, s.device, stream)
     if dweight is None:
-        dweight = torch.empty(d.cols, dtype=torch.float32, device=s.device)
+        dweight = _output(d.cols, torch.float32, s.device, stream)
     o, L = _rows(dx, "dx"), lib()
     at, size, keep = _workspace(workspace, L.lasnet_norm_rows_backward_workspace_bytes(d.rows, d.cols), s.device, stream)
     st = L.lasnet_norm_rows_backward(ctypes.byref(y), ctypes.byref(d), _dense(weight, "weight", d.cols, torch.float32),
@@ -611,11 +626,11 @@ def lasnet_route(experts: torch.Tensor, E: int, offsets: Optional[torch.Tensor] 
         raise ValueError("experts must be a contiguous int32 device tensor [tokens, k]")
     tokens, k = experts.shape
     if offsets is None:
-        offsets = torch.empty(E + 1, dtype=torch.int32, device=experts.device)
+        offsets = _output(E + 1, torch.int32, experts.device, stream)
     if order is None:
-        order = torch.empty(tokens * k, dtype=torch.int32, device=experts.device)
+        order = _output(tokens * k, torch.int32, experts.device, stream)
     if position is None:
-        position = torch.empty((tokens, k), dtype=torch.int32, device=experts.device)
+        position = _output((tokens, k), torch.int32, experts.device, stream)
     L = lib()
     at, size, keep = _workspace(workspace, L.lasnet_route_workspace_bytes(tokens, k, E), experts.device, stream)
     st = L.lasnet_route(_ptr(experts), tokens, k, E, _dense(offsets, "offsets", E + 1, torch.int32), _dense(order, "order", tokens * k, torch.int32),
@@ -650,9 +665,9 @@ def lasnet_dispatch_rows(x: torch.Tensor, position: torch.Tensor, offsets: torch
     if d.rows != tokens:
         raise ValueError("x and position must have as many tokens")
     if out is None:
-        out = torch.empty((tokens * k, d.cols), dtype=x.dtype, device=x.device)
+        out = _output((tokens * k, d.cols), x.dtype, x.device, stream)
     if out_scale is None and scale is not None:
-        out_scale = torch.empty(tokens * k, dtype=scale.dtype, device=x.device)
+        out_scale = _output(tokens * k, scale.dtype, x.device, stream)
     o = _rows(out, "out")
     st = lib().lasnet_dispatch_rows(ctypes.byref(d), _dense(scale, "scale", tokens, *_SCALE_DTYPES), _ptr(position), _ptr(offsets), k, E,
                                     ctypes.byref(o), _dense(out_scale, "out_scale", tokens * k, *_SCALE_DTYPES), _stream(stream))
@@ -672,7 +687,7 @@ def lasnet_combine_rows(y: torch.Tensor, position: torch.Tensor, weights: Option
     tokens, k = _slots(position)
     d, b = _rows(y, "y"), _rows(base, "base")
     if out is None:
-        out = torch.empty((tokens, d.cols) if base is None else base.shape, dtype=y.dtype, device=y.device)
+        out = _output((tokens, d.cols) if base is None else base.shape, y.dtype, y.device, stream)
     o = _rows(out, "out")
     if o.rows != tokens:
         raise ValueError("out and position must have as many tokens")
@@ -697,9 +712,9 @@ def lasnet_combine_rows_backward(dout: torch.Tensor, y: torch.Tensor, position: 
     if d.rows != tokens:
         raise ValueError("dout and position must have as many tokens")
     if dy is None:
-        dy = torch.empty(y.shape, dtype=y.dtype, device=y.device)
+        dy = _output(y.shape, y.dtype, y.device, stream)
     if dweights is None:
-        dweights = torch.empty((tokens, k), dtype=torch.float32, device=y.device)
+        dweights = _output((tokens, k), torch.float32, y.device, stream)
     o = _rows(dy, "dy")
     st = lib().lasnet_combine_rows_backward(ctypes.byref(d), ctypes.byref(v), _dense(weights, "weights", tokens * k, torch.float32), _ptr(position),
                                             _ptr(offsets), k, E, ctypes.byref(o), _dense(dweights, "dweights", tokens * k, torch.float32),
@@ -728,7 +743,7 @@ def lasnet_expert_product(x: torch.Tensor, offsets: torch.Tensor, W: torch.Tenso
         raise ValueError("the experts' matrices are [E, n, cols]")
     n = W.shape[1]
     if out is None:
-        out = torch.empty((d.rows, n), dtype=torch.bfloat16, device=x.device)
+        out = _output((d.rows, n), torch.bfloat16, x.device, stream)
     o = _rows(out, "out")
     if o.cols != n:
         raise ValueError("out must have %d columns" % n)
@@ -751,7 +766,7 @@ def lasnet_expert_product_dx(dy: torch.Tensor, offsets: torch.Tensor, W: torch.T
     if W.dim() != 3:
         raise ValueError("the experts' matrices are [E, n, cols]")
     if dx is None:
-        dx = torch.empty((d.rows, W.shape[2]), dtype=dy.dtype, device=dy.device)
+        dx = _output((d.rows, W.shape[2]), dy.dtype, dy.device, stream)
     o = _rows(dx, "dx")
     st = lib().lasnet_expert_product_dx(ctypes.byref(d), _ptr(offsets), E, _matrices(W, E, d.cols, o.cols, dy.dtype), ctypes.byref(o), _stream(stream))
     _check(st, "lasnet_expert_product_dx")
@@ -772,7 +787,7 @@ def lasnet_expert_product_dw(dy: torch.Tensor, x: torch.Tensor, offsets: torch.T
             return dW
     E, d, v = _offsets(offsets), _rows(dy, "dy"), _rows(x, "x")
     if dW is None:
-        dW = torch.empty((E, d.cols, v.cols), dtype=dtype or x.dtype, device=x.device)
+        dW = _output((E, d.cols, v.cols), dtype or x.dtype, x.device, stream)
     elif dtype is not None and dW.dtype != dtype:
         raise ValueError("dW has another type than dtype")
     at, size, keep = _workspace(workspace, L.lasnet_expert_product_dw_workspace_bytes(v.rows, E, d.cols, v.cols), x.device, stream)
