@@ -248,11 +248,11 @@ def lasnet_masker(x: torch.Tensor, Wm: torch.Tensor, bm: float, S: int, thr: flo
         _check(LASNET_ESHAPE if S > 0 else LASNET_EINVAL, "lasnet_masker")
     G, GW = H // S, W // S
     if mask is None:
-        mask = torch.empty((N, G, GW), dtype=torch.uint8, device=x.device)
+        mask = _output((N, G, GW), torch.uint8, x.device, stream)
     if idx is None:
-        idx = torch.empty((N * G * GW,), dtype=torch.int32, device=x.device)
+        idx = _output((N * G * GW,), torch.int32, x.device, stream)
     if count is None:
-        count = torch.empty((1,), dtype=torch.int32, device=x.device)
+        count = _output((1,), torch.int32, x.device, stream)
     st = lib().lasnet_masker(ctypes.byref(d), _ptr(_f32(Wm, "Wm")), float(bm), int(S), float(thr),
                              _ptr(mask), _ptr(idx), _ptr(count), _stream(stream))
     _check(st, "lasnet_masker")
@@ -276,11 +276,11 @@ def lasnet_masker_ex(x: torch.Tensor, Wm: torch.Tensor, bm: float, S: int, thr: 
         _check(LASNET_ESHAPE if S > 0 else LASNET_EINVAL, "lasnet_masker_ex")
     G, GW = H // S, W // S
     if mask is None:
-        mask = torch.empty((N, G, GW), dtype=torch.uint8, device=x.device)
+        mask = _output((N, G, GW), torch.uint8, x.device, stream)
     if idx is None:
-        idx = torch.empty((N * G * GW,), dtype=torch.int32, device=x.device)
+        idx = _output((N * G * GW,), torch.int32, x.device, stream)
     if count is None:
-        count = torch.empty((1,), dtype=torch.int32, device=x.device)
+        count = _output((1,), torch.int32, x.device, stream)
     po = None
     if pass_out is not None:
         po = _as_tensor_desc(pass_out)
@@ -298,7 +298,7 @@ def lasnet_masker_logits(x: torch.Tensor, Wm: torch.Tensor, bm: float, S: int,
     if S <= 0 or H % S or W % S:
         _check(LASNET_ESHAPE if S > 0 else LASNET_EINVAL, "lasnet_masker_logits")
     if logits is None:
-        logits = torch.empty((N, H // S, W // S), dtype=torch.float64, device=x.device)
+        logits = _output((N, H // S, W // S), torch.float64, x.device, stream)
     st = lib().lasnet_masker_logits(ctypes.byref(d), _ptr(_f32(Wm, "Wm")), float(bm), int(S),
                                     _ptr(logits), _stream(stream))
     _check(st, "lasnet_masker_logits")
@@ -344,7 +344,7 @@ def lasnet_sparse_bottleneck(x: torch.Tensor, idx: Optional[torch.Tensor],
             return out
     d = _as_tensor_desc(x)
     if out is None:
-        out = torch.empty_like(x)
+        out = _output(x.shape, x.dtype, x.device, stream)
     o = _as_tensor_desc(out)
     M, w = _weights(x, W1, b1, W2, b2, W3, b3)
     _check_list(d, idx, count, int(S))
@@ -418,7 +418,7 @@ def lasnet_dense_bottleneck(x: torch.Tensor, W1, b1, W2, b2, W3, b3,
             return out
     d = _as_tensor_desc(x)
     if out is None:
-        out = torch.empty_like(x)
+        out = _output(x.shape, x.dtype, x.device, stream)
     o = _as_tensor_desc(out)
     M, w = _weights(x, W1, b1, W2, b2, W3, b3)
     st = lib().lasnet_dense_bottleneck(ctypes.byref(d), M, *w, ctypes.byref(o), int(flags),
@@ -440,7 +440,7 @@ def lasnet_pack_weights(S: int, W1: torch.Tensor, W2: torch.Tensor, W3: torch.Te
     if nbytes == 0:
         _check(LASNET_EUNSUPPORTED, "lasnet_pack_weights")
     if packed is None:
-        packed = torch.empty((nbytes // 2,), dtype=torch.bfloat16, device=W1.device)
+        packed = _output((nbytes // 2,), torch.bfloat16, W1.device, stream)
     elif packed.numel() * packed.element_size() < nbytes or not packed.is_cuda:
         raise ValueError("packed buffer too small")
     st = lib().lasnet_pack_weights(LASNET_BF16, int(C), int(M), int(S), _ptr(W1), _ptr(W2), _ptr(W3),
@@ -462,7 +462,7 @@ def lasnet_sparse_bottleneck_packed(x: torch.Tensor, idx: Optional[torch.Tensor]
             return out
     d = _as_tensor_desc(x)
     if out is None:
-        out = torch.empty_like(x)
+        out = _output(x.shape, x.dtype, x.device, stream)
     o = _as_tensor_desc(out)
     _check_list(d, idx, count, int(S))
     need = lib().lasnet_packed_weights_bytes(LASNET_BF16, int(x.shape[3]), int(M), int(S))

@@ -42,6 +42,18 @@ def row_calls(k):
     yield "expert_product_dw", lambda: B.lasnet_expert_product_dw(q, q, off, **k), 1, 1
 
 
+def map_calls(k):
+    x, f, idx, M, C = dev(1, 4, 4, 64, dtype=BF16), dev(64), dev(4, dtype=I32), 16, 64
+    W = (dev(M, C, dtype=BF16), dev(M), dev(M, 3, 3, M, dtype=BF16), dev(M), dev(C, M, dtype=BF16), f)
+    yield "masker", lambda: B.lasnet_masker(x, f, 0.0, 2, **k), 3
+    yield "masker_ex", lambda: B.lasnet_masker_ex(x, f, 0.0, 2, pass_out=x, **k), 3
+    yield "masker_logits", lambda: B.lasnet_masker_logits(x, f, 0.0, 2, **k), 1
+    yield "block", lambda: B.lasnet_sparse_bottleneck(x, idx, idx[:1], 2, *W, **k), 1
+    yield "dense", lambda: B.lasnet_dense_bottleneck(x, *W, **k), 1
+    yield "pack", lambda: B.lasnet_pack_weights(2, W[0], W[2], W[4], **k), 1
+    yield "packed", lambda: B.lasnet_sparse_bottleneck_packed(x, idx, idx[:1], 2, M, dev(128), dev(M), dev(M), f, **k), 1
+
+
 @pytest.fixture
 def made(monkeypatch):
     """What is made: (tensor, the stream it is made under)."""
@@ -81,6 +93,45 @@ def test_rows_what_a_call_makes_is_memory_of_its_stream(which, made):
         assert [s for _, s in made] == [given or "current"] * (outputs + workspaces), name
         used = [getattr(t, "used_on", []) for t, _ in made]
         assert used == [["current"] if given else []] * outputs + [[]] * workspaces, name
+
+
+@pytest.mark.parametrize("which", range(7))
+def test_maps_what_a_call_makes_is_memory_of_its_stream(which, made):
+    side = _Stream()
+    for given in (None, side):
+        name, call, outputs = list(map_calls({} if given is None else {"stream": given}))[which]
+        made.clear()
+        call()
+        assert [s for _, s in made] == [given or "current"] * outputs, name
+        assert [getattr(t, "used_on", []) for t, _ in made] == [["current"] if given else []] * outputs, name
+
+
+@pytest.mark.gpu
+def test_maps_on_another_stream_while_the_current_one_is_busy():
+    """As below, for a masker, its list and a block (its memory beyond the arguments is the library's, one buffer for each stream)."""
+    g = torch.Generator().manual_seed(2)
+    x, Wm = torch.randn(2, 14, 14, 64, generator=g).to(BF16).cuda(), torch.randn(64, generator=g).cuda()
+    W = [torch.randn(*s, generator=g).mul_(0.05).to(BF16 if len(s) > 1 else torch.float32).cuda() for s in ((16, 64), (16,), (16, 3, 3, 16), (16,), (64, 16), (64,))]
+
+    def path(**s):
+        mask, idx, count = B.lasnet_masker(x, Wm, 0.0, 2, **s)
+        return mask, count, B.lasnet_sparse_bottleneck(x, idx, count, 2, *W, **s)
+
+    want = path()
+    side, a, b = torch.cuda.Stream(), torch.randn(4096, 4096, device="cuda"), torch.empty(4096, 4096, device="cuda")
+    torch.cuda.synchronize()
+    for i in range(5):
+        print("busy", i, flush=True)
+        side.wait_stream(torch.cuda.current_stream())
+        torch.mm(a, a, out=b)
+        blocks = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in (98, 392, 4, x.numel() * 2) for _ in range(2)]
+        for t in blocks:
+            t.fill_(255)
+        del blocks, t
+        got = path(stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+        for x1, x2 in zip(got, want):
+            assert torch.equal(x1, x2), i
 
 
 @pytest.mark.gpu
