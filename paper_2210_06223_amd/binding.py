@@ -554,6 +554,8 @@ def _workspace(t: Optional[torch.Tensor], need: int, device, stream):
     """(address, bytes, tensor to keep until the call is enqueued)."""
     if t is None and need:
         t = _empty(need, torch.uint8, device, stream)
+    elif t is not None and (not t.is_cuda or t.device != device or not t.is_contiguous()):
+        raise ValueError("workspace must be a contiguous device tensor, where the rows are")
     return (None, 0, None) if t is None else (t.data_ptr(), t.numel() * t.element_size(), t)
 
 

@@ -129,6 +129,15 @@ struct Plain {                                       // false from any of these:
     const int64_t shape[3] = {E, n, k};
     return need(t && t->defined() && t->scalar_type() == ty && t->is_cuda() && t->is_contiguous() && t->sizes() == at::IntArrayRef(shape, 3)) ? t->data_ptr() : nullptr;
   }
+  // None, or a dense tensor of any type on the device of another argument
+  void* workspace(PyObject* o, PyObject* beside, size_t& bytes) {
+    bytes = 0;
+    if (o == Py_None || !ok) return nullptr;
+    const at::Tensor* t = tensor(o);
+    if (!need(t && t->defined() && t->is_cuda() && t->device() == tensor(beside)->device() && t->is_contiguous())) return nullptr;
+    bytes = t->nbytes();
+    return t->data_ptr();
+  }
   // the list: storage for every cell of the map (the kernels may read entries past the count)
   void list(PyObject* idx, PyObject* count, const lasnet_tensor& x, int S, const int32_t*& i, const int32_t*& c) {
     i = c = nullptr;
@@ -317,9 +326,9 @@ PyObject* norm_rows_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const lasnet_rows* dsum = p.rows_or_none(a[5], sum);
     p.rows(a[6], dx);
     float* dweight = p.dense<float>(a[7], at::kFloat, s.cols);
-    void* workspace = a[8] == Py_None ? nullptr : p.any<void>(a[8]);
+    size_t bytes;
+    void* workspace = p.workspace(a[8], a[2], bytes);
     if (!p.ok) return 0;
-    const size_t bytes = a[8] == Py_None ? 0 : tensor(a[8])->nbytes();
     auto* f = entry<decltype(lasnet_norm_rows_backward)>(a[0]);
     ENQUEUE(f(&dy, &s, weight, rstd, dsum, &dx, dweight, workspace, bytes, st));
   });
@@ -336,9 +345,9 @@ PyObject* route(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int32_t* offsets = p.dense<int32_t>(a[3], at::kInt, (int64_t)E + 1);
     int32_t* order = p.dense<int32_t>(a[4], at::kInt, tokens * k);
     int32_t* position = p.dense<int32_t>(a[5], at::kInt, tokens * k);
-    void* workspace = a[6] == Py_None ? nullptr : p.any<void>(a[6]);
+    size_t bytes;
+    void* workspace = p.workspace(a[6], a[1], bytes);
     if (!p.ok) return 0;
-    const size_t bytes = a[6] == Py_None ? 0 : tensor(a[6])->nbytes();
     auto* f = entry<decltype(lasnet_route)>(a[0]);
     ENQUEUE(f(experts, tokens, k, E, offsets, order, position, workspace, bytes, st));
   });
@@ -453,9 +462,9 @@ PyObject* expert_product_dw(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const auto ty = dW->scalar_type();
     p.need(ty == at::kFloat || ty == at::kBFloat16);
     void* to = p.matrices(a[4], E, dy.cols, x.cols, ty);
-    void* workspace = a[5] == Py_None ? nullptr : p.any<void>(a[5]);
+    size_t bytes;
+    void* workspace = p.workspace(a[5], a[2], bytes);
     if (!p.ok) return 0;
-    const size_t bytes = a[5] == Py_None ? 0 : tensor(a[5])->nbytes();
     auto* f = entry<decltype(lasnet_expert_product_dw_ex)>(a[0]);
     ENQUEUE(f(&dy, &x, offsets, E, to, ty == at::kFloat ? LASNET_F32 : LASNET_BF16, workspace, bytes, st));
   });
