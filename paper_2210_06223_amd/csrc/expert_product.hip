@@ -117,6 +117,28 @@ struct Tile {
   }
 };
 
+// Scales of e4m3 products.  sum * wscale * 2^(b - 127), without the product of the two scales, which may leave fp32's range where the result does not (2^127 times 4, or
+// 2^-126 times 10^-6): the sum (2^-18 to 2^38 in size, or 0) times wscale's mantissa, from 1/2 to 1, then its exponent and the row's by v_ldexp, which rounds below the
+// normal numbers alone.  A row's byte of 255 is NaN: it comes as the addend of the multiplication, -0 for any other row (which changes nothing, not even the sign of 0).
+struct ColScale {
+  float mantissa;
+  int exponent;
+};
+__device__ __forceinline__ ColScale col_scale(float w) { return ColScale{__builtin_amdgcn_frexp_mantf(w), __builtin_amdgcn_frexp_expf(w)}; }
+struct RowScale {
+  int exponent;
+  float addend;
+};
+__device__ __forceinline__ RowScale row_scale(unsigned byte) { return RowScale{(int)byte - 127, byte == 255 ? __uint_as_float(0x7fc00000u) : -0.f}; }
+__device__ __forceinline__ float scaled(float sum, ColScale w, RowScale r) {
+  return __builtin_amdgcn_ldexpf(__builtin_fmaf(sum, w.mantissa, r.addend), w.exponent + r.exponent);
+}
+// Two multiplications in this order give the same bits where sum * wscale is a normal number (or 0, infinite, NaN) whatever the sum: the streaming kernel's tiles take
+// them where all of a wave's columns allow it (32768 rows, 4096 x 2048: 298 us; v_ldexp for every element 351; the other kernels take the same time either way).
+__device__ __forceinline__ bool plain_scale(float w) {
+  const int e = __builtin_amdgcn_frexp_expf(w);               // (0 of 0, infinities and NaN)
+  return e >= -107 && e <= 89;
+}
 // 2^(b - 127); 255: NaN
 __device__ __forceinline__ float scale_value(unsigned b) {
   return __uint_as_float(b == 255 ? 0x7fc00000u : b ? b << 23 : 0x00400000u);
@@ -155,13 +177,13 @@ __device__ __forceinline__ void store_tile(const ProductArgs& a, unsigned char* 
   constexpr int OB = F32OUT ? 4 : 2;
   const int lane = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));      // (made anew: no register holds it through the loop)
   const float floor = a.relu ? 0.f : -INFINITY;               // (NaN passes)
-  float up[NJ];
+  RowScale up[NJ];
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
-    up[j] = 1.0f;
+    up[j] = row_scale(127);
     if constexpr (FP8) {
       const int oj = oj0 + 16 * j + (lane & 15);
-      if (a.scale && expert < a.E && oj < j_end) up[j] = scale_value(a.scale[oj]);
+      if (a.scale && expert < a.E && oj < j_end) up[j] = row_scale(a.scale[oj]);
     }
   }
   if (oj0 >= j_end || oi0 >= a.ni) return;
@@ -176,13 +198,17 @@ __device__ __forceinline__ void store_tile(const ProductArgs& a, unsigned char* 
       float w[4] = {1.0f, 1.0f, 1.0f, 1.0f};
       if constexpr (FP8)
         if (a.wscale && expert < a.E) Elem<float>::widen(load_piece<float>((const unsigned char*)(a.wscale + (size_t)expert * a.ni + oi), a.ni - oi), w);
+      ColScale ws[4];
+      if constexpr (FP8)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) ws[r] = col_scale(w[r]);
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
         float v[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           v[r] = acc[i][j][r];
-          if constexpr (FP8) v[r] *= w[r] * up[j];
+          if constexpr (FP8) v[r] = scaled(v[r], ws[r], up[j]);
           v[r] = v[r] < floor ? floor : v[r];
         }
         store(i, j, oi, v);
@@ -719,22 +745,22 @@ __device__ __forceinline__ void store_big_tile(const ProductArgs& a, unsigned ch
   const unsigned long long first = (unsigned long long)(out + (long long)t.j0 * a.out.pitch + (long long)t.i0 * OB);
   const intx4 to = {(int)(unsigned)first, (int)(unsigned)(first >> 32), (int)((unsigned)(rows - 1) * pitch + (unsigned)(a.ni - t.i0) * OB), 0x00020000};
   // the scales of the wave's 64 rows and 128 columns, one and two a lane, all asked for before the first store
-  float row_scale = 1.f, col_scale[2] = {1.f, 1.f};
+  unsigned byte = 127;
+  float col[2] = {1.f, 1.f};
   if constexpr (FP8) {
-    unsigned byte = 127;
     if (a.scale) byte = __builtin_amdgcn_raw_buffer_load_b8(product_rsrc(a.scale + t.j0, (unsigned)rows), wj + lane, 0, 0);
     if (a.wscale) {
       const product_rsrc_t ws = product_rsrc(a.wscale + (size_t)t.expert * a.ni, (unsigned)a.ni * 4);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) col_scale[h] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(ws, (t.i0 + wi + 64 * h + lane) * 4, 0, 0));
+      for (int h = 0; h < 2; ++h) col[h] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(ws, (t.i0 + wi + 64 * h + lane) * 4, 0, 0));
     }
-    row_scale = scale_value(byte);
   }
+  const float row = FP8 ? scale_value(byte) : 1.f;
   float up[4] = {1.f, 1.f, 1.f, 1.f};
   if constexpr (FP8)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) up[j] = __shfl(row_scale, 16 * j + (lane & 15));
-  auto each = [&](auto relu) {
+    for (int j = 0; j < 4; ++j) up[j] = __shfl(row, 16 * j + (lane & 15));
+  auto each = [&](auto relu, auto plain) {
     const intx4 buffer = to;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -742,7 +768,7 @@ __device__ __forceinline__ void store_big_tile(const ProductArgs& a, unsigned ch
       float w[4] = {1.f, 1.f, 1.f, 1.f};
       if constexpr (FP8)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) w[r] = __shfl(col_scale[i / 4], 16 * (i % 4) + (lane >> 4) * 4 + r);
+        for (int r = 0; r < 4; ++r) w[r] = __shfl(col[i / 4], 16 * (i % 4) + (lane >> 4) * 4 + r);
       // (ni is a multiple of 4: a lane's four are stored or, beyond the buffer's 2^31 bytes, not)
       unsigned o = t.i0 + oi < a.ni ? (unsigned)(wj + (lane & 15)) * pitch + (unsigned)oi * OB : 0x80000000u;
 #pragma unroll
@@ -751,7 +777,8 @@ __device__ __forceinline__ void store_big_tile(const ProductArgs& a, unsigned ch
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           v[r] = acc[i][j][r];
-          if constexpr (FP8) v[r] *= w[r] * up[j];
+          if constexpr (FP8 && decltype(plain)::value) v[r] = v[r] * w[r] * up[j];
+          if constexpr (!decltype(plain)::value) v[r] = scaled(v[r], col_scale(w[r]), row_scale((unsigned)__shfl((int)byte, 16 * j + (lane & 15))));
           if constexpr (decltype(relu)::value) v[r] = v[r] < 0.f ? 0.f : v[r];              // (NaN passes)
         }
         // (s_nop: the registers of a store of more than 8 bytes may not be written by the very next instruction)
@@ -762,10 +789,15 @@ __device__ __forceinline__ void store_big_tile(const ProductArgs& a, unsigned ch
       }
     }
   };
-  if (a.relu)
-    each(std::true_type{});
-  else
-    each(std::false_type{});
+  auto store = [&](auto plain) {
+    if (a.relu)
+      each(std::true_type{}, plain);
+    else
+      each(std::false_type{}, plain);
+  };
+  if constexpr (FP8)
+    if (!__all(plain_scale(col[0]) && plain_scale(col[1]))) return store(std::false_type{});
+  store(std::true_type{});
 }
 
 template <bool FP8, bool IC, bool JC, bool RAGGED, bool F32OUT>
