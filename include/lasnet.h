@@ -303,8 +303,8 @@ LASNET_API int lasnet_has_fast_path(int dtype, int C, int M, int S);
  * faster in the products.  rows may be 0 (data then may be NULL, and nothing is enqueued but what the other outputs
  * need).  Limits: rows (and tokens * k) up to 2^30, cols up to 2^20 (norms: 16384), E up to 4096, k up to 64; beyond them
  * LASNET_EUNSUPPORTED.
- * An output must not overlap an input or another output, unless its description says so (the same address: LASNET_EALIAS; the
- * rest is not checked).
+ * An output (or workspace) must not overlap an input or another output, unless its description says so (the same address: LASNET_EALIAS;
+ * the rest is not checked).
  * The entry points allocate nothing; what needs device memory beyond its arguments takes a workspace from the caller
  * (256-byte aligned, LASNET_EINVAL if too small), owned by the call until its work on the stream has finished.  They can be
  * stream-captured.  Results do not depend on what else runs: no sum is made by atomics.

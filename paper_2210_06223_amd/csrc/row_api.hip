@@ -1,4 +1,6 @@
 // extern "C" boundary of the row operators: argument validation and launches only.
+#include <initializer_list>
+
 #include "row_ops.hpp"
 
 using namespace lasnet;
@@ -43,6 +45,18 @@ bool same(const lasnet_rows* a, const lasnet_rows* b) { return a && b && a->data
 bool may_share(const lasnet_rows* a, const lasnet_rows* b) {
   return !same(a, b) || (arg(a).pitch == arg(b).pitch && a->dtype == b->dtype);
 }
+const void* at(const lasnet_rows* t) { return t ? t->data : nullptr; }
+// whether an output lies where another one or an input does (pairs that may be the same rows are left out of the call)
+bool clash(std::initializer_list<const void*> outputs, std::initializer_list<const void*> inputs) {
+  for (const void* const* o = outputs.begin(); o != outputs.end(); ++o) {
+    if (!*o) continue;
+    for (const void* const* p = o + 1; p != outputs.end(); ++p)
+      if (*p == *o) return true;
+    for (const void* i : inputs)
+      if (i == *o) return true;
+  }
+  return false;
+}
 int enqueued(hipError_t e) { return e == hipSuccess ? LASNET_OK : LASNET_EHIP; }
 
 #define CHECK(call)                      \
@@ -73,7 +87,8 @@ int lasnet_norm_rows(const lasnet_rows* x, const lasnet_rows* residual, const fl
   if (!weight || !(eps >= 0.f)) return LASNET_EINVAL;
   if (x->rows > 0 && q != (scale != nullptr)) return LASNET_EINVAL;
   if (x->cols > kNormCols) return LASNET_EUNSUPPORTED;
-  if (same(out, sum_out) || !may_share(out, x) || !may_share(out, residual) || !may_share(sum_out, x) || !may_share(sum_out, residual))
+  if (!may_share(out, x) || !may_share(out, residual) || !may_share(sum_out, x) || !may_share(sum_out, residual) ||
+      clash({at(out), at(sum_out), scale, rstd_out}, {weight}) || clash({scale, rstd_out}, {at(x), at(residual)}))
     return LASNET_EALIAS;
   if (!device_ok()) return LASNET_EHIP;
   if (x->rows == 0) return LASNET_OK;
@@ -94,9 +109,11 @@ int lasnet_norm_rows_backward(const lasnet_rows* dy, const lasnet_rows* s, const
   CHECK(check_like(dx, s));
   if (!weight || !dweight || (s->rows > 0 && !rstd)) return LASNET_EINVAL;
   if (s->cols > kNormCols) return LASNET_EUNSUPPORTED;
-  if (same(dx, s) || !may_share(dx, dy) || !may_share(dx, dsum)) return LASNET_EALIAS;
   const size_t need = lasnet_norm_rows_backward_workspace_bytes(s->rows, s->cols);
   if (need && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255))) return LASNET_EINVAL;
+  if (!may_share(dx, dy) || !may_share(dx, dsum) || clash({at(dx), dweight, workspace}, {at(s), weight, rstd}) ||
+      clash({dweight, workspace}, {at(dy), at(dsum)}))
+    return LASNET_EALIAS;
   if (!device_ok()) return LASNET_EHIP;
   return enqueued(launch_norm_rows_backward(s->dtype, s->rows, s->cols, arg(dy), arg(s), weight, rstd, arg(dsum), arg(dx), dweight, workspace,
                                             (hipStream_t)hip_stream));
@@ -113,9 +130,9 @@ int lasnet_route(const int32_t* experts, int64_t tokens, int k, int E, int32_t* 
   CHECK(check_experts(k, E));
   if (tokens > kMaxRows || tokens * k > kMaxRows) return LASNET_EUNSUPPORTED;
   if (!offsets || (tokens > 0 && (!experts || !position))) return LASNET_EINVAL;
-  if (tokens > 0 && (experts == position || experts == order || position == order)) return LASNET_EALIAS;
   const size_t need = lasnet_route_workspace_bytes(tokens, k, E);
   if (need && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255))) return LASNET_EINVAL;
+  if (tokens > 0 && clash({offsets, order, position, workspace}, {experts})) return LASNET_EALIAS;
   if (!device_ok()) return LASNET_EHIP;
   return enqueued(launch_route(experts, tokens * k, E, offsets, order, position, workspace, (hipStream_t)hip_stream));
 }
@@ -127,7 +144,7 @@ int lasnet_dispatch_rows(const lasnet_rows* x, const uint8_t* scale, const int32
   CHECK(check_experts(k, E));
   if (out->dtype != x->dtype || out->cols != x->cols || out->rows != x->rows * k) return LASNET_ESHAPE;
   if (x->rows > 0 && (!position || !offsets || (scale != nullptr) != (out_scale != nullptr))) return LASNET_EINVAL;
-  if (same(out, x) || (scale && scale == out_scale)) return LASNET_EALIAS;
+  if (clash({at(out), out_scale}, {at(x), scale, position, offsets})) return LASNET_EALIAS;
   if (!device_ok()) return LASNET_EHIP;
   if (x->rows == 0) return LASNET_OK;
   return enqueued(launch_dispatch(x->rows, k, E, x->cols * bytes_of(x->dtype), arg(x), scale, position, offsets, arg(out), out_scale,
@@ -142,7 +159,7 @@ int lasnet_combine_rows(const lasnet_rows* y, const float* weights, const int32_
   if (base) CHECK(check_like(base, out));
   if (out->dtype != y->dtype || out->cols != y->cols || y->rows != out->rows * k) return LASNET_ESHAPE;
   if (out->rows > 0 && !position) return LASNET_EINVAL;
-  if (same(out, y) || !may_share(out, base)) return LASNET_EALIAS;
+  if (!may_share(out, base) || clash({at(out)}, {at(y), weights, position})) return LASNET_EALIAS;
   if (!device_ok()) return LASNET_EHIP;
   if (out->rows == 0) return LASNET_OK;
   return enqueued(launch_combine(y->dtype, out->rows, k, y->cols, arg(y), weights, position, arg(base), arg(out), (hipStream_t)hip_stream));
@@ -156,7 +173,7 @@ int lasnet_combine_rows_backward(const lasnet_rows* dout, const lasnet_rows* y, 
   CHECK(check_like(dy, y));
   if (dout->dtype != y->dtype || dout->cols != y->cols || y->rows != dout->rows * k) return LASNET_ESHAPE;
   if (dout->rows > 0 && (!position || !offsets)) return LASNET_EINVAL;
-  if (same(dy, dout) || !may_share(dy, y) || (weights && weights == dweights)) return LASNET_EALIAS;
+  if (!may_share(dy, y) || clash({at(dy), dweights}, {at(dout), weights, position, offsets}) || clash({dweights}, {at(y)})) return LASNET_EALIAS;
   if (!device_ok()) return LASNET_EHIP;
   if (dout->rows == 0) return LASNET_OK;
   return enqueued(launch_combine_backward(y->dtype, dout->rows, k, E, y->cols, arg(dout), arg(y), weights, position, offsets, arg(dy), dweights,
@@ -172,7 +189,7 @@ int lasnet_expert_product(const lasnet_rows* x, const uint8_t* scale, const int3
   if (!offsets || !W || (flags & ~(uint32_t)LASNET_POST_RELU)) return LASNET_EINVAL;
   if (x->dtype != LASNET_E4M3 && (scale || wscale)) return LASNET_EINVAL;
   CHECK(check_tiles(x->rows, E, out->cols, 0));
-  if (same(out, x) || out->data == W) return LASNET_EALIAS;
+  if (clash({at(out)}, {at(x), scale, offsets, W, wscale})) return LASNET_EALIAS;
   if (!device_ok()) return LASNET_EHIP;
   if (x->rows == 0) return LASNET_OK;
   return enqueued(launch_expert_product(x->dtype, x->rows, E, out->cols, x->cols, arg(x), scale, offsets, W, wscale, arg(out),
@@ -186,7 +203,7 @@ int lasnet_expert_product_dx(const lasnet_rows* dy, const int32_t* offsets, int 
   if (dx->rows != dy->rows) return LASNET_ESHAPE;
   if (!offsets || !W) return LASNET_EINVAL;
   CHECK(check_tiles(dy->rows, E, dx->cols, 0));
-  if (same(dx, dy) || dx->data == W) return LASNET_EALIAS;
+  if (clash({at(dx)}, {at(dy), offsets, W})) return LASNET_EALIAS;
   if (!device_ok()) return LASNET_EHIP;
   if (dy->rows == 0) return LASNET_OK;
   return enqueued(launch_expert_product_dx(dy->rows, E, dy->cols, dx->cols, arg(dy), offsets, W, arg(dx), (hipStream_t)hip_stream));
@@ -206,7 +223,7 @@ int lasnet_expert_product_dw_ex(const lasnet_rows* dy, const lasnet_rows* x, con
   if (!offsets || !dW || (dw_dtype != LASNET_F32 && dw_dtype != LASNET_BF16)) return LASNET_EINVAL;
   CHECK(check_tiles(x->rows, E, x->cols, dy->cols));
   if (workspace && (workspace_bytes < lasnet_expert_product_dw_workspace_bytes(x->rows, E, dy->cols, x->cols) || ((uintptr_t)workspace & 255))) return LASNET_EINVAL;
-  if (dW == x->data || dW == dy->data) return LASNET_EALIAS;
+  if (clash({dW, workspace}, {at(x), at(dy), offsets})) return LASNET_EALIAS;
   if (!device_ok()) return LASNET_EHIP;
   return enqueued(launch_expert_product_dw(x->rows, E, dy->cols, x->cols, arg(dy), arg(x), offsets, dW, dw_dtype == LASNET_F32, workspace,
                                            (hipStream_t)hip_stream));

@@ -1,4 +1,6 @@
-"""Arguments of the calls on rows that are refused before anything is enqueued: workspaces in the wrong memory."""
+"""Arguments of the calls on rows that are refused before anything is enqueued: workspaces in the wrong memory, outputs at the address of another argument."""
+import ctypes
+
 import pytest
 import torch
 
@@ -59,3 +61,67 @@ def test_a_host_workspace_is_refused_natively_too():
     torch.cuda.synchronize()
     L, x = B.lib(), make(6, 8, dtype=BF16)
     assert B._marshal.norm_rows_backward(L.at_norm_rows_backward, x, x, make(8), make(6), None, make(6, 8, dtype=BF16), make(8), torch.zeros(1 << 20, dtype=torch.uint8)) is None
+
+
+# Entries: their arguments in order, (name, kind) of an address ("i": input, "o": output; "ri", "ro": rows, with their numbers of rows and columns and type) or a plain value; and the
+# pairs that may be the same rows.
+F, H = B.LASNET_F32, B.LASNET_BF16
+ENTRIES = {
+    "norm_rows": ([("x", "ri", 8, 16, H), ("residual", "ri", 8, 16, H), ("weight", "i"), 1e-6, ("sum_out", "ro", 8, 16, H), ("out", "ro", 8, 16, B.LASNET_E4M3), ("scale", "o"),
+                   ("rstd", "o"), None], {("sum_out", "x"), ("sum_out", "residual")}),
+    "norm_rows_backward": ([("dy", "ri", 8, 16, H), ("s", "ri", 8, 16, H), ("weight", "i"), ("rstd", "i"), ("dsum", "ri", 8, 16, H), ("dx", "ro", 8, 16, H), ("dweight", "o"),
+                            ("workspace", "o"), 1 << 20, None], {("dx", "dy"), ("dx", "dsum")}),
+    "route": ([("experts", "i"), 100000, 2, 4, ("offsets", "o"), ("order", "o"), ("position", "o"), ("workspace", "o"), 1 << 24, None], set()),
+    "dispatch_rows": ([("x", "ri", 8, 16, B.LASNET_E4M3), ("scale", "i"), ("position", "i"), ("offsets", "i"), 2, 4, ("out", "ro", 16, 16, B.LASNET_E4M3), ("out_scale", "o"), None],
+                      set()),
+    "combine_rows": ([("y", "ri", 16, 16, F), ("weights", "i"), ("position", "i"), 2, ("base", "ri", 8, 16, F), ("out", "ro", 8, 16, F), None], {("out", "base")}),
+    "combine_rows_backward": ([("dout", "ri", 8, 16, F), ("y", "ri", 16, 16, F), ("weights", "i"), ("position", "i"), ("offsets", "i"), 2, 4, ("dy", "ro", 16, 16, F),
+                               ("dweights", "o"), None], {("dy", "y")}),
+    "expert_product": ([("x", "ri", 8, 16, B.LASNET_E4M3), ("scale", "i"), ("offsets", "i"), 2, ("W", "i"), ("wscale", "i"), ("out", "ro", 8, 16, H), 0, None], set()),
+    "expert_product_dx": ([("dy", "ri", 8, 16, H), ("offsets", "i"), 2, ("W", "i"), ("dx", "ro", 8, 16, H), None], set()),
+    "expert_product_dw_ex": ([("dy", "ri", 8, 16, H), ("x", "ri", 8, 16, H), ("offsets", "i"), 2, ("dW", "o"), F, ("workspace", "o"), 1 << 20, None], set()),
+}
+
+_PROBE = r"""
+class Rows(ctypes.Structure):
+    _fields_ = [("data", vp), ("rows", ctypes.c_int64), ("stride", ctypes.c_int64), ("cols", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+def enter(name, args, same=None):
+    # the entry's status; same: two names, the first of which gets the second's address
+    at = {a[0]: (i + 1) << 32 for i, a in enumerate(args) if isinstance(a, list)}
+    if same:
+        at[same[0]] = at[same[1]]
+    passed = []
+    for a in args:
+        if not isinstance(a, list):
+            passed.append(ctypes.c_float(a) if isinstance(a, float) else vp(None) if a is None else ctypes.c_longlong(a))
+        elif a[1][0] == "r":
+            passed.append(ctypes.byref(Rows(at[a[0]], a[2], 0, a[3], a[4])))
+        else:
+            passed.append(vp(at[a[0]]))
+    F.fake_set(-1, 0, 0)
+    st = getattr(L, "lasnet_" + name)(*passed)
+    return st, sum(l.startswith("launch") for l in F.fake_log().decode().splitlines())
+result = {}
+for name, (args, pairs) in ENTRIES.items():
+    result[name] = {"apart": enter(name, args), "pairs": [[p, enter(name, args, p)] for p in pairs]}
+"""
+
+
+def test_an_output_at_the_address_of_another_argument_is_refused():
+    """Of every output with every input and every other output, as the header says; pairs that may be the same rows, and arguments all apart, are enqueued.  (On the
+    recording runtime: nothing runs.)"""
+    from tests import _fake_hip
+    table = {}
+    for name, (args, allowed) in ENTRIES.items():
+        named = [a for a in args if isinstance(a, tuple)]
+        outs = [a[0] for a in named if a[1].endswith("o")]
+        table[name] = ([list(a) if isinstance(a, tuple) else a for a in args], [[o, a[0]] for o in outs for a in named if a[0] != o])
+    got = _fake_hip.run("ENTRIES = %r\n" % table + _PROBE)
+    for name, (args, allowed) in ENTRIES.items():
+        st, launches = got[name]["apart"]
+        assert st == B.LASNET_OK and launches > 0, name
+        for (o, other), (st, launches) in got[name]["pairs"]:
+            if (o, other) in allowed or (other, o) in allowed:
+                assert st == B.LASNET_OK and launches > 0, (name, o, other)
+            else:
+                assert st == B.LASNET_EALIAS and launches == 0, (name, o, other, st)
