@@ -9,7 +9,7 @@
 // is: W for dx, both for dW).  In LDS a tile by rows lies as it is read, 128 bytes of k a row; one by columns lies as it is in memory, and
 // the transposing LDS read (ds_read_b64_tr_b16: 4 k x 16 columns for 16 lanes) turns it.
 //
-// Five kernels, from what bounds them: many tiles, the matrix cores (product_stream_kernel); fewer, the latency of a step and the loads to LDS, 64 bytes a clock
+// Four kinds of kernel, from what bounds them: many tiles, the matrix cores (product_stream_kernel); fewer, the latency of a step and the loads to LDS, 64 bytes a clock
 // for a CU (product_tile_kernel; dW from many rows in parts); few rows, the weights' bytes (product_few_kernel); rows of any alignment through registers
 // (product_kernel).  go() says when which one runs.  Sums are held in 32 bits and rounded once, where they are stored.
 #include <type_traits>
@@ -712,9 +712,10 @@ hipError_t go_tile(ProductArgs a, hipStream_t st) {
 //
 // LDS holds five units of 32 KiB, each the 128 bytes of k of one operand's tile, loaded in the order J0 I0 J1 I1 ... of the workgroup's steps, whatever
 // tile they belong to.  In step s a wave multiplies the I fragments of its eight blocks, a ring of four read three blocks ahead, with the four J fragments it
-// holds, and reads the J fragments of step s + 1.  Two barriers a step, each of which waits for one unit, frees one and is followed by the loads of one:
-//   Y, before block 1: J of s + 1 has landed, J of s has been read by all -> I of s + 2
-//   X, before block 5: I of s + 1 has landed, I of s and J of s + 1 have been read by all -> J of s + 3
+// holds, and reads the J fragments of step s + 1 (behind Y, the last of them in block 7).  Two barriers a step, each of which waits for one unit, frees one and is followed
+// by the loads of one into it:
+//   Y, before block 1: J of s + 1 has landed, J of s has been read by all -> I of s + 2 where J of s was
+//   X, before block 5: I of s + 1 has landed, I of s has been read by all -> J of s + 3 where I of s was (J of s + 1 is still being read, up to Y of s + 1)
 // so each load has a step and a half (some 2 us) to arrive.  Behind a barrier MFMAs come first, loads and reads between them: all eight waves are at the
 // same place there, and whatever came before the MFMAs would leave the matrix cores idle.
 // The loop over a tile's steps has no branch but that at a tile's end.
@@ -902,7 +903,6 @@ __global__ __launch_bounds__(512, 2) void product_stream_kernel(ProductArgs a) {
     w.steps = n && n < 4 ? 4 : n;
     return w;
   };
-  // the next tile from t on that has a reduction; dW of an expert without rows is stored as zeros on the way
   floatx4 acc[8][4];
   auto clear = [&] {
 #pragma unroll
@@ -911,6 +911,7 @@ __global__ __launch_bounds__(512, 2) void product_stream_kernel(ProductArgs a) {
       for (int j = 0; j < 4; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
   };
   auto tile_of = [&](int round) { return round * stride + (RAGGED && (round & 1) ? stride - 1 - slot : slot); };
+  // the tile of this round; dW: of the first round from this one on whose tile has a reduction (none left: round is past the end)
   auto next_work = [&](int& round) {
     TileWork w;
     w.steps = 0;
@@ -922,7 +923,7 @@ __global__ __launch_bounds__(512, 2) void product_stream_kernel(ProductArgs a) {
     }
     return w;
   };
-  if constexpr (RAGGED) {
+  if constexpr (RAGGED) {                                      // dW of experts without rows: zeros, ahead of everything else
     clear();
     for (int round = 0; round * stride < end; ++round) {
       const int p = tile_of(round);
