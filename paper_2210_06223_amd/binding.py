@@ -594,7 +594,7 @@ def lasnet_norm_rows_backward(dy: torch.Tensor, s: torch.Tensor, weight: torch.T
     """(dx, dweight) from the gradient dy of lasnet_norm_rows' out and dsum of its sum; s, rstd: as the forward call wrote them."""
     if stream is None and dx is not None and dweight is not None:
         L = lib()
-        cols = s.shape[-1]
+        cols = s.shape[-1] if s.dim() else 0
         need = L.lasnet_norm_rows_backward_workspace_bytes(s.numel() // cols, cols) if cols and workspace is None else 0
         st = _marshal.norm_rows_backward(L.at_norm_rows_backward, dy, s, weight, rstd, dsum, dx, dweight, _workspace(workspace, need, s.device, None)[2])
         if st is not None:

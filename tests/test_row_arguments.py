@@ -49,6 +49,20 @@ def test_a_workspace_in_other_memory_is_refused(which, monkeypatch):
     assert len(L.enqueued) == 1, name
 
 
+def test_tensors_without_rows_are_refused_as_such():
+    """(With all outputs given and without.)"""
+    x, w, none, i = torch.zeros(2, 4), torch.zeros(4), torch.zeros(()), torch.zeros((), dtype=I32)
+    for kw in (dict(), dict(dx=x, dweight=w)):
+        with pytest.raises(ValueError, match="rows"):
+            B.lasnet_norm_rows_backward(none.as_subclass(OnDevice), none.as_subclass(OnDevice), w, w, **kw)
+    for kw in (dict(), dict(offsets=i, order=i, position=i)):
+        with pytest.raises(ValueError, match="experts"):
+            B.lasnet_route(i, 3, **kw)
+    for kw in (dict(), dict(dW=none)):
+        with pytest.raises(ValueError, match="rows|offsets"):
+            B.lasnet_expert_product_dw(none, none, dev(3, dtype=I32), **kw)
+
+
 @pytest.mark.gpu
 def test_a_host_workspace_is_refused_natively_too():
     """(With the outputs given, the calls are offered to the native marshalling: it leaves them to the checks.)"""
