@@ -57,21 +57,23 @@ def map_calls(k):
 @pytest.fixture
 def made(monkeypatch):
     """What is made: (tensor, the stream it is made under)."""
-    under, made, empty = [], [], torch.empty
+    current, made, empty = [CURRENT], [], torch.empty
 
     @contextlib.contextmanager
-    def stream(s):
-        under.append(s)
+    def switched(s):
+        before, current[0] = current[0], s
         yield
-        under.pop()
+        current[0] = before
 
     def recorded(*a, **k):
-        made.append((empty(*a, **k).as_subclass(OnDevice), under[-1] if under else "current"))
+        made.append((empty(*a, **k).as_subclass(OnDevice), current[0]))
         return made[-1][0]
 
-    monkeypatch.setattr(torch.cuda, "stream", stream)
-    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: "current")
+    monkeypatch.setattr(torch.cuda, "stream", switched)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: current[0])
     monkeypatch.setattr(torch.cuda, "Stream", _Stream)
+    monkeypatch.setattr(torch._C, "_cuda_setStream", lambda stream_id, device_index, device_type: current.__setitem__(0, _Stream.by_id[stream_id]), raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
     monkeypatch.setattr(torch, "empty", recorded)
     monkeypatch.setattr(B, "_stream", lambda s: 0 if s is None else s.cuda_stream)
     monkeypatch.setattr(B, "_lib", NoLibrary())
@@ -80,30 +82,35 @@ def made(monkeypatch):
 
 
 class _Stream:
-    cuda_stream = 0x77
+    device_index, device_type, by_id = 0, 1, {}
+
+    def __init__(self, handle):
+        self.stream_id = self.cuda_stream = handle
+        self.by_id[handle] = self
+
+
+CURRENT, SIDE = _Stream(0x11), _Stream(0x77)
 
 
 @pytest.mark.parametrize("which", range(9))
 def test_rows_what_a_call_makes_is_memory_of_its_stream(which, made):
-    side = _Stream()
-    for given in (None, side):
+    for given in (None, CURRENT, SIDE):
         name, call, outputs, workspaces = list(row_calls({} if given is None else {"stream": given}))[which]
         made.clear()
         call()
-        assert [s for _, s in made] == [given or "current"] * (outputs + workspaces), name
+        assert [s for _, s in made] == [given or CURRENT] * (outputs + workspaces), name
         used = [getattr(t, "used_on", []) for t, _ in made]
-        assert used == [["current"] if given else []] * outputs + [[]] * workspaces, name
+        assert used == [[CURRENT] if given is SIDE else []] * outputs + [[]] * workspaces, name
 
 
 @pytest.mark.parametrize("which", range(7))
 def test_maps_what_a_call_makes_is_memory_of_its_stream(which, made):
-    side = _Stream()
-    for given in (None, side):
+    for given in (None, CURRENT, SIDE):
         name, call, outputs = list(map_calls({} if given is None else {"stream": given}))[which]
         made.clear()
         call()
-        assert [s for _, s in made] == [given or "current"] * outputs, name
-        assert [getattr(t, "used_on", []) for t, _ in made] == [["current"] if given else []] * outputs, name
+        assert [s for _, s in made] == [given or CURRENT] * outputs, name
+        assert [getattr(t, "used_on", []) for t, _ in made] == [[CURRENT] if given is SIDE else []] * outputs, name
 
 
 @pytest.mark.gpu
