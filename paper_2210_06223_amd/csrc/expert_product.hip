@@ -706,9 +706,10 @@ hipError_t go_tile(ProductArgs a, hipStream_t st) {
 }
 
 // ---- many tiles: 256 x 256 by eight waves, one workgroup a CU that goes from tile to tile without letting its loads run dry ----
-// 8192 x 8192 x 8192 bf16 810 us, 1360 TFLOP/s (the library's product 745 to 757 us), 8 bits 412 us, 2660 TFLOP/s.  Reductions of 2048 leave a tile's
-// stores more to say: 128 KiB from each of 256 CUs at once, some 9 us a round of tiles at the rate memory takes them (16384 x 2048 x 2048 128 to 137 us, 1000 to
-// 1070 TFLOP/s; 32768 x 4096 x 2048 in 8 bits 301 us, 1830 TFLOP/s).
+// 8192 x 8192 x 8192 bf16 810 us, 1360 TFLOP/s (the library's product 745 to 757 us), 8 bits 412 us, 2660 TFLOP/s.  Reductions of 2048 leave the end of a
+// tile more to say, some 9 to 11 us of each round of tiles beside the loop's rate (16384 x 2048 x 2048 128 to 137 us, 1000 to 1070 TFLOP/s; 32768 x 4096 x 2048 in 8 bits
+// 295 to 302 us, 1830 TFLOP/s): 128 KiB of stores a CU, 8 bytes a lane in bf16, 32 of a row's bytes at a time.  That all CUs store at once is not what it
+// costs: with every second workgroup at another place of its tile it was the same.
 //
 // LDS holds five units of 32 KiB, each the 128 bytes of k of one operand's tile, loaded in the order J0 I0 J1 I1 ... of the workgroup's steps, whatever
 // tile they belong to.  In step s a wave multiplies the I fragments of its eight blocks, a ring of four read three blocks ahead, with the four J fragments it

@@ -5,7 +5,7 @@
 // table's value before plus the lanes ahead of it.  What moves rows is bound by memory: each token's row is read once, the k copies are written
 // (or read) once, and sums run over j in order, so nothing depends on timing.
 //
-//   sort: a chain of LDS and memory accesses: 32 slots of 64 experts 3 us, 65536 10, 4 Mi 71.  Rows, at the rate of large copies: dispatch of 16384 x 2048 bf16 to
+//   sort: a chain of LDS and memory accesses: 32 slots of 64 experts 3 us, 65536 11, 4 Mi 67 (of 8 experts 56, of 256 115).  Rows, at the rate of large copies: dispatch of 16384 x 2048 bf16 to
 //   four experts each (335 MB) with the sort 60 us, sum of them into the residual (386 MB) 74, its gradient (604 MB) 109.
 #include "row_ops.hpp"
 
