@@ -8,6 +8,9 @@ Rows are tokens, or the pixels of a feature map [N,H,W,C] (N*H*W rows as they li
 serve() runs it with W1 in 8 bits (rows and weights e4m3, as lasnet_norm_rows and pack() write them) and W2 in bfloat16; train_step() in bfloat16, with all
 gradients.  Both take any number of rows, one included.  The router's small product, top-k and softmax are torch's.
 
+The router reads the rows as the experts do: in 8 bits in serve(), in bfloat16 in train_step(), so where two logits are closer than that rounding the two may choose
+different experts for a row.
+
 `python -m paper_2210_06223_amd.expert_layer` times both on synthetic rows.
 """
 from __future__ import annotations
