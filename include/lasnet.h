@@ -60,6 +60,8 @@ typedef enum { LASNET_F32 = 0, LASNET_BF16 = 1 } lasnet_dtype;
  * E4M3: 1 sign, 4 exponent, 3 fraction bits, bias 7, no infinity, 0x7f / 0xff = NaN, largest value 448.
  * A scale of 8-bit rows is a byte b that stands for 2^(b - 127) (255: NaN). */
 enum { LASNET_E4M3 = 2 };
+/* The type of scales that are such bytes, where a call takes other ones, too. */
+enum { LASNET_E8M0 = 3 };
 
 /* Dense NHWC feature map in device memory: element (n,h,w,c) at ((n*H+h)*W+w)*C+c. */
 typedef struct {
@@ -81,6 +83,8 @@ enum {
                                   the library would pick the fused one; LASNET_EUNSUPPORTED where
                                   it has none, or in lasnet_sparse_bottleneck_noalloc           */
 };
+/* Flag of lasnet_choose_experts and its backward: weights are shares of all experts' sum, not of the chosen ones'. */
+enum { LASNET_WEIGHTS_OF_ALL = 32 };
 
 LASNET_API int lasnet_version(void);
 LASNET_API const char* lasnet_status_string(int status); /* host pointer to a static string */
@@ -416,6 +420,71 @@ LASNET_API size_t lasnet_expert_product_dw_workspace_bytes(int64_t rows, int E, 
 LASNET_API int lasnet_expert_product_dw_ex(const lasnet_rows* dy, const lasnet_rows* x, const int32_t* offsets, int E,
                                            void* dW, int dw_dtype, void* workspace, size_t workspace_bytes,
                                            void* hip_stream);
+
+/*
+ * The router's choice.  logits: tokens rows (F32 or BF16) of E columns, E up to 4096.  For each token that takes part
+ *   experts [tokens * k]   the k largest logits' experts, largest first; among equal ones the lowest number comes first.  k up to 64 (more than E: the rest as below)
+ *   weights [tokens * k]   softmax over those k logits; LASNET_WEIGHTS_OF_ALL: over all E
+ *   lse     [tokens]       log sum_e exp(logits[t][e]).  NULL: not written
+ * mask: NULL, or [tokens] bytes: a token of 0 takes no part, and its logits may be anything.  A logit of -inf is never chosen.  A slot for which nothing is left, and all
+ * slots of a token that takes no part or has no other logits: expert -1 (lasnet_route sends nothing), weight 0; such a token's lse is -inf.
+ * NaN is above every number; a token that has one, or +inf, has experts as the others, and NaN for its weights and lse.
+ * flags: LASNET_WEIGHTS_OF_ALL.
+ */
+LASNET_API int lasnet_choose_experts(const lasnet_rows* logits, const uint8_t* mask, int k, int32_t* experts, float* weights, float* lse,
+                                     uint32_t flags, void* hip_stream);
+
+/*
+ * How evenly the experts are used.  logits, lse, experts as above (experts may be others: entries outside [0, E), slots beyond a capacity, do not count).  With T = the tokens
+ * whose lse is not -inf, p[t][e] = exp(logits[t][e] - lse[t]):
+ *   counts [E + 1]   rows of each expert; counts[E] = T
+ *   share  [E]       1/T sum_t p[t][e]
+ *   loss   [2]       E sum_e counts[e] / (k T) share[e] (1 where all are used alike), and 1/T sum_t lse[t]^2.  T = 0: zeros
+ * Sums over tokens in 64 bits and a fixed order.  workspace: lasnet_balance_workspace_bytes(tokens, E) bytes (0: NULL will do).
+ */
+LASNET_API size_t lasnet_balance_workspace_bytes(int64_t tokens, int E);
+LASNET_API int lasnet_balance(const lasnet_rows* logits, const float* lse, const int32_t* experts, int k, int32_t* counts, float* share,
+                              float* loss, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * The logits' gradient of both: of the weights (dweights, [tokens * k], NULL = 0), and of dloss[0] * loss[0] + dloss[1] * loss[1] (dloss: [2] on the device, NULL = 0; with
+ * counts as lasnet_balance wrote them, which are constants here):
+ *   dlogits[t][e] = p (c[e] - sum_e p c) + 2 dloss[1] lse p / T + (weights' part)          c[e] = dloss[0] E counts[e] / (k T^2)
+ *   weights' part, s = sum_j weights[j] dweights[j]:  sum over the slots j with expert e of weights[j] (dweights[j] - s)
+ *                  LASNET_WEIGHTS_OF_ALL:             sum over those slots of weights[j] dweights[j], minus p s
+ * A slot with an expert outside [0, E) adds to s alone; an expert may be in several slots.  A token whose lse is -inf gets zeros.
+ * dlogits: as logits, and may be the same rows.  In fp32, rounded once.  flags: as the forward call's.
+ */
+LASNET_API int lasnet_choose_experts_backward(const lasnet_rows* logits, const float* lse, const int32_t* experts, const float* weights, int k,
+                                              const float* dweights, const int32_t* counts, const float* dloss, const lasnet_rows* dlogits,
+                                              uint32_t flags, void* hip_stream);
+
+/*
+ * Rows in 8 bits with a scale for each 128 columns:  out = E4M3(x / 2^e), scale = e + 127: the least e, at least -126, with max |x| over the block <= 448 * 2^e (NaN aside).
+ * x: tokens rows, F32 or BF16.  position NULL: out has as many rows (offsets NULL, k and E not looked at).  Else they are laid out by expert on the way, as lasnet_dispatch_rows
+ * would (position [tokens * k], offsets [E + 1]): out has tokens * k rows, those from offsets[E] on are zeros with scales of 127.
+ * scale: [out.rows][(cols + 127) / 128] bytes, dense.
+ */
+LASNET_API int lasnet_quantize_rows(const lasnet_rows* x, const int32_t* position, const int32_t* offsets, int k, int E, const lasnet_rows* out,
+                                    uint8_t* scale, void* hip_stream);
+
+/*
+ * The experts' matrices in 8 bits with a scale for each block of 128 x 128, by the same rule.  W: [E][n][k], dense, dtype F32 or BF16; out: [E][n][k], scale:
+ * [E][(n + 127) / 128][(k + 127) / 128] bytes.  out_t, scale_t: both NULL, or the same matrices transposed, [E][k][n], with their scales, as the gradient of the rows needs them.
+ */
+LASNET_API int lasnet_quantize_matrices(const void* W, int dtype, int E, int n, int k, void* out, uint8_t* scale, void* out_t, uint8_t* scale_t,
+                                        void* hip_stream);
+
+/*
+ * The experts' products of such rows and matrices: for every row p of expert e
+ *   out[p][i] = sum over blocks b of 2^(scale[p][b] - 127) * wscale[e][i / 128][b] * sum_{c in b} x[p][c] * W[e][i][c]
+ * x: E4M3, scale [rows][(cols + 127) / 128]; W: [E][out.cols][x.cols], E4M3, dense; wscale: [E][(out.cols + 127) / 128][(cols + 127) / 128], wscale_dtype LASNET_E8M0
+ * (bytes, as lasnet_quantize_matrices writes them: applied by the matrix core) or LASNET_F32.  A block's sum is the matrix core's own, as with lasnet_expert_product; blocks are added
+ * in fp32, and out (BF16) is rounded once.  Rows from offsets[E] on are set to zero.  flags, offsets: as there.
+ * The gradient of x is the same product of dy and the transposed matrices; that of W: lasnet_expert_product_dw of the rows in BF16.
+ */
+LASNET_API int lasnet_block_product(const lasnet_rows* x, const uint8_t* scale, const int32_t* offsets, int E, const void* W, const void* wscale,
+                                    int wscale_dtype, const lasnet_rows* out, uint32_t flags, void* hip_stream);
 
 /*
  * Microbenchmarks for the measurement harness (what this GPU sustains, beside the data-sheet peaks the

@@ -18,8 +18,9 @@ _LIB_PATH = os.environ.get("LASNET_LIBRARY") or os.path.join(
 _lib = None
 _marshal = None
 
-LASNET_F32, LASNET_BF16, LASNET_E4M3 = 0, 1, 2
+LASNET_F32, LASNET_BF16, LASNET_E4M3, LASNET_E8M0 = 0, 1, 2, 3
 LASNET_POST_RELU, LASNET_FORCE_GENERIC, LASNET_SKIP_IDENTITY, LASNET_FORCE_FUSED, LASNET_FORCE_TILED = 1, 2, 4, 8, 16
+LASNET_WEIGHTS_OF_ALL = 32
 LASNET_OK, LASNET_EINVAL, LASNET_ESHAPE, LASNET_EUNSUPPORTED, LASNET_EALIAS, LASNET_EHIP = 0, -1, -2, -3, -4, -5
 LASNET_ETOOBIG = -6
 LASNET_NOALLOC_MAX_PACKED_BYTES = 4 << 20
@@ -35,12 +36,15 @@ EXPORTS = (
     "lasnet_route", "lasnet_route_workspace_bytes", "lasnet_dispatch_rows", "lasnet_combine_rows",
     "lasnet_combine_rows_backward", "lasnet_expert_product", "lasnet_expert_product_dx", "lasnet_expert_product_dw",
     "lasnet_expert_product_dw_ex", "lasnet_expert_product_dw_workspace_bytes",
+    "lasnet_choose_experts", "lasnet_choose_experts_backward", "lasnet_balance", "lasnet_balance_workspace_bytes",
+    "lasnet_quantize_rows", "lasnet_quantize_matrices", "lasnet_block_product",
 )
 
 
 # the calls on rows that _marshal takes
 _ROW_CALLS = ("norm_rows", "norm_rows_backward", "route", "dispatch_rows", "combine_rows", "combine_rows_backward", "expert_product",
-              "expert_product_dx", "expert_product_dw_ex")
+              "expert_product_dx", "expert_product_dw_ex", "choose_experts", "choose_experts_backward", "balance", "quantize_rows", "quantize_matrices",
+              "block_product")
 
 
 class LasnetError(RuntimeError):
@@ -122,7 +126,14 @@ def load_library(path: str) -> ctypes.CDLL:
             ("expert_product_dx", ip, [rp, vp, ip, vp, rp, vp]),
             ("expert_product_dw", ip, [rp, rp, vp, ip, vp, ip, vp]),
             ("expert_product_dw_workspace_bytes", sz, [i64, ip, ip, ip]),
-            ("expert_product_dw_ex", ip, [rp, rp, vp, ip, vp, ip, vp, sz, vp])):
+            ("expert_product_dw_ex", ip, [rp, rp, vp, ip, vp, ip, vp, sz, vp]),
+            ("choose_experts", ip, [rp, vp, ip, vp, vp, vp, ctypes.c_uint32, vp]),
+            ("choose_experts_backward", ip, [rp, vp, vp, vp, ip, vp, vp, vp, rp, ctypes.c_uint32, vp]),
+            ("balance_workspace_bytes", sz, [i64, ip]),
+            ("balance", ip, [rp, vp, vp, ip, vp, vp, vp, vp, sz, vp]),
+            ("quantize_rows", ip, [rp, vp, vp, ip, ip, rp, vp, vp]),
+            ("quantize_matrices", ip, [vp, ip, ip, ip, ip, vp, vp, vp, vp, vp]),
+            ("block_product", ip, [rp, vp, vp, ip, vp, vp, ip, rp, ctypes.c_uint32, vp])):
         f = getattr(L, "lasnet_" + name)
         f.restype, f.argtypes = result, args
     # the entry points that _marshal calls, by address
@@ -140,6 +151,7 @@ class _AllThroughCtypes:
     masker_ex = block_ex = block_dense = block_packed = block_planned = staticmethod(lambda *args: None)
     norm_rows = norm_rows_backward = route = dispatch_rows = combine_rows = combine_rows_backward = masker_ex
     expert_product = expert_product_dx = expert_product_dw = masker_ex
+    choose_experts = choose_experts_backward = balance = quantize_rows = quantize_matrices = block_product = masker_ex
 
 
 def _load_marshal() -> None:
@@ -811,3 +823,172 @@ def lasnet_expert_product_dw(dy: torch.Tensor, x: torch.Tensor, offsets: torch.T
                                        _matrices(dW, E, d.cols, v.cols, torch.bfloat16, torch.float32), _ROW_DTYPES[dW.dtype], at, size, _stream(stream))
     _check(st, "lasnet_expert_product_dw_ex")
     return dW
+
+
+# ---- the router, and products in 8 bits with scales for blocks of 128 ----
+
+def lasnet_choose_experts(logits: torch.Tensor, k: int, mask: Optional[torch.Tensor] = None, experts: Optional[torch.Tensor] = None,
+                          weights: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, flags: int = 0, stream=None):
+    """(experts int32 [tokens, k], weights [tokens, k], lse [tokens]): each token's k largest of logits [tokens, E], their softmax (LASNET_WEIGHTS_OF_ALL: among all), and
+    the logarithm of the sum of exponentials.  mask (uint8 or bool [tokens]): 0, the token takes no part (experts -1)."""
+    if stream is None and experts is not None and weights is not None and lse is not None:
+        L = lib()
+        st = _marshal.choose_experts(L.at_choose_experts, logits, mask, k, experts, weights, lse, flags)
+        if st is not None:
+            _check(st, "lasnet_choose_experts")
+            return experts, weights, lse
+    d = _rows(logits, "logits")
+    if k > 0:
+        if experts is None:
+            experts = _output((d.rows, k), torch.int32, logits.device, stream)
+        if weights is None:
+            weights = _output((d.rows, k), torch.float32, logits.device, stream)
+    if lse is None:
+        lse = _output(d.rows, torch.float32, logits.device, stream)
+    st = lib().lasnet_choose_experts(ctypes.byref(d), _dense(mask, "mask", d.rows, torch.uint8, torch.bool), k, _dense(experts, "experts", d.rows * k, torch.int32),
+                                     _dense(weights, "weights", d.rows * k, torch.float32), _dense(lse, "lse", d.rows, torch.float32), flags, _stream(stream))
+    _check(st, "lasnet_choose_experts")
+    return experts, weights, lse
+
+
+def _chosen(experts: torch.Tensor) -> int:
+    if experts.dim() != 2 or experts.dtype != torch.int32 or not experts.is_cuda or not experts.is_contiguous():
+        raise ValueError("experts must be a contiguous int32 device tensor [tokens, k]")
+    return experts.shape[1]
+
+
+def lasnet_balance(logits: torch.Tensor, lse: torch.Tensor, experts: torch.Tensor, counts: Optional[torch.Tensor] = None, share: Optional[torch.Tensor] = None,
+                   loss: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """(counts int32 [E + 1], share [E], loss [2]): rows of each expert (and, last, the tokens that took part), mean probabilities, the balance loss and the mean of lse^2."""
+    L = lib()
+    if stream is None and counts is not None and share is not None and loss is not None:
+        need = L.lasnet_balance_workspace_bytes(logits.shape[0], logits.shape[1]) if workspace is None and logits.dim() == 2 else 0
+        st = _marshal.balance(L.at_balance, logits, lse, experts, counts, share, loss, _workspace(workspace, need, logits.device, None)[2])
+        if st is not None:
+            _check(st, "lasnet_balance")
+            return counts, share, loss
+    d, k = _rows(logits, "logits"), _chosen(experts)
+    if counts is None:
+        counts = _output(d.cols + 1, torch.int32, logits.device, stream)
+    if share is None:
+        share = _output(d.cols, torch.float32, logits.device, stream)
+    if loss is None:
+        loss = _output(2, torch.float32, logits.device, stream)
+    at, size, keep = _workspace(workspace, L.lasnet_balance_workspace_bytes(d.rows, d.cols), logits.device, stream)
+    st = L.lasnet_balance(ctypes.byref(d), _dense(lse, "lse", d.rows, torch.float32), _dense(experts, "experts", d.rows * k, torch.int32), k,
+                          _dense(counts, "counts", d.cols + 1, torch.int32), _dense(share, "share", d.cols, torch.float32),
+                          _dense(loss, "loss", 2, torch.float32), at, size, _stream(stream))
+    _check(st, "lasnet_balance")
+    return counts, share, loss
+
+
+def lasnet_choose_experts_backward(logits: torch.Tensor, lse: torch.Tensor, experts: torch.Tensor, weights: torch.Tensor, dweights: Optional[torch.Tensor] = None,
+                                   counts: Optional[torch.Tensor] = None, dloss: Optional[torch.Tensor] = None, dlogits: Optional[torch.Tensor] = None,
+                                   flags: int = 0, stream=None) -> torch.Tensor:
+    """dlogits (as logits) from the gradient dweights of the weights and dloss [2] of lasnet_balance's loss (with its counts)."""
+    if stream is None and dlogits is not None:
+        L = lib()
+        st = _marshal.choose_experts_backward(L.at_choose_experts_backward, logits, lse, experts, weights, dweights, counts, dloss, dlogits, flags)
+        if st is not None:
+            _check(st, "lasnet_choose_experts_backward")
+            return dlogits
+    d, k = _rows(logits, "logits"), _chosen(experts)
+    if dlogits is None:
+        dlogits = _output(logits.shape, logits.dtype, logits.device, stream)
+    o = _rows(dlogits, "dlogits")
+    st = lib().lasnet_choose_experts_backward(ctypes.byref(d), _dense(lse, "lse", d.rows, torch.float32), _dense(experts, "experts", d.rows * k, torch.int32),
+                                              _dense(weights, "weights", d.rows * k, torch.float32), k, _dense(dweights, "dweights", d.rows * k, torch.float32),
+                                              _dense(counts, "counts", d.cols + 1, torch.int32), _dense(dloss, "dloss", 2, torch.float32), ctypes.byref(o),
+                                              flags, _stream(stream))
+    _check(st, "lasnet_choose_experts_backward")
+    return dlogits
+
+
+def _blocks(n: int) -> int:
+    return (n + 127) // 128
+
+
+def lasnet_quantize_rows(x: torch.Tensor, position: Optional[torch.Tensor] = None, offsets: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                         scale: Optional[torch.Tensor] = None, stream=None):
+    """(out e4m3, scale [rows, ceil(cols / 128)]): x in 8 bits with a scale for each 128 columns; with position and offsets laid out by expert, as lasnet_dispatch_rows does."""
+    if stream is None and out is not None and scale is not None:
+        L = lib()
+        st = _marshal.quantize_rows(L.at_quantize_rows, x, position, offsets, out, scale)
+        if st is not None:
+            _check(st, "lasnet_quantize_rows")
+            return out, scale
+    d = _rows(x, "x")
+    if (position is None) != (offsets is None):
+        raise ValueError("position and offsets come together")
+    if position is None:
+        k, E, rows = 1, 1, d.rows
+    else:
+        tokens, k = _slots(position)
+        E, rows = _offsets(offsets), tokens * k
+        if d.rows != tokens:
+            raise ValueError("x and position must have as many tokens")
+    if out is None:
+        out = _output(x.shape if position is None else (rows, d.cols), torch.float8_e4m3fn, x.device, stream)
+    if scale is None:
+        scale = _output((rows, _blocks(d.cols)), torch.float8_e8m0fnu, x.device, stream)
+    o = _rows(out, "out")
+    st = lib().lasnet_quantize_rows(ctypes.byref(d), _ptr(position), _ptr(offsets), k, E, ctypes.byref(o),
+                                    _dense(scale, "scale", rows * _blocks(d.cols), *_SCALE_DTYPES), _stream(stream))
+    _check(st, "lasnet_quantize_rows")
+    return out, scale
+
+
+def lasnet_quantize_matrices(W: torch.Tensor, transposed: bool = False, out: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                             out_t: Optional[torch.Tensor] = None, scale_t: Optional[torch.Tensor] = None, stream=None):
+    """(out e4m3 [E, n, k], scale [E, ceil(n / 128), ceil(k / 128)], out_t [E, k, n], scale_t): the experts' matrices in 8 bits with a scale for each block of 128 x 128.
+    transposed: makes the last two, too (else None, where they are not given)."""
+    if stream is None and out is not None and scale is not None and (not transposed or (out_t is not None and scale_t is not None)):
+        L = lib()
+        st = _marshal.quantize_matrices(L.at_quantize_matrices, W, out, scale, out_t, scale_t)
+        if st is not None:
+            _check(st, "lasnet_quantize_matrices")
+            return out, scale, out_t, scale_t
+    if W.dim() != 3 or W.dtype not in _DTYPES:
+        raise ValueError("the experts' matrices are float32 or bfloat16 [E, n, k]")
+    E, n, k = W.shape
+    if (out_t is None) != (scale_t is None):
+        raise ValueError("out_t and scale_t come together")
+    if out is None:
+        out = _output((E, n, k), torch.float8_e4m3fn, W.device, stream)
+    if scale is None:
+        scale = _output((E, _blocks(n), _blocks(k)), torch.float8_e8m0fnu, W.device, stream)
+    if out_t is None and transposed:
+        out_t = _output((E, k, n), torch.float8_e4m3fn, W.device, stream)
+        scale_t = _output((E, _blocks(k), _blocks(n)), torch.float8_e8m0fnu, W.device, stream)
+    cells = E * _blocks(n) * _blocks(k)
+    st = lib().lasnet_quantize_matrices(_matrices(W, E, n, k, W.dtype), _DTYPES[W.dtype], E, n, k, _matrices(out, E, n, k, torch.float8_e4m3fn),
+                                        _dense(scale, "scale", cells, *_SCALE_DTYPES), None if out_t is None else _matrices(out_t, E, k, n, torch.float8_e4m3fn),
+                                        _dense(scale_t, "scale_t", cells, *_SCALE_DTYPES), _stream(stream))
+    _check(st, "lasnet_quantize_matrices")
+    return out, scale, out_t, scale_t
+
+
+def lasnet_block_product(x: torch.Tensor, scale: torch.Tensor, offsets: torch.Tensor, W: torch.Tensor, wscale: torch.Tensor,
+                         out: Optional[torch.Tensor] = None, flags: int = 0, stream=None) -> torch.Tensor:
+    """out[p] = W[e] x[p] for the rows p of each expert e: e4m3 rows with scale [rows, ceil(cols / 128)] and matrices [E, n, cols] with wscale
+    [E, ceil(n / 128), ceil(cols / 128)] (e8m0 as lasnet_quantize_matrices writes them, or float32); out bfloat16."""
+    if stream is None and out is not None:
+        L = lib()
+        st = _marshal.block_product(L.at_block_product, x, scale, offsets, W, wscale, out, flags)
+        if st is not None:
+            _check(st, "lasnet_block_product")
+            return out
+    E, d = _offsets(offsets), _rows(x, "x")
+    if W.dim() != 3:
+        raise ValueError("the experts' matrices are [E, n, cols]")
+    n = W.shape[1]
+    if out is None:
+        out = _output((d.rows, n), torch.bfloat16, x.device, stream)
+    o = _rows(out, "out")
+    if o.cols != n:
+        raise ValueError("out must have %d columns" % n)
+    st = lib().lasnet_block_product(ctypes.byref(d), _dense(scale, "scale", d.rows * _blocks(d.cols), *_SCALE_DTYPES), _ptr(offsets), E,
+                                    _matrices(W, E, n, d.cols, x.dtype), _dense(wscale, "wscale", E * _blocks(n) * _blocks(d.cols), torch.float32, *_SCALE_DTYPES),
+                                    LASNET_F32 if wscale.dtype == torch.float32 else LASNET_E8M0, ctypes.byref(o), flags, _stream(stream))
+    _check(st, "lasnet_block_product")
+    return out

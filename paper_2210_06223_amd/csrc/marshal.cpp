@@ -109,6 +109,13 @@ struct Plain {                                       // false from any of these:
     if (!need(t && t->defined())) return nullptr;
     return dense<T>(o, t->scalar_type() == at::kByte ? at::kByte : at::ScalarType::Float8_e8m0fnu, n);
   }
+  // bytes or truth values, or None
+  const uint8_t* mask(PyObject* o, int64_t n) {
+    if (o == Py_None || !ok) return nullptr;
+    const at::Tensor* t = tensor(o);
+    if (!need(t && t->defined())) return nullptr;
+    return dense<const uint8_t>(o, t->scalar_type() == at::kBool ? at::kBool : at::kByte, n);
+  }
   // [tokens, k]
   const int32_t* slots(PyObject* o, int64_t& tokens, int& k) {
     const int32_t* p = of_type<const int32_t>(o, at::kInt);
@@ -470,7 +477,138 @@ PyObject* expert_product_dw(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// (logits, mask, k, experts, weights, lse, flags)
+PyObject* choose_experts(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 8, [&](Plain& p) {
+    lasnet_rows logits;
+    p.rows(a[1], logits);
+    const int k = p.integer(a[3]), flags = p.integer(a[7]);
+    if (!p.ok) return 0;
+    const uint8_t* mask = p.mask(a[2], logits.rows);
+    int32_t* experts = p.dense<int32_t>(a[4], at::kInt, logits.rows * k);
+    float* weights = p.dense<float>(a[5], at::kFloat, logits.rows * k);
+    float* lse = p.dense<float>(a[6], at::kFloat, logits.rows);
+    if (!p.ok) return 0;
+    auto* f = entry<decltype(lasnet_choose_experts)>(a[0]);
+    ENQUEUE(f(&logits, mask, k, experts, weights, lse, (uint32_t)flags, st));
+  });
+}
+
+// (logits, lse, experts, counts, share, loss, workspace)
+PyObject* balance(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 8, [&](Plain& p) {
+    lasnet_rows logits;
+    int64_t tokens;
+    int k;
+    p.rows(a[1], logits);
+    const int32_t* experts = p.slots(a[3], tokens, k);
+    if (!p.ok || !p.need(tokens == logits.rows)) return 0;
+    const float* lse = p.dense<const float>(a[2], at::kFloat, logits.rows);
+    int32_t* counts = p.dense<int32_t>(a[4], at::kInt, (int64_t)logits.cols + 1);
+    float* share = p.dense<float>(a[5], at::kFloat, logits.cols);
+    float* loss = p.dense<float>(a[6], at::kFloat, 2);
+    size_t bytes;
+    void* workspace = p.workspace(a[7], a[1], bytes);
+    if (!p.ok) return 0;
+    auto* f = entry<decltype(lasnet_balance)>(a[0]);
+    ENQUEUE(f(&logits, lse, experts, k, counts, share, loss, workspace, bytes, st));
+  });
+}
+
+// (logits, lse, experts, weights, dweights, counts, dloss, dlogits, flags)
+PyObject* choose_experts_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 10, [&](Plain& p) {
+    lasnet_rows logits, dlogits;
+    int64_t tokens;
+    int k;
+    p.rows(a[1], logits);
+    const int32_t* experts = p.slots(a[3], tokens, k);
+    p.rows(a[8], dlogits);
+    const int flags = p.integer(a[9]);
+    if (!p.ok || !p.need(tokens == logits.rows)) return 0;
+    const float* lse = p.dense<const float>(a[2], at::kFloat, logits.rows);
+    const float* weights = p.dense<const float>(a[4], at::kFloat, tokens * k);
+    const float* dweights = p.dense<const float>(a[5], at::kFloat, tokens * k);
+    const int32_t* counts = p.dense<const int32_t>(a[6], at::kInt, (int64_t)logits.cols + 1);
+    const float* dloss = p.dense<const float>(a[7], at::kFloat, 2);
+    if (!p.ok) return 0;
+    auto* f = entry<decltype(lasnet_choose_experts_backward)>(a[0]);
+    ENQUEUE(f(&logits, lse, experts, weights, k, dweights, counts, dloss, &dlogits, (uint32_t)flags, st));
+  });
+}
+
+inline int64_t blocks(int64_t n) { return (n + 127) / 128; }
+
+// (x, position, offsets, out, scale)
+PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 6, [&](Plain& p) {
+    lasnet_rows x, out;
+    int64_t tokens = 0;
+    int k = 1, E = 1;
+    p.rows(a[1], x);
+    p.rows(a[4], out);
+    const int32_t *position = nullptr, *offsets = nullptr;
+    if (!p.ok || !p.need((a[2] == Py_None) == (a[3] == Py_None))) return 0;
+    if (a[2] != Py_None) {
+      position = p.slots(a[2], tokens, k);
+      offsets = p.offsets(a[3], E);
+      if (!p.ok || !p.need(tokens == x.rows)) return 0;
+    }
+    uint8_t* scale = p.scale<uint8_t>(a[5], x.rows * k * blocks(x.cols));
+    if (!p.ok) return 0;
+    auto* f = entry<decltype(lasnet_quantize_rows)>(a[0]);
+    ENQUEUE(f(&x, position, offsets, k, E, &out, scale, st));
+  });
+}
+
+// (W, out, scale, out_t, scale_t)
+PyObject* quantize_matrices(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 6, [&](Plain& p) {
+    const at::Tensor* W = tensor(a[1]);
+    if (!p.need(W && W->defined() && W->dim() == 3 && W->size(0) <= INT32_MAX && W->size(1) <= INT32_MAX && W->size(2) <= INT32_MAX)) return 0;
+    const auto ty = W->scalar_type();
+    if (!p.need((ty == at::kFloat || ty == at::kBFloat16) && (a[4] == Py_None) == (a[5] == Py_None))) return 0;
+    const int64_t E = W->size(0), rows = W->size(1), k = W->size(2), cells = E * blocks(rows) * blocks(k);
+    const void* from = p.matrices(a[1], E, rows, k, ty);
+    void* out = p.matrices(a[2], E, rows, k, at::ScalarType::Float8_e4m3fn);
+    uint8_t* scale = p.scale<uint8_t>(a[3], cells);
+    void* out_t = a[4] == Py_None ? nullptr : p.matrices(a[4], E, k, rows, at::ScalarType::Float8_e4m3fn);
+    uint8_t* scale_t = p.scale<uint8_t>(a[5], cells);
+    if (!p.ok) return 0;
+    auto* f = entry<decltype(lasnet_quantize_matrices)>(a[0]);
+    ENQUEUE(f(from, ty == at::kFloat ? LASNET_F32 : LASNET_BF16, (int)E, (int)rows, (int)k, out, scale, out_t, scale_t, st));
+  });
+}
+
+// (x, scale, offsets, W, wscale, out, flags)
+PyObject* block_product(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 8, [&](Plain& p) {
+    lasnet_rows x, out;
+    int E;
+    p.rows(a[1], x);
+    const int32_t* offsets = p.offsets(a[3], E);
+    p.rows(a[6], out);
+    const int flags = p.integer(a[7]);
+    const at::Tensor* ws = tensor(a[5]);
+    if (!p.ok || !p.need(ws && ws->defined())) return 0;
+    const bool floats = ws->scalar_type() == at::kFloat;
+    const int64_t cells = E * blocks(out.cols) * blocks(x.cols);
+    const void* W = p.matrices(a[4], E, out.cols, x.cols, row_type(x.dtype));
+    const uint8_t* scale = p.scale<const uint8_t>(a[2], x.rows * blocks(x.cols));
+    const void* wscale = floats ? (const void*)p.dense<const float>(a[5], at::kFloat, cells) : p.scale<const uint8_t>(a[5], cells);
+    if (!p.ok) return 0;
+    auto* f = entry<decltype(lasnet_block_product)>(a[0]);
+    ENQUEUE(f(&x, scale, offsets, E, W, wscale, floats ? LASNET_F32 : LASNET_E8M0, &out, (uint32_t)flags, st));
+  });
+}
+
 PyMethodDef methods[] = {
+    {"choose_experts", (PyCFunction)(void*)choose_experts, METH_FASTCALL, nullptr},
+    {"choose_experts_backward", (PyCFunction)(void*)choose_experts_backward, METH_FASTCALL, nullptr},
+    {"balance", (PyCFunction)(void*)balance, METH_FASTCALL, nullptr},
+    {"quantize_rows", (PyCFunction)(void*)quantize_rows, METH_FASTCALL, nullptr},
+    {"quantize_matrices", (PyCFunction)(void*)quantize_matrices, METH_FASTCALL, nullptr},
+    {"block_product", (PyCFunction)(void*)block_product, METH_FASTCALL, nullptr},
     {"norm_rows", (PyCFunction)(void*)norm_rows, METH_FASTCALL, nullptr},
     {"norm_rows_backward", (PyCFunction)(void*)norm_rows_backward, METH_FASTCALL, nullptr},
     {"route", (PyCFunction)(void*)route, METH_FASTCALL, nullptr},

@@ -35,13 +35,6 @@ __device__ __forceinline__ void load_weights(const float* w, int n, float* f, in
   }
 }
 
-// Exponent field (127 + e) of the row's scale 2^e: a = M 2^E with 1 <= M < 2 needs e = E - 8 up to M = 1.75 (448 = 1.75 2^8), else E - 7.
-__device__ __forceinline__ int scale_byte(float a) {
-  const unsigned u = __float_as_uint(a);
-  const int e = (int)(u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u);
-  return e < 1 ? 1 : e;
-}
-
 // T: the rows' type; E4M3: out has 8 bits.
 template <class T, bool E4M3, int L, int N>
 __global__ __launch_bounds__(L < 256 ? 256 : L) void norm_rows_kernel(NormArgs a) {

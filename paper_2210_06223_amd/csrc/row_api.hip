@@ -59,6 +59,15 @@ bool clash(std::initializer_list<const void*> outputs, std::initializer_list<con
 }
 int enqueued(hipError_t e) { return e == hipSuccess ? LASNET_OK : LASNET_EHIP; }
 
+// logits: rows of E columns
+int check_logits(const lasnet_rows* t, int k) {
+  const int s = check_rows(t, 1u << LASNET_F32 | 1u << LASNET_BF16);
+  if (s != LASNET_OK) return s;
+  const int c = check_experts(k, t->cols);
+  if (c != LASNET_OK) return c;
+  return t->rows * k > kMaxRows ? LASNET_EUNSUPPORTED : LASNET_OK;
+}
+
 #define CHECK(call)                      \
   do {                                   \
     const int s_ = (call);               \
@@ -227,6 +236,92 @@ int lasnet_expert_product_dw_ex(const lasnet_rows* dy, const lasnet_rows* x, con
   if (!device_ok()) return LASNET_EHIP;
   return enqueued(launch_expert_product_dw(x->rows, E, dy->cols, x->cols, arg(dy), arg(x), offsets, dW, dw_dtype == LASNET_F32, workspace,
                                            (hipStream_t)hip_stream));
+}
+
+int lasnet_choose_experts(const lasnet_rows* logits, const uint8_t* mask, int k, int32_t* experts, float* weights, float* lse, uint32_t flags,
+                          void* hip_stream) {
+  CHECK(check_logits(logits, k));
+  if (flags & ~(uint32_t)LASNET_WEIGHTS_OF_ALL) return LASNET_EINVAL;
+  if (logits->rows > 0 && (!experts || !weights)) return LASNET_EINVAL;
+  if (clash({experts, weights, lse}, {at(logits), mask})) return LASNET_EALIAS;
+  if (!device_ok()) return LASNET_EHIP;
+  if (logits->rows == 0) return LASNET_OK;
+  return enqueued(launch_choose(logits->dtype, logits->rows, logits->cols, k, (flags & LASNET_WEIGHTS_OF_ALL) != 0, arg(logits), mask, experts,
+                                weights, lse, (hipStream_t)hip_stream));
+}
+
+size_t lasnet_balance_workspace_bytes(int64_t tokens, int E) {
+  if (tokens <= 0 || tokens > kMaxRows || check_experts(1, E) != LASNET_OK) return 0;
+  return balance_workspace_bytes(tokens, E);
+}
+
+int lasnet_balance(const lasnet_rows* logits, const float* lse, const int32_t* experts, int k, int32_t* counts, float* share, float* loss,
+                   void* workspace, size_t workspace_bytes, void* hip_stream) {
+  CHECK(check_logits(logits, k));
+  if (!counts || !share || !loss || (logits->rows > 0 && (!lse || !experts))) return LASNET_EINVAL;
+  const size_t need = lasnet_balance_workspace_bytes(logits->rows, logits->cols);
+  if (need && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255))) return LASNET_EINVAL;
+  if (clash({counts, share, loss, workspace}, {at(logits), lse, experts})) return LASNET_EALIAS;
+  if (!device_ok()) return LASNET_EHIP;
+  return enqueued(launch_balance(logits->dtype, logits->rows, logits->cols, k, arg(logits), lse, experts, counts, share, loss, workspace,
+                                 (hipStream_t)hip_stream));
+}
+
+int lasnet_choose_experts_backward(const lasnet_rows* logits, const float* lse, const int32_t* experts, const float* weights, int k,
+                                   const float* dweights, const int32_t* counts, const float* dloss, const lasnet_rows* dlogits, uint32_t flags,
+                                   void* hip_stream) {
+  CHECK(check_logits(logits, k));
+  CHECK(check_like(dlogits, logits));
+  if (flags & ~(uint32_t)LASNET_WEIGHTS_OF_ALL) return LASNET_EINVAL;
+  if (logits->rows > 0 && (!lse || (dweights && (!experts || !weights)))) return LASNET_EINVAL;
+  if (dloss && !counts) return LASNET_EINVAL;
+  if (!may_share(dlogits, logits) || clash({at(dlogits)}, {lse, experts, weights, dweights, counts, dloss})) return LASNET_EALIAS;
+  if (!device_ok()) return LASNET_EHIP;
+  if (logits->rows == 0) return LASNET_OK;
+  return enqueued(launch_choose_grad(logits->dtype, logits->rows, logits->cols, k, (flags & LASNET_WEIGHTS_OF_ALL) != 0, arg(logits), lse, experts,
+                                     weights, dweights, counts, dloss, arg(dlogits), (hipStream_t)hip_stream));
+}
+
+int lasnet_quantize_rows(const lasnet_rows* x, const int32_t* position, const int32_t* offsets, int k, int E, const lasnet_rows* out,
+                         uint8_t* scale, void* hip_stream) {
+  CHECK(check_rows(x, kFloats));
+  CHECK(check_rows(out, 1u << LASNET_E4M3));
+  if (position) CHECK(check_experts(k, E));
+  if (out->cols != x->cols || out->rows != x->rows * (position ? k : 1)) return LASNET_ESHAPE;
+  if (x->rows > 0 && (!scale || (position != nullptr) != (offsets != nullptr))) return LASNET_EINVAL;
+  if (clash({at(out), scale}, {at(x), position, offsets})) return LASNET_EALIAS;
+  if (!device_ok()) return LASNET_EHIP;
+  if (x->rows == 0) return LASNET_OK;
+  return enqueued(launch_quantize_rows(x->dtype, x->rows, k, E, x->cols, arg(x), position, offsets, arg(out), scale, (hipStream_t)hip_stream));
+}
+
+int lasnet_quantize_matrices(const void* W, int dtype, int E, int n, int k, void* out, uint8_t* scale, void* out_t, uint8_t* scale_t,
+                             void* hip_stream) {
+  if (dtype < 0 || dtype > 2) return LASNET_EINVAL;
+  if (!(kFloats >> dtype & 1)) return LASNET_EUNSUPPORTED;
+  CHECK(check_experts(1, E));
+  if (n <= 0 || k <= 0) return LASNET_ESHAPE;
+  if (n > kMaxCols || k > kMaxCols || (long long)E * ((n + 127) / 128) * ((k + 127) / 128) >= 1 << 24) return LASNET_EUNSUPPORTED;
+  if (!W || !out || !scale || (out_t != nullptr) != (scale_t != nullptr)) return LASNET_EINVAL;
+  if (clash({out, scale, out_t, scale_t}, {W})) return LASNET_EALIAS;
+  if (!device_ok()) return LASNET_EHIP;
+  return enqueued(launch_quantize_matrices(dtype, E, n, k, W, out, scale, out_t, scale_t, (hipStream_t)hip_stream));
+}
+
+int lasnet_block_product(const lasnet_rows* x, const uint8_t* scale, const int32_t* offsets, int E, const void* W, const void* wscale,
+                         int wscale_dtype, const lasnet_rows* out, uint32_t flags, void* hip_stream) {
+  CHECK(check_rows(x, 1u << LASNET_E4M3));
+  CHECK(check_rows(out, 1u << LASNET_BF16));
+  CHECK(check_experts(1, E));
+  if (out->rows != x->rows) return LASNET_ESHAPE;
+  if (!offsets || !W || !wscale || (x->rows > 0 && !scale) || (flags & ~(uint32_t)LASNET_POST_RELU)) return LASNET_EINVAL;
+  if (wscale_dtype != LASNET_E8M0 && wscale_dtype != LASNET_F32) return LASNET_EINVAL;
+  CHECK(check_tiles(x->rows, E, out->cols, 0));
+  if (clash({at(out)}, {at(x), scale, offsets, W, wscale})) return LASNET_EALIAS;
+  if (!device_ok()) return LASNET_EHIP;
+  if (x->rows == 0) return LASNET_OK;
+  return enqueued(launch_block_product(x->rows, E, out->cols, x->cols, arg(x), scale, offsets, W, wscale, wscale_dtype == LASNET_F32, arg(out),
+                                       (flags & LASNET_POST_RELU) != 0, (hipStream_t)hip_stream));
 }
 
 int lasnet_expert_product_dw(const lasnet_rows* dy, const lasnet_rows* x, const int32_t* offsets, int E, void* dW, int dw_dtype,

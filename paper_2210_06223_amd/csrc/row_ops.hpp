@@ -1,4 +1,4 @@
-// What the row operators (norm_rows.hip, route_rows.hip, expert_product.hip) share: rows as kernels see them, and pieces of rows.
+// What the row operators (norm_rows.hip, route_rows.hip, router.hip, quantize_rows.hip, expert_product.hip, block_product.hip) share: rows as kernels see them, and pieces of rows.
 #pragma once
 #include "common.hpp"
 
@@ -34,6 +34,20 @@ hipError_t launch_expert_product_dx(long long rows, int E, int n, int k, RowsArg
 hipError_t launch_expert_product_dw(long long rows, int E, int n, int k, RowsArg dy, RowsArg x, const int32_t* offsets, void* dW, bool f32,
                                     void* workspace, hipStream_t st);
 size_t product_dw_workspace_bytes(long long rows, int E, int n, int k);
+hipError_t launch_choose(int dtype, long long tokens, int E, int k, bool all, RowsArg logits, const uint8_t* mask, int32_t* experts, float* weights,
+                         float* lse, hipStream_t st);
+size_t balance_workspace_bytes(long long tokens, int E);
+hipError_t launch_balance(int dtype, long long tokens, int E, int k, RowsArg logits, const float* lse, const int32_t* experts, int32_t* counts,
+                          float* share, float* loss, void* workspace, hipStream_t st);
+hipError_t launch_choose_grad(int dtype, long long tokens, int E, int k, bool all, RowsArg logits, const float* lse, const int32_t* experts,
+                              const float* weights, const float* dweights, const int32_t* counts, const float* dloss, RowsArg dlogits,
+                              hipStream_t st);
+hipError_t launch_quantize_rows(int dtype, long long tokens, int k, int E, int cols, RowsArg x, const int32_t* position, const int32_t* offsets,
+                                RowsArg out, uint8_t* scale, hipStream_t st);
+hipError_t launch_quantize_matrices(int dtype, int E, int n, int k, const void* W, void* out, uint8_t* scale, void* out_t, uint8_t* scale_t,
+                                    hipStream_t st);
+hipError_t launch_block_product(long long rows, int E, int n, int k, RowsArg x, const uint8_t* scale, const int32_t* offsets, const void* W,
+                                const void* wscale, bool f32_scales, RowsArg out, bool relu, hipStream_t st);
 
 // Whether a call that writes so many bytes writes them past the caches: more than the 256 MB Infinity Cache would still hold when the next kernel reads them.
 // Dispatch of 268 MB and the sum that reads it: 156 us with ordinary stores, 116 past the caches; of 134 MB 56 and 61, of 67 MB 31 and 33.
@@ -129,6 +143,13 @@ __device__ __forceinline__ void store_piece(unsigned char* p, int n, uint4_t v) 
 #pragma unroll
   for (int i = 0; i < E::PER; ++i)
     if (i < n) E::put(p + i * E::BYTES, v[i * E::BYTES / 4] >> (8 * (i * E::BYTES % 4)));
+}
+
+// Exponent field (127 + e) of the scale 2^e of a row or block: a = M 2^E with 1 <= M < 2 needs e = E - 8 up to M = 1.75 (448 = 1.75 2^8), else E - 7.
+__device__ __forceinline__ int scale_byte(float a) {
+  const unsigned u = __float_as_uint(a);
+  const int e = (int)(u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u);
+  return e < 1 ? 1 : e;
 }
 
 template <int L = 64>
