@@ -8,6 +8,306 @@
 namespace lasnet {
 namespace {
 
+// ---- many tiles: 256 x 256 by eight waves, one workgroup a CU that goes from tile to tile without letting its loads run dry ----
+//
+// LDS holds two steps, each 32 KiB of either operand, and each wave's scales of them in slots of its own.  In step s a wave multiplies the I fragments of its eight blocks, a ring of four
+// read three blocks ahead, with the four J fragments it holds, and reads those of step s + 1 in block 7.  One barrier a step, before block 5, where all of I of step s has been read (and J, in block
+// 7 of the step before): step s + 1 has landed, and the loads of step s + 2 go where step s was; they have a step, some 1.6 us, to arrive.
+// FLOATS: the sum of a block of 128, four registers, is added to the whole kLag MFMAs later, when it is there.
+constexpr int kBlockStage = 65536, kBlockSlots = 2 * kScaleSlot, kLag = 2;
+constexpr int kBlockAside = 2 * kBlockStage + 8 * kBlockSlots, kBlockQuarter = 4 * (32768 + 8 * kScaleSlot);
+constexpr int kBlockTable = kBlockQuarter, kBlockLds = kBlockTable + 512;   // (behind what a quarter of a tile uses, and a stream)
+static_assert(kBlockAside + 8 * 64 <= kBlockTable && kBlockLds <= 160 * 1024, "a CU's LDS");
+constexpr int kStepLoads = 8 + kScaleLoads;
+
+// A workgroup's tile.
+struct BlockTile {
+  int expert, i0, j0, j_end;
+};
+
+// Where a wave's scales are: those of its rows of J (a byte each lane, kb apart) and that of its columns.
+template <int SCALES>
+struct ScaleStream {
+  unsigned long long x, w;
+  unsigned size_x;
+  __device__ __forceinline__ void start(const ProductArgs& a, int expert, int i0, int row0, int j_end) {
+    constexpr int WB = SCALES == FLOATS ? 4 : 1;
+    const int rows = j_end - row0 < 64 ? j_end - row0 : 64, nb = (a.ni + 127) >> 7, ib = i0 >> 7 < nb ? i0 >> 7 : nb - 1;
+    auto uniform = [](unsigned long long v) {
+      return (unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((unsigned)(v >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((unsigned)v);
+    };
+    x = uniform((unsigned long long)a.xblocks + (unsigned long long)((long long)row0 * a.kb));
+    w = uniform((unsigned long long)a.wblocks + (unsigned long long)(((long long)expert * nb + ib) * a.kb * WB));
+    size_x = __builtin_amdgcn_readfirstlane(rows > 0 ? (unsigned)((rows - 1) * a.kb + 1) : 0u);
+  }
+  // a step's, of a tile that has any left (else zeros: NaN times nothing would be NaN)
+  __device__ __forceinline__ void load(unsigned off_x, unsigned to, int left) {
+    constexpr int WB = SCALES == FLOATS ? 4 : 1;
+    const int there = ~((left - 1) >> 31);
+    scales_to_lds<true>(intx4{(int)(unsigned)x, (int)(unsigned)(x >> 32), (int)__builtin_amdgcn_readfirstlane(size_x & (unsigned)there), 0x00020000}, off_x, to);
+    scales_to_lds<SCALES == POWERS>(intx4{(int)(unsigned)w, (int)(unsigned)(w >> 32), (int)__builtin_amdgcn_readfirstlane((unsigned)(WB & there)), 0x00020000}, off_x & 0u, to + 256);
+    x += 1;
+    w += WB;
+  }
+};
+
+template <int SCALES>
+__global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
+  constexpr int KS = 128;
+  using S = Stage<false, 256, 8>;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char product_lds[];
+  const unsigned lds = (unsigned)(size_t)(lds_byte*)product_lds;
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int wi = wave % 2 * 128, wj = wave / 2 * 64;
+
+  // The experts' rows, one expert a lane (up to 63 of them; else they are looked up anew for each tile): first row, and tiles up to and with it.  In LDS (every wave writes
+  // the same), until a tile is looked up.
+  typedef __attribute__((address_space(3))) unsigned lds_dword;
+  int tiles_j;
+  const bool kept = a.E <= 63;
+  if (kept) {
+    const int lo = bound(a, lane < a.E ? lane : a.E), hi = __shfl(lo, lane < 63 ? lane + 1 : 63);
+    int upto = hi > lo ? (hi - lo + 255) / 256 : 0;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int u = __shfl_up(upto, d);
+      if (lane >= d) upto += u;
+    }
+    tiles_j = __builtin_amdgcn_readlane(upto, 63);
+    *(lds_dword*)(size_t)(lds + kBlockTable + lane * 8) = (unsigned)lo;
+    *(lds_dword*)(size_t)(lds + kBlockTable + lane * 8 + 4) = (unsigned)upto;
+  } else {
+    const int rest = (int)a.rows - __builtin_amdgcn_readfirstlane(bound(a, a.E));
+    tiles_j = row_tiles<256>(a) - (rest + 255) / 256;
+  }
+  // the rows that no expert has
+  for (long long r = bound(a, a.E) + (long long)blockIdx.x; r < a.rows; r += gridDim.x)
+    for (int c = (int)threadIdx.x * 8; c < a.ni * 2; c += 512 * 8) *(uint2_t*)(a.out.data + r * a.out.pitch + c) = uint2_t{0, 0};
+  // Workgroups are dealt to the eight XCDs in turn, each of which has an L2: an XCD takes consecutive tiles, its workgroups one each in turn.  A last round that would
+  // leave half of the XCD idle or more is cut into quarters of tiles.
+  const int xcd = (int)blockIdx.x & 7, slot = (int)blockIdx.x >> 3, stride = (int)gridDim.x >> 3;
+  const int total = tiles_j * a.tiles_i, chunk = (total + 7) / 8;
+  int end = total - xcd * chunk < chunk ? total - xcd * chunk : chunk;
+  const int rest = end > 0 && end % stride <= stride / 2 ? end % stride : 0;
+  end -= rest;
+
+  auto work = [&](int p) {                                    // the XCD's tile p
+    BlockTile w;
+    int ti, tj;
+    tile_at(xcd * chunk + p, a.tiles_i, tiles_j, ti, tj);
+    if (kept) {
+      const int lo = (int)read_dword(lds + kBlockTable + lane * 8), upto = (int)read_dword(lds + kBlockTable + lane * 8 + 4);
+      const int l = __ffsll((long long)__ballot(tj < upto)) - 1;
+      const int before = l ? __builtin_amdgcn_readlane(upto, l - 1) : 0;
+      w.expert = l;
+      w.j0 = __builtin_amdgcn_readlane(lo, l) + (tj - before) * 256;
+      w.j_end = __builtin_amdgcn_readlane(lo, l + 1);
+    } else {
+      int e = 0, j0 = 0, j1 = 0;
+      find_rows(a, 256, tj, e, j0, j1);
+      w.expert = __builtin_amdgcn_readfirstlane(e);
+      w.j0 = __builtin_amdgcn_readfirstlane(j0);
+      w.j_end = __builtin_amdgcn_readfirstlane(j1);
+    }
+    w.i0 = ti * 256;
+    return w;
+  };
+  const int steps = a.nk <= KS ? 2 : (a.nk + KS - 1) / KS;    // (two at least, so that loads are never further ahead than the next tile)
+
+  // ---- loads ----
+  const unsigned pitch_i = (unsigned)a.I.pitch, pitch_j = (unsigned)a.J.pitch, kb = (unsigned)a.nk;
+  struct Loads {
+    Feed<false> i, j;
+    ScaleStream<SCALES> s;
+  };
+  auto feed = [&](const BlockTile& w) {
+    Loads l;
+    l.i.start(a.I.data + (long long)w.expert * a.i_expert + (long long)w.i0 * a.I.pitch, a.ni - w.i0, 256, a.I.pitch, kb);
+    l.j.start(a.J.data + (long long)w.j0 * a.J.pitch, w.j_end - w.j0, 256, a.J.pitch, kb);
+    l.s.start(a, w.expert, w.i0 + wi, w.j0 + wj, w.j_end);
+    return l;
+  };
+  Loads l;                                                    // of the tile being loaded
+  int l_k = 0, after_k = 0;                                   // its k left, and that of the next (past the last tile: none)
+  // Those of the next tile wait in LDS, where a wave has a place for them: registers are short.
+  constexpr int WORDS = sizeof(Loads) / 4;
+  const unsigned aside = lds + kBlockAside + wave * 64;
+  union Words { Loads l; unsigned u[WORDS]; __device__ Words() {} };
+  auto put_aside = [&](const Loads& v) {
+    Words w;
+    w.l = v;
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) *(lds_dword*)(size_t)(aside + 4 * i) = w.u[i];
+  };
+  auto take_up = [&] {
+    Words w;
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) w.u[i] = __builtin_amdgcn_readfirstlane(read_dword(aside + 4 * i));
+    l = w.l;
+  };
+  const unsigned slots = lds + 2 * kBlockStage + wave * kBlockSlots;
+  unsigned l_to = lds, l_slot = slots;
+  auto nothing = [](int) {};
+  // A step's loads, between the eight parts of `meanwhile`.
+  auto issue = [&](auto meanwhile) {
+    meanwhile(0);
+    int at = lane;                                             // (made where it is used, not kept)
+    asm volatile("" : "+v"(at));
+    l.s.load((unsigned)(at * a.kb), l_slot, l_k);
+    const unsigned to = l_to + wave * 4096;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {                             // J, I
+      const intx4 rsrc = h ? l.i.rsrc(l_k, pitch_i) : l.j.rsrc(l_k, pitch_j);
+      // this lane's first piece of the operand's tile; the next lies a segment's rows further with bit 6 of its byte turned over (bit 2 of the lane), the other two likewise two
+      // segments further
+      const unsigned first = (unsigned)S::row(wave * 4, at) * (h ? pitch_i : pitch_j) + (unsigned)S::byte(wave * 4, at);
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const unsigned o = first + (s & 1 ? 64u - ((unsigned)at & 4) * 32 : 0u) + (unsigned)(s * 8) * (h ? pitch_i : pitch_j);
+        if (h || s) meanwhile(h * 4 + s);
+        __builtin_amdgcn_sched_barrier(0);
+        buffer_to_lds(rsrc, o, to + h * 32768 + s * 1024);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    l_to = 2 * lds + kBlockStage - l_to;
+    l_slot = 2 * slots + kScaleSlot - l_slot;
+    l.i.move(KS);
+    l.j.move(KS);
+    l_k -= KS;
+  };
+
+  // ---- products ----
+  floatx4 acc[8][4];
+  Fragment fi[4], fj[4];
+  unsigned sx[4], sw = 0, sw_next = 0, sw_before = 0;
+  floatx4 part[kLag];
+  const unsigned base = S::lane_base(0, lane);                // where a lane reads block 0 of an operand's first rows from
+  unsigned c = lds, c_slot = slots;                           // the step that fragments are read from
+  unsigned at_i = base + c + 32768 + wi * 128;
+  auto read_i = [&](int i) { S::fragment(at_i, i, fi[i % 4]); };
+  auto read_j = [&](int j) {
+    unsigned of = (unsigned)lane;
+    asm volatile("" : "+v"(of));
+    S::fragment(base + c + wj * 128, j, fj[j]);
+    sx[j] = read_dword(c_slot + (of & 15) * 4 + 64 * j);
+  };
+  auto add_part = [&](int m, unsigned w) {                    // that of the m-th MFMA of a step
+    const int i = m / 4, j = m % 4 ^ 2;
+    acc[i][j] = add_scaled(acc[i][j], part[m % kLag], w);
+  };
+  auto multiply = [&](int i, int p) {                         // the p-th MFMA of block i
+    const int j = p ^ 2, m = 4 * i + p;
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (SCALES == FLOATS) {
+      add_part(m >= kLag ? m - kLag : 32 + m - kLag, m >= kLag ? sw : sw_before);
+      part[m % kLag] = scaled_mfma<SCALES>(fi[i % 4].all, fj[j].all, floatx4{}, 0, sx[j]);
+    } else {
+      acc[i][j] = scaled_mfma<SCALES>(fi[i % 4].all, fj[j].all, acc[i][j], sw, sx[j]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  bool young = false;                                         // whether a tile's stores are younger than the loads waited for
+  auto step = [&] {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (i == 5) {
+        if (young)
+          counted_barrier<kTileStores>();
+        else
+          counted_barrier<0>();
+        young = false;
+        c = 2 * lds + kBlockStage - c;
+        c_slot = 2 * slots + kScaleSlot - c_slot;
+        at_i = base + c + 32768 + wi * 128;
+        asm volatile("" : "+v"(at_i));                         // (a sum in a register: reads add constants to it)
+        issue([&](int p) {
+          multiply(5 + p / 4, p % 4);
+          if (p == 0) read_i(0);
+          if (p == 4) read_i(1);
+          if (p == 5) sw_next = read_dword(c_slot + 256);
+        });
+      } else if (i != 6) {
+        read_i((i + 3) % 8);
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          multiply(i, p);
+          if (i == 7) read_j(p ^ 2);                           // (in place of the one that has been used up)
+        }
+      }
+    }
+    sw_before = sw;
+    sw = sw_next;
+  };
+
+  int round = 0;
+  if (slot < end) {
+    BlockTile w = work(slot);
+    l = feed(w);
+    l_k = a.nk;
+    issue(nothing);
+    issue(nothing);
+    counted_barrier<kStepLoads>();
+#pragma unroll
+    for (int j = 0; j < 4; ++j) read_j(j);
+    sw = read_dword(c_slot + 256);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) read_i(i);
+    while (true) {
+      ++round;
+      const bool more = round * stride + slot < end;
+      BlockTile next = w;
+      if (more) {
+        next = work(round * stride + slot);
+        put_aside(feed(next));
+      }
+      after_k = more ? a.nk : 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+      if constexpr (SCALES == FLOATS) {
+        sw_before = 0;
+#pragma unroll
+        for (int r = 0; r < kLag; ++r) part[r] = floatx4{0.f, 0.f, 0.f, 0.f};
+      }
+      for (int s = 0; s < steps; ++s) {
+        if (s == steps - 2) {                                  // (loads are two steps ahead)
+          if (more) take_up();
+          l_k = after_k;
+        }
+        step();
+      }
+      if constexpr (SCALES == FLOATS)
+#pragma unroll
+        for (int m = 32 - kLag; m < 32; ++m) add_part(m, sw_before);
+      store_big_tile<false, false>(a, a.out.data, TileWork{w.expert, w.i0, w.j0, w.j_end, 0, 0, 0}, wi, wj, lane, acc);
+      if (!more) break;
+      young = true;
+      w = next;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // (the last loads write to this workgroup's LDS)
+  }
+  for (int q = slot; q < 4 * rest; q += stride) {
+    const BlockTile v = work(end + q / 4);
+    const int i0 = v.i0 + (q & 1) * 128, j0 = v.j0 + (q >> 1 & 1) * 128;
+    if (i0 >= a.ni || j0 >= v.j_end) continue;
+    __syncthreads();
+    tile_product<true, false, false, false, false, 128, 128, 2, 4, 4, 1, SCALES>(a, product_lds, v.expert, i0, j0, v.j_end, 0, a.nk);
+  }
+}
+
+template <int SCALES>
+hipError_t go_block_stream(ProductArgs a, hipStream_t st) {
+  a.tiles_i = (a.ni + 255) / 256;
+  auto kernel = block_stream_kernel<SCALES>;
+  static std::atomic<unsigned long long> allowed{0};
+  const hipError_t e = allow_lds((const void*)kernel, kBlockLds, allowed);
+  if (e != hipSuccess) return e;
+  kernel<<<dim3(256), dim3(512), kBlockLds, st>>>(a);
+  return hipGetLastError();
+}
+
 template <int SCALES>
 hipError_t go_blocks(ProductArgs a, hipStream_t st) {
   if (whole<false, false>(a, 1, 256)) {
@@ -17,6 +317,9 @@ hipError_t go_blocks(ProductArgs a, hipStream_t st) {
       const long long mean = a.rows / BJ + blocks / 2, rows = mean > blocks ? mean : blocks;
       return rows * ((a.ni + BI - 1) / BI);
     };
+    if ((a.rows / 256 + blocks / 2) * ((a.ni + 255) / 256) >= 200 && a.nk >= 256 && a.ni % 4 == 0 && !(((unsigned long long)a.out.data | (unsigned long long)a.out.pitch) & 15) &&
+        a.out.pitch < (1ll << 31) / 256)
+      return go_block_stream<SCALES>(a, st);
     const int steps = a.nk / 128;
     if (steps >= 12 && tiles(64, 32) <= 256) return go_tile<true, false, false, false, false, 64, 32, 1, 2, 3, 4, SCALES>(a, st);
     if (steps >= 6 && tiles(64, 64) <= 256) return go_tile<true, false, false, false, false, 64, 64, 1, 4, 4, 2, SCALES>(a, st);

@@ -58,7 +58,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantizeRowsArgs a) 
       float top = 0.f;
 #pragma unroll
       for (int j = 0; j < El::PER; ++j) top = fmaxf(top, fabsf(f[j]));
-      top = wave_max<BL>(top);
+      top = lanes_max<BL>(top);
       const int byte = scale_byte(top);
       const float up = __uint_as_float((unsigned)(254 - byte) << 23);          // 2^-e, exact
       unsigned q[2];

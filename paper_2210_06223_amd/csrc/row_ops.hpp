@@ -1,5 +1,7 @@
 // What the row operators (norm_rows.hip, route_rows.hip, router.hip, quantize_rows.hip, expert_product.hip, block_product.hip) share: rows as kernels see them, and pieces of rows.
 #pragma once
+#include <type_traits>
+
 #include "common.hpp"
 
 namespace lasnet {
@@ -164,6 +166,38 @@ __device__ __forceinline__ float wave_max(float v) {
   for (int d = L / 2; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
   return v;
 }
+// The same without LDS: rotations within 16 lanes, then the rows of 16 and the halves of a wave change places (a result is the same bits in every lane; v: 32 bits of any kind).
+template <int L, class T, class Op>
+__device__ __forceinline__ T lanes_join(T v, Op op) {
+  static_assert(sizeof(T) == 4 && L >= 16 && L <= 64, "whole rows of lanes");
+  auto turned = [](T x, auto by) { return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x120 + decltype(by)::value, 0xf, 0xf, true)); };   // row_ror
+  v = op(v, turned(v, std::integral_constant<int, 8>{}));
+  v = op(v, turned(v, std::integral_constant<int, 4>{}));
+  v = op(v, turned(v, std::integral_constant<int, 2>{}));
+  v = op(v, turned(v, std::integral_constant<int, 1>{}));
+  if constexpr (L >= 32) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
+    v = op(__builtin_bit_cast(T, (unsigned)r[0]), __builtin_bit_cast(T, (unsigned)r[1]));
+  }
+  if constexpr (L >= 64) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
+    v = op(__builtin_bit_cast(T, (unsigned)r[0]), __builtin_bit_cast(T, (unsigned)r[1]));
+  }
+  return v;
+}
+template <int L> __device__ __forceinline__ float lanes_sum(float v) { return lanes_join<L>(v, [](float a, float b) { return a + b; }); }
+template <int L> __device__ __forceinline__ float lanes_max(float v) { return lanes_join<L>(v, [](float a, float b) { return fmaxf(a, b); }); }
+template <int L> __device__ __forceinline__ unsigned lanes_max(unsigned v) { return lanes_join<L>(v, [](unsigned a, unsigned b) { return a > b ? a : b; }); }
+template <int L> __device__ __forceinline__ unsigned lanes_min(unsigned v) { return lanes_join<L>(v, [](unsigned a, unsigned b) { return a < b ? a : b; }); }
+
+// e^x for x up to 88 to 2 units in the last place: 2^(x log2 e), what the product's rounding and the constant's lose put back to first order.  (0 below 2^-126.)
+__device__ __forceinline__ float exp_of(float x) {
+  constexpr float c = 1.44269502f, rest = 1.92596299e-8f, ln2 = 0.693147182f;
+  x = x < -200.f ? -200.f : x;                                 // (NaN passes)
+  const float t = x * c, r = __builtin_fmaf(x, rest, __builtin_fmaf(x, c, -t)), e = __builtin_amdgcn_exp2f(t);
+  return __builtin_fmaf(e, r * ln2, e);
+}
+
 // Sum (or maximum) over the L threads that share a row, the same bits in each.  at: L / 64 floats of LDS that nobody else writes before the next barrier but one.
 template <int L, bool MAX>
 __device__ __forceinline__ float row_join(float v, float* at) {
