@@ -51,6 +51,55 @@ struct ScaleStream {
   }
 };
 
+// The wave's 128 x 64 of a tile, rounded and stored through a buffer that ends with the tile's last row.  Of two blocks of 16 columns a row's four lanes hold four columns each, 8 bytes;
+// they change places (halves of the wave, then odd rows of 16 lanes with even ones), so that a lane has 8 of the 32 and a row's 64 bytes are stored as one piece.
+// Always kBlockStores stores (by hand: they are counted).  ni: a multiple of 8.
+constexpr int kBlockStores = 16;
+__device__ __forceinline__ void store_block_tile(const ProductArgs& a, const BlockTile& t, int wi, int wj, int lane, const floatx4 (&acc)[8][4]) {
+  asm volatile("" : "+v"(lane));
+  const unsigned pitch = (unsigned)a.out.pitch;
+  const int rows = t.j_end - t.j0 < 256 ? t.j_end - t.j0 : 256;
+  const unsigned long long first = (unsigned long long)(a.out.data + (long long)t.j0 * a.out.pitch + (long long)t.i0 * 2);
+  const intx4 to = {(int)(unsigned)first, (int)(unsigned)(first >> 32), (int)((unsigned)(rows - 1) * pitch + (unsigned)(a.ni - t.i0) * 2), 0x00020000};
+  auto each = [&](auto relu) {
+    const intx4 buffer = to;
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      const int col = wi + 16 * i + (lane >> 4) * 8;
+      unsigned o = t.i0 + col < a.ni ? (unsigned)(wj + (lane & 15)) * pitch + (unsigned)col * 2 : 0x80000000u;      // (beyond the buffer's 2^31 bytes: not stored)
+#pragma unroll
+      for (int j = 0; j < 4; ++j, o += 16 * pitch) {
+        unsigned v[2][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            float x = acc[i + h][j][2 * r], y = acc[i + h][j][2 * r + 1];
+            if constexpr (decltype(relu)::value) {
+              x = x < 0.f ? 0.f : x;                           // (NaN passes)
+              y = y < 0.f ? 0.f : y;
+            }
+            v[h][r] = bf16_pair(x, y);
+          }
+        uint4_t piece;
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const auto half = __builtin_amdgcn_permlane32_swap(v[0][r], v[1][r], false, false);
+          const auto row = __builtin_amdgcn_permlane16_swap(half[0], half[1], false, false);
+          piece[r] = row[0];
+          piece[2 + r] = row[1];
+        }
+        // (s_nop: the registers of a store of more than 8 bytes may not be written by the very next instruction)
+        asm volatile("buffer_store_dwordx4 %0, %1, %2, 0 offen\n\ts_nop 1" ::"v"(piece), "v"(o), "s"(buffer) : "memory");
+      }
+    }
+  };
+  if (a.relu)
+    each(std::true_type{});
+  else
+    each(std::false_type{});
+}
+
 template <int SCALES>
 __global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
   constexpr int KS = 128;
@@ -160,10 +209,11 @@ __global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
       const intx4 rsrc = h ? l.i.rsrc(l_k, pitch_i) : l.j.rsrc(l_k, pitch_j);
       // this lane's first piece of the operand's tile; the next lies a segment's rows further with bit 6 of its byte turned over (bit 2 of the lane), the other two likewise two
       // segments further
-      const unsigned first = (unsigned)S::row(wave * 4, at) * (h ? pitch_i : pitch_j) + (unsigned)S::byte(wave * 4, at);
+      const unsigned byte = (unsigned)S::byte(wave * 4, at), first = (unsigned)S::row(wave * 4, at) * (h ? pitch_i : pitch_j) + byte;
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
-        const unsigned o = first + (s & 1 ? 64u - ((unsigned)at & 4) * 32 : 0u) + (unsigned)(s * 8) * (h ? pitch_i : pitch_j);
+        unsigned o = first + (s & 1 ? 64u - ((unsigned)at & 4) * 32 : 0u) + (unsigned)(s * 8) * (h ? pitch_i : pitch_j);
+        if ((int)(byte ^ (s & 1 ? 64u : 0u)) >= l_k) o = 0xffffffffu;             // what is beyond the end of k lies inside the buffer
         if (h || s) meanwhile(h * 4 + s);
         __builtin_amdgcn_sched_barrier(0);
         buffer_to_lds(rsrc, o, to + h * 32768 + s * 1024);
@@ -213,7 +263,7 @@ __global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
     for (int i = 0; i < 8; ++i) {
       if (i == 5) {
         if (young)
-          counted_barrier<kTileStores>();
+          counted_barrier<kBlockStores>();
         else
           counted_barrier<0>();
         young = false;
@@ -281,7 +331,7 @@ __global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
       if constexpr (SCALES == FLOATS)
 #pragma unroll
         for (int m = 32 - kLag; m < 32; ++m) add_part(m, sw_before);
-      store_big_tile<false, false>(a, a.out.data, TileWork{w.expert, w.i0, w.j0, w.j_end, 0, 0, 0}, wi, wj, lane, acc);
+      store_block_tile(a, w, wi, wj, lane, acc);
       if (!more) break;
       young = true;
       w = next;
@@ -317,7 +367,7 @@ hipError_t go_blocks(ProductArgs a, hipStream_t st) {
       const long long mean = a.rows / BJ + blocks / 2, rows = mean > blocks ? mean : blocks;
       return rows * ((a.ni + BI - 1) / BI);
     };
-    if ((a.rows / 256 + blocks / 2) * ((a.ni + 255) / 256) >= 200 && a.nk >= 256 && a.ni % 4 == 0 && !(((unsigned long long)a.out.data | (unsigned long long)a.out.pitch) & 15) &&
+    if ((a.rows / 256 + blocks / 2) * ((a.ni + 255) / 256) >= 200 && a.nk >= 256 && a.ni % 8 == 0 && !(((unsigned long long)a.out.data | (unsigned long long)a.out.pitch) & 15) &&
         a.out.pitch < (1ll << 31) / 256)
       return go_block_stream<SCALES>(a, st);
     const int steps = a.nk / 128;
