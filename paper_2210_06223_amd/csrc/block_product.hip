@@ -14,7 +14,7 @@ namespace {
 // read three blocks ahead, with the four J fragments it holds, and reads those of step s + 1 in block 7.  One barrier a step, before block 5, where all of I of step s has been read (and J, in block
 // 7 of the step before): step s + 1 has landed, and the loads of step s + 2 go where step s was; they have a step, some 1.6 us, to arrive.
 // FLOATS: the sum of a block of 128, four registers, is added to the whole kLag MFMAs later, when it is there.
-constexpr int kBlockStage = 65536, kBlockSlots = 2 * kScaleSlot, kLag = 2;
+constexpr int kBlockStage = 65536, kBlockSlots = 2 * kScaleSlot, kLag = 4;
 constexpr int kBlockAside = 2 * kBlockStage + 8 * kBlockSlots, kBlockQuarter = 4 * (32768 + 8 * kScaleSlot);
 constexpr int kBlockTable = kBlockQuarter, kBlockLds = kBlockTable + 512;   // (behind what a quarter of a tile uses, and a stream)
 static_assert(kBlockAside + 8 * 64 <= kBlockTable && kBlockLds <= 160 * 1024, "a CU's LDS");
@@ -51,8 +51,9 @@ struct ScaleStream {
   }
 };
 
-// The wave's 128 x 64 of a tile, rounded and stored through a buffer that ends with the tile's last row.  Of two blocks of 16 columns a row's four lanes hold four columns each, 8 bytes;
-// they change places (halves of the wave, then odd rows of 16 lanes with even ones), so that a lane has 8 of the 32 and a row's 64 bytes are stored as one piece.
+// The wave's 64 x 128 of a tile, rounded and stored through a buffer that ends with the tile's last row.  Row 16 i + c of the wave's matrix rows in LDS is row 8 c + i in memory, and the rows of J
+// are the MFMA's first operand: so a lane has 8 columns next to each other of 16 rows, 16 lanes a row's 256 bytes, and a store is 4 rows of two whole lines each.  What a CU's 128 KiB take by
+// themselves goes by the lines that 16 lanes touch: 1.1 us so, 2.0 of 8 rows, 3.6 of 16 rows by 16 bytes, 7.1 of 16 by 8; 256 CUs at once, 5.3 (memory), 8.1 of 16 by 8.
 // Always kBlockStores stores (by hand: they are counted).  ni: a multiple of 8.
 constexpr int kBlockStores = 16;
 __device__ __forceinline__ void store_block_tile(const ProductArgs& a, const BlockTile& t, int wi, int wj, int lane, const floatx4 (&acc)[8][4]) {
@@ -63,36 +64,26 @@ __device__ __forceinline__ void store_block_tile(const ProductArgs& a, const Blo
   const intx4 to = {(int)(unsigned)first, (int)(unsigned)(first >> 32), (int)((unsigned)(rows - 1) * pitch + (unsigned)(a.ni - t.i0) * 2), 0x00020000};
   auto each = [&](auto relu) {
     const intx4 buffer = to;
+    const int col = wi + (lane & 15) * 8;
+    const bool there = t.i0 + col < a.ni;
+    unsigned o = (unsigned)(wj + (lane >> 4) * 4) * pitch + (unsigned)col * 2;
 #pragma unroll
-    for (int i = 0; i < 8; i += 2) {
-      const int col = wi + 16 * i + (lane >> 4) * 8;
-      unsigned o = t.i0 + col < a.ni ? (unsigned)(wj + (lane & 15)) * pitch + (unsigned)col * 2 : 0x80000000u;      // (beyond the buffer's 2^31 bytes: not stored)
+    for (int j = 0; j < 4; ++j, o += 12 * pitch)
 #pragma unroll
-      for (int j = 0; j < 4; ++j, o += 16 * pitch) {
-        unsigned v[2][2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            float x = acc[i + h][j][2 * r], y = acc[i + h][j][2 * r + 1];
-            if constexpr (decltype(relu)::value) {
-              x = x < 0.f ? 0.f : x;                           // (NaN passes)
-              y = y < 0.f ? 0.f : y;
-            }
-            v[h][r] = bf16_pair(x, y);
-          }
+      for (int r = 0; r < 4; ++r, o += pitch) {
         uint4_t piece;
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          const auto half = __builtin_amdgcn_permlane32_swap(v[0][r], v[1][r], false, false);
-          const auto row = __builtin_amdgcn_permlane16_swap(half[0], half[1], false, false);
-          piece[r] = row[0];
-          piece[2 + r] = row[1];
+        for (int q = 0; q < 4; ++q) {
+          float x = acc[2 * q][j][r], y = acc[2 * q + 1][j][r];
+          if constexpr (decltype(relu)::value) {
+            x = x < 0.f ? 0.f : x;                             // (NaN passes)
+            y = y < 0.f ? 0.f : y;
+          }
+          piece[q] = bf16_pair(x, y);
         }
-        // (s_nop: the registers of a store of more than 8 bytes may not be written by the very next instruction)
-        asm volatile("buffer_store_dwordx4 %0, %1, %2, 0 offen\n\ts_nop 1" ::"v"(piece), "v"(o), "s"(buffer) : "memory");
+        // (beyond the buffer's 2^31 bytes: not stored; s_nop: the registers of a store of more than 8 bytes may not be written by the very next instruction)
+        asm volatile("buffer_store_dwordx4 %0, %1, %2, 0 offen\n\ts_nop 1" ::"v"(piece), "v"(there ? o : 0x80000000u), "s"(buffer) : "memory");
       }
-    }
   };
   if (a.relu)
     each(std::true_type{});
@@ -209,10 +200,12 @@ __global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
       const intx4 rsrc = h ? l.i.rsrc(l_k, pitch_i) : l.j.rsrc(l_k, pitch_j);
       // this lane's first piece of the operand's tile; the next lies a segment's rows further with bit 6 of its byte turned over (bit 2 of the lane), the other two likewise two
       // segments further
-      const unsigned byte = (unsigned)S::byte(wave * 4, at), first = (unsigned)S::row(wave * 4, at) * (h ? pitch_i : pitch_j) + byte;
+      // (I: row 16 i + c of a wave's 128 in LDS is row 8 c + i in memory)
+      const unsigned byte = (unsigned)S::byte(wave * 4, at);
+      const unsigned first = (h ? (unsigned)(wave / 4 * 128 + wave % 4 * 2 + (at >> 3) * 8) * pitch_i : (unsigned)S::row(wave * 4, at) * pitch_j) + byte;
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
-        unsigned o = first + (s & 1 ? 64u - ((unsigned)at & 4) * 32 : 0u) + (unsigned)(s * 8) * (h ? pitch_i : pitch_j);
+        unsigned o = first + (s & 1 ? 64u - ((unsigned)at & 4) * 32 : 0u) + (h ? (unsigned)(s % 2 * 64 + s / 2) * pitch_i : (unsigned)(s * 8) * pitch_j);
         if ((int)(byte ^ (s & 1 ? 64u : 0u)) >= l_k) o = 0xffffffffu;             // what is beyond the end of k lies inside the buffer
         if (h || s) meanwhile(h * 4 + s);
         __builtin_amdgcn_sched_barrier(0);
@@ -230,30 +223,30 @@ __global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
   // ---- products ----
   floatx4 acc[8][4];
   Fragment fi[4], fj[4];
-  unsigned sx[4], sw = 0, sw_next = 0, sw_before = 0;
-  floatx4 part[kLag];
-  const unsigned base = S::lane_base(0, lane);                // where a lane reads block 0 of an operand's first rows from
+  unsigned sx[4], sw = 0, sw_next = 0;
+  unsigned sw_before = 0;
+  floatx4 part[kLag];                                         // FLOATS: the sums of a block of 128
   unsigned c = lds, c_slot = slots;                           // the step that fragments are read from
-  unsigned at_i = base + c + 32768 + wi * 128;
+  unsigned at_i = S::lane_base(0, lane) + c + 32768 + wi * 128;                           // where a lane reads block 0 of I's from (and of J's, wi and wj apart)
   auto read_i = [&](int i) { S::fragment(at_i, i, fi[i % 4]); };
   auto read_j = [&](int j) {
     unsigned of = (unsigned)lane;
     asm volatile("" : "+v"(of));
-    S::fragment(base + c + wj * 128, j, fj[j]);
+    S::fragment(at_i + (unsigned)((wj - wi) * 128 - 32768), j, fj[j]);
     sx[j] = read_dword(c_slot + (of & 15) * 4 + 64 * j);
   };
   auto add_part = [&](int m, unsigned w) {                    // that of the m-th MFMA of a step
-    const int i = m / 4, j = m % 4 ^ 2;
-    acc[i][j] = add_scaled(acc[i][j], part[m % kLag], w);
+    floatx4& sum = acc[m / 4][m % 4 ^ 2];
+    sum = add_scaled(sum, part[m % kLag], w);
   };
   auto multiply = [&](int i, int p) {                         // the p-th MFMA of block i
     const int j = p ^ 2, m = 4 * i + p;
     __builtin_amdgcn_sched_barrier(0);
     if constexpr (SCALES == FLOATS) {
       add_part(m >= kLag ? m - kLag : 32 + m - kLag, m >= kLag ? sw : sw_before);
-      part[m % kLag] = scaled_mfma<SCALES>(fi[i % 4].all, fj[j].all, floatx4{}, 0, sx[j]);
+      part[m % kLag] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fj[j].all, fi[i % 4].all, floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, (int)sx[j], 0, 0x7f7f7f7f);
     } else {
-      acc[i][j] = scaled_mfma<SCALES>(fi[i % 4].all, fj[j].all, acc[i][j], sw, sx[j]);
+      acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fj[j].all, fi[i % 4].all, acc[i][j], 0, 0, 0, (int)sx[j], 0, (int)sw);
     }
     __builtin_amdgcn_sched_barrier(0);
   };
@@ -267,9 +260,9 @@ __global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
         else
           counted_barrier<0>();
         young = false;
+        at_i += 2 * (lds - c) + kBlockStage;
         c = 2 * lds + kBlockStage - c;
         c_slot = 2 * slots + kScaleSlot - c_slot;
-        at_i = base + c + 32768 + wi * 128;
         asm volatile("" : "+v"(at_i));                         // (a sum in a register: reads add constants to it)
         issue([&](int p) {
           multiply(5 + p / 4, p % 4);
@@ -287,7 +280,7 @@ __global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
       }
     }
     sw_before = sw;
-    sw = sw_next;
+    sw = SCALES == FLOATS ? (unsigned)__builtin_amdgcn_readfirstlane(sw_next) : sw_next;
   };
 
   int round = 0;
@@ -301,6 +294,7 @@ __global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) read_j(j);
     sw = read_dword(c_slot + 256);
+    if constexpr (SCALES == FLOATS) sw = __builtin_amdgcn_readfirstlane(sw);
 #pragma unroll
     for (int i = 0; i < 3; ++i) read_i(i);
     while (true) {
