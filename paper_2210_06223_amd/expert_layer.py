@@ -8,6 +8,10 @@ Rows are tokens, or the pixels of a feature map [N,H,W,C] (N*H*W rows as they li
 serve() runs it with W1 in 8 bits (rows and weights e4m3, as lasnet_norm_rows and pack() write them) and W2 in bfloat16; train_step() in bfloat16, with all
 gradients.  Both take any number of rows, one included.  The router's small product, top-k and softmax are torch's.
 
+serve_blocks() and train_step_blocks() run every product but those of the weights' gradients in 8 bits, with a power-of-two scale for each 128 columns of a row and each block of 128 x 128
+of a matrix, and choose experts by the library, which also balances them: train_step_blocks() adds balance[0] * (E sum_e f_e P_e) + balance[1] * mean lse^2 to the loss, f the shares of
+the rows that the experts get and P their mean probabilities (lasnet_balance).  Tokens that a mask leaves out (padding; its rows have to be finite for the gradients' sake) are sent nowhere, count nowhere, and pass x through.
+
 The router reads the rows as the experts do: in 8 bits in serve(), in bfloat16 in train_step(), so where two logits are closer than that rounding the two may choose
 different experts for a row.
 
@@ -42,6 +46,10 @@ class ExpertLayer:
         w = self.W1.float()
         self.w1_scale = (w.abs().amax(-1) / 448.0).clamp_(min=1e-30).contiguous()
         self.W1_8 = (w / self.w1_scale[..., None]).to(torch.float8_e4m3fn)
+
+    def pack_blocks(self) -> None:
+        """W1 and W2 in 8 bits in blocks for serve_blocks(); to be called (again) after they have changed."""
+        self.blocks = B.lasnet_quantize_matrices(self.W1)[:2] + B.lasnet_quantize_matrices(self.W2)[:2]
 
     def choose(self, h: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
         """(experts int32 [rows,k], weights float32 [rows,k]) of normalised rows."""
@@ -84,6 +92,48 @@ class ExpertLayer:
         grads["x"], grads["g"] = B.lasnet_norm_rows_backward(dh.view(x.shape), s, self.g, rstd, dsum=dout)
         return out, grads
 
+    def serve_blocks(self, x: torch.Tensor, addend: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None) -> torch.Tensor:
+        h, _, s = B.lasnet_norm_rows(x, self.g, _EPS, residual=addend)
+        h = h.reshape(-1, self.C)
+        W1, s1, W2, s2 = self.blocks
+        experts, weights, _ = B.lasnet_choose_experts(h.float() @ self.R.t(), self.k, mask=mask)
+        offsets, _, position = B.lasnet_route(experts, self.E)
+        mid = B.lasnet_block_product(*B.lasnet_quantize_rows(h, position, offsets), offsets, W1, s1, flags=B.LASNET_POST_RELU)
+        y = B.lasnet_block_product(*B.lasnet_quantize_rows(mid), offsets, W2, s2)
+        return B.lasnet_combine_rows(y, position, weights=weights, base=x if s is None else s)
+
+    def train_step_blocks(self, x: torch.Tensor, dout: torch.Tensor, addend: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None,
+                          balance: Tuple[float, float] = (0.01, 0.001)) -> Tuple[torch.Tensor, Dict[str, torch.Tensor], torch.Tensor, torch.Tensor]:
+        """(out, gradients as train_step()'s, with those of the balance, loss [2], counts [E + 1]: the rows of each expert and the tokens that took part)."""
+        rstd = torch.empty(x.numel() // self.C, device=x.device)
+        h, _, s = B.lasnet_norm_rows(x, self.g, _EPS, residual=addend, rstd=rstd)
+        s, h = x if s is None else s, h.reshape(-1, self.C)
+        W1, s1, W1t, s1t = B.lasnet_quantize_matrices(self.W1, transposed=True)
+        W2, s2, W2t, s2t = B.lasnet_quantize_matrices(self.W2, transposed=True)
+        logits = h.float() @ self.R.t()
+        experts, weights, lse = B.lasnet_choose_experts(logits, self.k, mask=mask)
+        counts, _, loss = B.lasnet_balance(logits, lse, experts)
+        offsets, _, position = B.lasnet_route(experts, self.E)
+        rows, _ = B.lasnet_dispatch_rows(h, position, offsets)                                      # (the weights' gradient reads them as they are)
+        mid = B.lasnet_block_product(*B.lasnet_quantize_rows(h, position, offsets), offsets, W1, s1, flags=B.LASNET_POST_RELU)
+        y = B.lasnet_block_product(*B.lasnet_quantize_rows(mid), offsets, W2, s2)
+        out = B.lasnet_combine_rows(y, position, weights=weights, base=s)
+
+        dy, dweights = B.lasnet_combine_rows_backward(dout.reshape(-1, self.C), y, position, offsets, weights=weights)
+        grads = {"W2": B.lasnet_expert_product_dw(dy, mid, offsets, dtype=torch.float32)}
+        dmid = B.lasnet_block_product(*B.lasnet_quantize_rows(dy), offsets, W2t, s2t)
+        dmid.mul_(mid > 0)
+        grads["W1"] = B.lasnet_expert_product_dw(dmid, rows, offsets, dtype=torch.float32)
+        drows = B.lasnet_block_product(*B.lasnet_quantize_rows(dmid), offsets, W1t, s1t)
+        dloss = torch.empty(2, device=x.device)
+        for i in range(2):
+            dloss[i:i + 1].fill_(balance[i])                                                        # (a tensor made of numbers would wait for the stream)
+        dlogits = B.lasnet_choose_experts_backward(logits, lse, experts, weights, dweights=dweights, counts=counts, dloss=dloss)
+        grads["R"] = dlogits.t() @ h.float()
+        dh = B.lasnet_combine_rows(drows, position, base=(dlogits @ self.R).to(h.dtype))
+        grads["x"], grads["g"] = B.lasnet_norm_rows_backward(dh.view(x.shape), s, self.g, rstd, dsum=dout)
+        return out, grads, loss, counts
+
 
 def _timed(f, n: int = 20) -> float:
     for _ in range(3):
@@ -100,10 +150,13 @@ def _timed(f, n: int = 20) -> float:
 
 def main() -> None:
     layer = ExpertLayer(C=1024, M=1024, E=16, k=2)
+    layer.pack_blocks()
     for rows in (1, 16, 196, 25088):                # one token, a small batch, one 14x14 map, 128 of them
         x = torch.randn(rows, layer.C, device="cuda").bfloat16()
         dout = torch.randn_like(x)
-        print("%6d rows: serve %8.1f us, training step %8.1f us" % (rows, _timed(lambda: layer.serve(x)), _timed(lambda: layer.train_step(x, dout))), flush=True)
+        print("%6d rows: serve %8.1f us, training step %8.1f us; in blocks %8.1f us, %8.1f us" % (
+            rows, _timed(lambda: layer.serve(x)), _timed(lambda: layer.train_step(x, dout)), _timed(lambda: layer.serve_blocks(x)),
+            _timed(lambda: layer.train_step_blocks(x, dout))), flush=True)
 
 
 if __name__ == "__main__":

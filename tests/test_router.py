@@ -335,3 +335,39 @@ def test_tensors_that_are_refused(monkeypatch):
         B.lasnet_choose_experts_backward(l, lse, e, w, counts=dev(9, dtype=torch.int32), dloss=dev(3))
     with pytest.raises(ValueError, match="dweights"):
         B.lasnet_choose_experts_backward(l, lse, e, w, dweights=dev(4, 3))
+
+
+# (see test_row_arguments.py)
+F, H, Q = B.LASNET_F32, B.LASNET_BF16, B.LASNET_E4M3
+ENTRIES = {
+    "choose_experts": ([("logits", "ri", 8, 16, F), ("mask", "i"), 2, ("experts", "o"), ("weights", "o"), ("lse", "o"), 0, None], set()),
+    "balance": ([("logits", "ri", 30000, 16, F), ("lse", "i"), ("experts", "i"), 2, ("counts", "o"), ("share", "o"), ("loss", "o"), ("workspace", "o"), 1 << 24, None], set()),
+    "choose_experts_backward": ([("logits", "ri", 8, 16, F), ("lse", "i"), ("experts", "i"), ("weights", "i"), 2, ("dweights", "i"), ("counts", "i"), ("dloss", "i"),
+                                 ("dlogits", "ro", 8, 16, F), 0, None], {("dlogits", "logits")}),
+    "quantize_rows": ([("x", "ri", 8, 16, H), ("position", "i"), ("offsets", "i"), 2, 4, ("out", "ro", 16, 16, Q), ("scale", "o"), None], set()),
+    "quantize_matrices": ([("W", "i"), F, 2, 16, 32, ("out", "o"), ("scale", "o"), ("out_t", "o"), ("scale_t", "o"), None], set()),
+    "block_product": ([("x", "ri", 8, 16, Q), ("scale", "i"), ("offsets", "i"), 2, ("W", "i"), ("wscale", "i"), B.LASNET_E8M0, ("out", "ro", 8, 16, H), 0, None], set()),
+}
+
+
+def test_an_output_at_the_address_of_another_argument_is_refused(monkeypatch):
+    from tests import test_row_arguments
+    monkeypatch.setattr(test_row_arguments, "ENTRIES", ENTRIES)
+    test_row_arguments.test_an_output_at_the_address_of_another_argument_is_refused()
+
+
+def test_a_workspace_in_other_memory_is_refused(monkeypatch):
+    from tests.test_row_arguments import Recording
+    L, real = Recording(), torch.empty
+    monkeypatch.setattr(B, "_lib", L)
+    monkeypatch.setattr(B, "_marshal", B._AllThroughCtypes)
+    monkeypatch.setattr(B, "_stream", lambda s: 0)
+    monkeypatch.setattr(torch, "empty", lambda *a, **k: real(*a, **k).as_subclass(OnDevice))
+    l, lse, e = dev(6, 8), dev(6), dev(6, 2, dtype=torch.int32)
+    for kw in (dict(), dict(counts=dev(9, dtype=torch.int32), share=dev(8), loss=dev(2))):
+        for ws in (torch.zeros(4096, dtype=torch.uint8), torch.zeros(4096, dtype=torch.uint8, device="meta").as_subclass(OnDevice), dev(64, 128, dtype=torch.uint8)[:, ::2]):
+            with pytest.raises(ValueError, match="workspace"):
+                B.lasnet_balance(l, lse, e, workspace=ws, **kw)
+        assert not L.enqueued
+        B.lasnet_balance(l, lse, e, workspace=dev(4096, dtype=torch.uint8), **kw)
+        assert L.enqueued.pop() == "lasnet_balance"
