@@ -352,25 +352,43 @@ hipError_t go_block_stream(ProductArgs a, hipStream_t st) {
   return hipGetLastError();
 }
 
+template <int SCALES, int BI, int BJ, int WI, int WJ, int STAGES, int WK = 1>
+hipError_t go_block_tile(const ProductArgs& a, hipStream_t st) {
+  return go_tile<true, false, false, false, false, BI, BJ, WI, WJ, STAGES, WK, SCALES>(a, st);
+}
+
 template <int SCALES>
 hipError_t go_blocks(ProductArgs a, hipStream_t st) {
   if (whole<false, false>(a, 1, 256)) {
-    const long long blocks = a.E < a.rows ? a.E : a.rows, units = (blocks > (a.rows + 15) / 16 ? blocks : (a.rows + 15) / 16) * ((a.ni + 15) / 16);
-    if (a.rows <= 64 && units <= 384) return a.rows <= 16 || a.rows / a.E <= 8 ? go_few<true, 1, SCALES>(a, st) : go_few<true, 2, SCALES>(a, st);
+    const long long experts = a.E < a.rows ? a.E : a.rows, each = a.rows / experts;            // experts with rows at most, and rows of one
+    const int steps = (a.nk + 127) / 128;
+    // Tiles of BI x BJ, about (how the rows are spread is not known here).
     auto tiles = [&](int BI, int BJ) {
-      const long long mean = a.rows / BJ + blocks / 2, rows = mean > blocks ? mean : blocks;
+      const long long mean = a.rows / BJ + experts / 2, rows = mean > experts ? mean : experts;
       return rows * ((a.ni + BI - 1) / BI);
     };
-    if ((a.rows / 256 + blocks / 2) * ((a.ni + 255) / 256) >= 200 && a.nk >= 256 && a.ni % 8 == 0 && !(((unsigned long long)a.out.data | (unsigned long long)a.out.pitch) & 15) &&
+    // us, bytes as scales, three sets of inputs in turn.
+    // One workgroup a CU or little more, straight to registers: 1 row, 4096 x 4096 7.1 (64 x 16 by four groups of waves 8.5), 1024 x 2048 5.6 (6.5); 8 rows of 4 experts, 2048 x 4096 7.6
+    // (8.6).  Of more of them or shorter reductions the loads of a few rows do not pay: 4 rows, 8192 x 2048 9.3 (7.2), 8 of 8, 1024 x 1024 7.6 (5.5).
+    const long long units = tiles(16, 16);
+    if (a.rows <= 64 && units <= (steps >= 32 ? 512 : 384)) return a.rows <= 16 || each <= 8 ? go_few<true, 1, SCALES>(a, st) : go_few<true, 2, SCALES>(a, st);
+    // All at once, one workgroup a CU, the reduction shared by four groups of waves.  Rows of up to 16 an expert: 16 rows of 16 experts, 1024 x 2048 7.7 (64 x 32 8.1), 30 of 30,
+    // 512 x 1024 5.6 (6.2), 32 of 4, 2048 x 2048 6.9 (7.4); beyond, tiles of 32 and 64 rows: 128 rows, 4096 x 4096 11.6 (64 x 64 13.1, 128 x 64 16.9), 512 rows, 2048 x 2048 14.5 (9.6, 11.1).
+    if (steps >= 4 && each <= 16 && tiles(64, 16) <= 256) return go_block_tile<SCALES, 64, 16, 1, 1, 3, 4>(a, st);
+    if (steps >= 12 && tiles(64, 32) <= 256) return go_block_tile<SCALES, 64, 32, 1, 2, 3, 4>(a, st);
+    if (steps >= 6 && tiles(64, 64) <= 256) return go_block_tile<SCALES, 64, 64, 1, 4, 4, 2>(a, st);
+    // Few rows an expert, more workgroups, three a CU: 64 rows of 64 experts, 1024 x 1024 10.9 (128 x 64 11.9), 64 of 8, 2048 x 2048 9.1 (10.7); 256 of 16, 2048 x 4096 39.3 (35.5).
+    if (each <= 8 && tiles(64, 32) <= 1024) return go_block_tile<SCALES, 64, 32, 1, 2, 4>(a, st);
+    // 256 x 256 where there are enough for the chip, or more of 128 x 128 than run at once (two a CU): 8000 rows of 8 experts, 2048 x 1024 29 (128 x 128 40), 8192 of 2, 1024 x 4096
+    // 50 (67), 1024 x 512 14.8 (18.7), 3000 of 16, 2048 x 4096 62 (85).  Else not: 4096 rows, 2048 x 4096, 128 of them, 51 (41); 20000 of 2, 256 x 1024 19.9 (15.9).
+    const long long halves = (a.rows / 128 + experts / 2 + experts / 4) * ((a.ni + 127) / 128);           // (rows are hardly ever spread evenly)
+    if ((tiles(256, 256) >= 200 || halves > 512) && a.nk >= 256 && a.ni % 8 == 0 && !(((unsigned long long)a.out.data | (unsigned long long)a.out.pitch) & 15) &&
         a.out.pitch < (1ll << 31) / 256)
       return go_block_stream<SCALES>(a, st);
-    const int steps = a.nk / 128;
-    if (steps >= 12 && tiles(64, 32) <= 256) return go_tile<true, false, false, false, false, 64, 32, 1, 2, 3, 4, SCALES>(a, st);
-    if (steps >= 6 && tiles(64, 64) <= 256) return go_tile<true, false, false, false, false, 64, 64, 1, 4, 4, 2, SCALES>(a, st);
-    if (tiles(128, 64) <= 256) return go_tile<true, false, false, false, false, 128, 64, 2, 2, 3, 1, SCALES>(a, st);
-    if (tiles(128, 128) <= 240) return go_tile<true, false, false, false, false, 128, 128, 2, 4, 4, 1, SCALES>(a, st);
-    if (tiles(128, 64) <= 512) return go_tile<true, false, false, false, false, 128, 64, 2, 2, 3, 1, SCALES>(a, st);
-    return go_tile<true, false, false, false, false, 128, 128, 2, 2, 2, 1, SCALES>(a, st);
+    // 128 x 64 in three stages, two a CU, up to two rounds, else 128 x 128: 1000 rows of 8 experts, 1024 x 1024 8.1 (128 x 128 11.9), 1500 of 4, 1024 x 8192 30 (56); 4096 rows, 2048 x 1024
+    // 21.0 (17.9), 4001 of 8, 1000 x 528 13.7 (11.7).  128 x 128 by eight waves: 2048 rows, 2048 x 4096 26.6 (28.8 and 32.7), 2048 of 16, 4096 x 2048 55 (51, 57).
+    if (tiles(128, 64) <= 512) return go_block_tile<SCALES, 128, 64, 2, 2, 3>(a, st);
+    return go_block_tile<SCALES, 128, 128, 2, 2, 2>(a, st);
   }
   a.tiles_i = (a.ni + 127) / 128;
   const long long tiles = a.rows / 128 + a.E + 1;              // (each expert and the rest may have one tile that is not full)
