@@ -14,10 +14,11 @@ namespace {
 // read three blocks ahead, with the four J fragments it holds, and reads those of step s + 1 in block 7.  One barrier a step, before block 5, where all of I of step s has been read (and J, in block
 // 7 of the step before): step s + 1 has landed, and the loads of step s + 2 go where step s was; they have a step, some 1.6 us, to arrive.
 // FLOATS: the sum of a block of 128, four registers, is added to the whole kLag MFMAs later, when it is there.
-constexpr int kBlockStage = 65536, kBlockSlots = 2 * kScaleSlot, kLag = 4;
-constexpr int kBlockAside = 2 * kBlockStage + 8 * kBlockSlots, kBlockQuarter = 4 * (32768 + 8 * kScaleSlot);
-constexpr int kBlockTable = kBlockQuarter, kBlockLds = kBlockTable + 512;   // (behind what a quarter of a tile uses, and a stream)
-static_assert(kBlockAside + 8 * 64 <= kBlockTable && kBlockLds <= 160 * 1024, "a CU's LDS");
+constexpr int kBlockStage = 65536, kBlockSlots = 2 * kScaleSlot, kLag = 2;
+constexpr int kBlockQuarter = 4 * (32768 + 8 * kScaleSlot);    // what a quarter of a tile uses, and more than a stream
+constexpr int kBlockTiles = 512;                               // tiles that are looked up ahead
+constexpr int kBlockTable = kBlockQuarter, kBlockLds = kBlockTable + kBlockTiles * 16;
+static_assert(2 * kBlockStage + 8 * kBlockSlots <= kBlockTable && kBlockLds <= 160 * 1024, "a CU's LDS");
 constexpr int kStepLoads = 8 + kScaleLoads;
 
 // A workgroup's tile.
@@ -54,6 +55,8 @@ struct ScaleStream {
 // The wave's 64 x 128 of a tile, rounded and stored through a buffer that ends with the tile's last row.  Row 16 i + c of the wave's matrix rows in LDS is row 8 c + i in memory, and the rows of J
 // are the MFMA's first operand: so a lane has 8 columns next to each other of 16 rows, 16 lanes a row's 256 bytes, and a store is 4 rows of two whole lines each.  What a CU's 128 KiB take by
 // themselves goes by the lines that 16 lanes touch: 1.1 us so, 2.0 of 8 rows, 3.6 of 16 rows by 16 bytes, 7.1 of 16 by 8; 256 CUs at once, 5.3 (memory), 8.1 of 16 by 8.
+// While memory takes what all CUs store at once the loads behind wait (32768 rows, 4096 x 2048: without the stores 209 us, with half of them 235, with all 262): whole lines of a large output
+// go past the caches, 230 us (f32 scales 307 -> 261); 67 MB, which stay in them, 107 us, past them 110.
 // Always kBlockStores stores (by hand: they are counted).  ni: a multiple of 8.
 constexpr int kBlockStores = 16;
 __device__ __forceinline__ void store_block_tile(const ProductArgs& a, const BlockTile& t, int wi, int wj, int lane, const floatx4 (&acc)[8][4]) {
@@ -62,7 +65,7 @@ __device__ __forceinline__ void store_block_tile(const ProductArgs& a, const Blo
   const int rows = t.j_end - t.j0 < 256 ? t.j_end - t.j0 : 256;
   const unsigned long long first = (unsigned long long)(a.out.data + (long long)t.j0 * a.out.pitch + (long long)t.i0 * 2);
   const intx4 to = {(int)(unsigned)first, (int)(unsigned)(first >> 32), (int)((unsigned)(rows - 1) * pitch + (unsigned)(a.ni - t.i0) * 2), 0x00020000};
-  auto each = [&](auto relu) {
+  auto each = [&](auto relu, auto past) {
     const intx4 buffer = to;
     const int col = wi + (lane & 15) * 8;
     const bool there = t.i0 + col < a.ni;
@@ -82,13 +85,23 @@ __device__ __forceinline__ void store_block_tile(const ProductArgs& a, const Blo
           piece[q] = bf16_pair(x, y);
         }
         // (beyond the buffer's 2^31 bytes: not stored; s_nop: the registers of a store of more than 8 bytes may not be written by the very next instruction)
-        asm volatile("buffer_store_dwordx4 %0, %1, %2, 0 offen\n\ts_nop 1" ::"v"(piece), "v"(there ? o : 0x80000000u), "s"(buffer) : "memory");
+        const unsigned at = there ? o : 0x80000000u;
+        if constexpr (decltype(past)::value)
+          asm volatile("buffer_store_dwordx4 %0, %1, %2, 0 offen nt\n\ts_nop 1" ::"v"(piece), "v"(at), "s"(buffer) : "memory");
+        else
+          asm volatile("buffer_store_dwordx4 %0, %1, %2, 0 offen\n\ts_nop 1" ::"v"(piece), "v"(at), "s"(buffer) : "memory");
       }
   };
-  if (a.relu)
-    each(std::true_type{});
+  auto store = [&](auto past) {
+    if (a.relu)
+      each(std::true_type{}, past);
+    else
+      each(std::false_type{}, past);
+  };
+  if (a.past)
+    store(std::true_type{});
   else
-    each(std::false_type{});
+    store(std::false_type{});
 }
 
 template <int SCALES>
@@ -100,26 +113,7 @@ __global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int wi = wave % 2 * 128, wj = wave / 2 * 64;
 
-  // The experts' rows, one expert a lane (up to 63 of them; else they are looked up anew for each tile): first row, and tiles up to and with it.  In LDS (every wave writes
-  // the same), until a tile is looked up.
-  typedef __attribute__((address_space(3))) unsigned lds_dword;
-  int tiles_j;
-  const bool kept = a.E <= 63;
-  if (kept) {
-    const int lo = bound(a, lane < a.E ? lane : a.E), hi = __shfl(lo, lane < 63 ? lane + 1 : 63);
-    int upto = hi > lo ? (hi - lo + 255) / 256 : 0;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int u = __shfl_up(upto, d);
-      if (lane >= d) upto += u;
-    }
-    tiles_j = __builtin_amdgcn_readlane(upto, 63);
-    *(lds_dword*)(size_t)(lds + kBlockTable + lane * 8) = (unsigned)lo;
-    *(lds_dword*)(size_t)(lds + kBlockTable + lane * 8 + 4) = (unsigned)upto;
-  } else {
-    const int rest = (int)a.rows - __builtin_amdgcn_readfirstlane(bound(a, a.E));
-    tiles_j = row_tiles<256>(a) - (rest + 255) / 256;
-  }
+  const int unsent = (int)a.rows - __builtin_amdgcn_readfirstlane(bound(a, a.E)), tiles_j = row_tiles<256>(a) - (unsent + 255) / 256;
   // the rows that no expert has
   for (long long r = bound(a, a.E) + (long long)blockIdx.x; r < a.rows; r += gridDim.x)
     for (int c = (int)threadIdx.x * 8; c < a.ni * 2; c += 512 * 8) *(uint2_t*)(a.out.data + r * a.out.pitch + c) = uint2_t{0, 0};
@@ -131,26 +125,48 @@ __global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
   const int rest = end > 0 && end % stride <= stride / 2 ? end % stride : 0;
   end -= rest;
 
-  auto work = [&](int p) {                                    // the XCD's tile p
-    BlockTile w;
+  // The workgroup's tiles are looked up ahead of the loop, 64 at once, one a lane, and held in LDS.  (Every wave writes the same: none has to wait for another.)
+  typedef __attribute__((address_space(3))) unsigned lds_dword;
+  auto describe = [&](int p, bool there, unsigned at) {       // p: the lane's tile of the XCD's
     int ti, tj;
-    tile_at(xcd * chunk + p, a.tiles_i, tiles_j, ti, tj);
-    if (kept) {
-      const int lo = (int)read_dword(lds + kBlockTable + lane * 8), upto = (int)read_dword(lds + kBlockTable + lane * 8 + 4);
-      const int l = __ffsll((long long)__ballot(tj < upto)) - 1;
-      const int before = l ? __builtin_amdgcn_readlane(upto, l - 1) : 0;
-      w.expert = l;
-      w.j0 = __builtin_amdgcn_readlane(lo, l) + (tj - before) * 256;
-      w.j_end = __builtin_amdgcn_readlane(lo, l + 1);
-    } else {
-      int e = 0, j0 = 0, j1 = 0;
-      find_rows(a, 256, tj, e, j0, j1);
-      w.expert = __builtin_amdgcn_readfirstlane(e);
-      w.j0 = __builtin_amdgcn_readfirstlane(j0);
-      w.j_end = __builtin_amdgcn_readfirstlane(j1);
+    tile_at(there ? xcd * chunk + p : 0, a.tiles_i, tiles_j, ti, tj);
+    BlockTile w{0, ti * 256, 0, 0};
+    int before = 0;
+    for (int e0 = 0; e0 < a.E && before < tiles_j; e0 += 64) {
+      const int lo = e0 + lane < a.E ? bound(a, e0 + lane) : 0, hi = e0 + lane < a.E ? bound(a, e0 + lane + 1) : 0;
+      int upto = hi > lo ? (hi - lo + 255) / 256 : 0;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const int u = __shfl_up(upto, d);
+        if (lane >= d) upto += u;
+      }
+      int l = 0, last = 0;                                    // experts whose tiles come before tj, and how many tiles they have
+      for (int e = 0; e < 64; ++e) {
+        const int u = __builtin_amdgcn_readlane(upto, e);
+        if (before + u <= tj) {
+          ++l;
+          last = u;
+        }
+      }
+      const int jl = __shfl(lo, l & 63), jh = __shfl(hi, l & 63);
+      if (l < 64 && tj >= before) {
+        w.expert = e0 + l;
+        w.j0 = jl + (tj - before - last) * 256;
+        w.j_end = jh;
+      }
+      before += __builtin_amdgcn_readlane(upto, 63);
     }
-    w.i0 = ti * 256;
-    return w;
+    if (there) {
+      lds_dword* to = (lds_dword*)(size_t)(at + lane * 16);
+      to[0] = (unsigned)w.expert;
+      to[1] = (unsigned)w.i0;
+      to[2] = (unsigned)w.j0;
+      to[3] = (unsigned)w.j_end;
+    }
+  };
+  auto described = [&](unsigned at) {
+    auto word = [&](int i) { return __builtin_amdgcn_readfirstlane((int)read_dword(at + 4 * i)); };
+    return BlockTile{word(0), word(1), word(2), word(3)};
   };
   const int steps = a.nk <= KS ? 2 : (a.nk + KS - 1) / KS;    // (two at least, so that loads are never further ahead than the next tile)
 
@@ -168,23 +184,7 @@ __global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
     return l;
   };
   Loads l;                                                    // of the tile being loaded
-  int l_k = 0, after_k = 0;                                   // its k left, and that of the next (past the last tile: none)
-  // Those of the next tile wait in LDS, where a wave has a place for them: registers are short.
-  constexpr int WORDS = sizeof(Loads) / 4;
-  const unsigned aside = lds + kBlockAside + wave * 64;
-  union Words { Loads l; unsigned u[WORDS]; __device__ Words() {} };
-  auto put_aside = [&](const Loads& v) {
-    Words w;
-    w.l = v;
-#pragma unroll
-    for (int i = 0; i < WORDS; ++i) *(lds_dword*)(size_t)(aside + 4 * i) = w.u[i];
-  };
-  auto take_up = [&] {
-    Words w;
-#pragma unroll
-    for (int i = 0; i < WORDS; ++i) w.u[i] = __builtin_amdgcn_readfirstlane(read_dword(aside + 4 * i));
-    l = w.l;
-  };
+  int l_k = 0;                                                // its k left (past the last tile: none)
   const unsigned slots = lds + 2 * kBlockStage + wave * kBlockSlots;
   unsigned l_to = lds, l_slot = slots;
   auto nothing = [](int) {};
@@ -283,29 +283,25 @@ __global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
     sw = SCALES == FLOATS ? (unsigned)__builtin_amdgcn_readfirstlane(sw_next) : sw_next;
   };
 
-  int round = 0;
-  if (slot < end) {
-    BlockTile w = work(slot);
+  for (int p0 = slot; p0 < end; p0 += kBlockTiles * stride) { // (as many tiles as there is room for at a time)
+    const int left = (end - p0 + stride - 1) / stride, rounds = left < kBlockTiles ? left : kBlockTiles;
+    for (int r = 0; r < rounds; r += 64) describe(p0 + (r + lane) * stride, r + lane < rounds, lds + kBlockTable + r * 16);
+    BlockTile w = described(lds + kBlockTable);
     l = feed(w);
     l_k = a.nk;
     issue(nothing);
     issue(nothing);
     counted_barrier<kStepLoads>();
+    young = false;
 #pragma unroll
     for (int j = 0; j < 4; ++j) read_j(j);
     sw = read_dword(c_slot + 256);
     if constexpr (SCALES == FLOATS) sw = __builtin_amdgcn_readfirstlane(sw);
 #pragma unroll
     for (int i = 0; i < 3; ++i) read_i(i);
-    while (true) {
-      ++round;
-      const bool more = round * stride + slot < end;
-      BlockTile next = w;
-      if (more) {
-        next = work(round * stride + slot);
-        put_aside(feed(next));
-      }
-      after_k = more ? a.nk : 0;
+    unsigned at_next = lds + kBlockTable + 16;
+    for (int round = 0; round < rounds; ++round, at_next += 16) {
+      const bool more = round + 1 < rounds;
 #pragma unroll
       for (int i = 0; i < 8; ++i)
 #pragma unroll
@@ -317,8 +313,11 @@ __global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
       }
       for (int s = 0; s < steps; ++s) {
         if (s == steps - 2) {                                  // (loads are two steps ahead)
-          if (more) take_up();
-          l_k = after_k;
+          l_k = 0;
+          if (more) {
+            l = feed(described(at_next));
+            l_k = a.nk;
+          }
         }
         step();
       }
@@ -326,14 +325,16 @@ __global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
 #pragma unroll
         for (int m = 32 - kLag; m < 32; ++m) add_part(m, sw_before);
       store_block_tile(a, w, wi, wj, lane, acc);
-      if (!more) break;
       young = true;
-      w = next;
+      if (more) w = described(at_next);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // (the last loads write to this workgroup's LDS)
+    __syncthreads();
   }
-  for (int q = slot; q < 4 * rest; q += stride) {
-    const BlockTile v = work(end + q / 4);
+  const int quarters = 4 * rest;                              // two a workgroup at most
+  if (slot < quarters) describe(end + (slot + lane * stride) / 4, slot + lane * stride < quarters, lds + kBlockTable);
+  for (int q = slot; q < quarters; q += stride) {
+    const BlockTile v = described(lds + kBlockTable + q / stride * 16);
     const int i0 = v.i0 + (q & 1) * 128, j0 = v.j0 + (q >> 1 & 1) * 128;
     if (i0 >= a.ni || j0 >= v.j_end) continue;
     __syncthreads();
@@ -401,7 +402,7 @@ hipError_t go_blocks(ProductArgs a, hipStream_t st) {
 
 hipError_t launch_block_product(long long rows, int E, int n, int k, RowsArg x, const uint8_t* scale, const int32_t* offsets, const void* W,
                                 const void* wscale, bool f32_scales, RowsArg out, bool relu, hipStream_t st) {
-  const ProductArgs a{{(unsigned char*)W, k}, x, out, (long long)n * k, 0, offsets, nullptr, nullptr, rows, E, n, 0, k, 0, 0, 0, 0, relu, scale, wscale, (k + 127) / 128};
+  const ProductArgs a{{(unsigned char*)W, k}, x, out, (long long)n * k, 0, offsets, nullptr, nullptr, rows, E, n, 0, k, 0, 0, 0, 0, relu, scale, wscale, (k + 127) / 128, writes_past(rows * n * 2)};
   return f32_scales ? go_blocks<FLOATS>(a, st) : go_blocks<POWERS>(a, st);
 }
 

@@ -26,6 +26,7 @@ struct ProductArgs {
   const uint8_t* xblocks;          // scales of blocks of 128 (see SCALES): [rows][kb] bytes
   const void* wblocks;             // [E][(ni + 127) / 128][kb] bytes or floats
   int kb;                          // blocks of the reduction
+  bool past;                       // whether the output is written past the caches (see writes_past)
 };
 
 // Which scales 8-bit operands have (SCALES).  ROWS: one for each row of J and of I, applied where the sums are stored.  Blocks of 128 of the reduction, those of I shared by 128 of

@@ -264,3 +264,18 @@ def test_tensors_that_are_refused(monkeypatch):
         args = dict(x=x, scale=s, offsets=off, W=W, wscale=ws, **{}) | bad
         with pytest.raises(ValueError):
             B.lasnet_block_product(args["x"], args["scale"], args["offsets"], args["W"], args["wscale"], out=args.get("out"))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("floats", [False, True], ids=["e8m0", "f32"])
+def test_an_output_written_past_the_caches(floats):
+    """Large outputs are: 26000 x 4096 in bf16, 213 MB.  Whole numbers up to 256, which bf16 holds."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x, W = (torch.randint(-1, 2, s, generator=g, device="cuda").float() for s in ((26000, 256), (1, 4096, 256)))
+    scale = torch.full((26000, 2), 127, dtype=torch.uint8, device="cuda")
+    wscale = torch.ones(1, 32, 2, device="cuda") if floats else torch.full((1, 32, 2), 127, dtype=torch.uint8, device="cuda")
+    offsets = torch.tensor([0, 25990], dtype=torch.int32).cuda()
+    got = B.lasnet_block_product(x.to(E4M3), scale, offsets, W.to(E4M3), wscale)
+    want = x @ W[0].T
+    want[25990:] = 0
+    assert torch.equal(got.float(), want)
