@@ -15,10 +15,10 @@ namespace {
 // 7 of the step before): step s + 1 has landed, and the loads of step s + 2 go where step s was; they have a step, some 1.6 us, to arrive.
 // FLOATS: the sum of a block of 128, four registers, is added to the whole kLag MFMAs later, when it is there.
 constexpr int kBlockStage = 65536, kBlockSlots = 2 * kScaleSlot, kLag = 2;
-constexpr int kBlockQuarter = 4 * (32768 + 8 * kScaleSlot);    // what a quarter of a tile uses, and more than a stream
-constexpr int kBlockTiles = 512;                               // tiles that are looked up ahead
-constexpr int kBlockTable = kBlockQuarter, kBlockLds = kBlockTable + kBlockTiles * 16;
-static_assert(2 * kBlockStage + 8 * kBlockSlots <= kBlockTable && kBlockLds <= 160 * 1024, "a CU's LDS");
+constexpr int kBlockPieces = 6 * (24576 + 4 * kScaleSlot);      // what an eighth of a tile uses, and more than a quarter or a stream
+constexpr int kBlockTiles = 256;                               // tiles that are looked up ahead
+constexpr int kBlockTable = kBlockPieces, kBlockLds = kBlockTable + kBlockTiles * 16;
+static_assert(2 * kBlockStage + 8 * kBlockSlots <= kBlockTable && 4 * (32768 + 8 * kScaleSlot) <= kBlockTable && kBlockLds <= 160 * 1024, "a CU's LDS");
 constexpr int kStepLoads = 8 + kScaleLoads;
 
 // A workgroup's tile.
@@ -118,7 +118,7 @@ __global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
   for (long long r = bound(a, a.E) + (long long)blockIdx.x; r < a.rows; r += gridDim.x)
     for (int c = (int)threadIdx.x * 8; c < a.ni * 2; c += 512 * 8) *(uint2_t*)(a.out.data + r * a.out.pitch + c) = uint2_t{0, 0};
   // Workgroups are dealt to the eight XCDs in turn, each of which has an L2: an XCD takes consecutive tiles, its workgroups one each in turn.  A last round that would
-  // leave half of the XCD idle or more is cut into quarters of tiles.
+  // leave half of the XCD idle or more is cut into pieces of tiles.
   const int xcd = (int)blockIdx.x & 7, slot = (int)blockIdx.x >> 3, stride = (int)gridDim.x >> 3;
   const int total = tiles_j * a.tiles_i, chunk = (total + 7) / 8;
   int end = total - xcd * chunk < chunk ? total - xcd * chunk : chunk;
@@ -331,14 +331,19 @@ __global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // (the last loads write to this workgroup's LDS)
     __syncthreads();
   }
-  const int quarters = 4 * rest;                              // two a workgroup at most
-  if (slot < quarters) describe(end + (slot + lane * stride) / 4, slot + lane * stride < quarters, lds + kBlockTable);
-  for (int q = slot; q < quarters; q += stride) {
+  // What is left in pieces, two a workgroup at most.  Few: eighths of tiles, the reduction shared by two groups of waves (a step of a quarter is 0.6 us, whatever it does: 16640 rows, 2048 x
+  // 4096 129 -> 122 us, with scales in 32 bits 149 -> 137).
+  const int cut = 8 * rest <= stride ? 8 : 4, pieces = cut * rest;
+  if (slot < pieces) describe(end + (slot + lane * stride) / cut, slot + lane * stride < pieces, lds + kBlockTable);
+  for (int q = slot; q < pieces; q += stride) {
     const BlockTile v = described(lds + kBlockTable + q / stride * 16);
-    const int i0 = v.i0 + (q & 1) * 128, j0 = v.j0 + (q >> 1 & 1) * 128;
+    const int i0 = v.i0 + (cut == 8 ? (q & 3) * 64 : (q & 1) * 128), j0 = v.j0 + (cut == 8 ? q >> 2 & 1 : q >> 1 & 1) * 128;
     if (i0 >= a.ni || j0 >= v.j_end) continue;
     __syncthreads();
-    tile_product<true, false, false, false, false, 128, 128, 2, 4, 4, 1, SCALES>(a, product_lds, v.expert, i0, j0, v.j_end, 0, a.nk);
+    if (cut == 8)
+      tile_product<true, false, false, false, false, 64, 128, 1, 4, 3, 2, SCALES>(a, product_lds, v.expert, i0, j0, v.j_end, 0, a.nk);
+    else
+      tile_product<true, false, false, false, false, 128, 128, 2, 4, 4, 1, SCALES>(a, product_lds, v.expert, i0, j0, v.j_end, 0, a.nk);
   }
 }
 

@@ -66,7 +66,8 @@ SHAPES = [(1, 1, 1, 1), (1, 1, 64, 128), (1, 1, 300, 2048), (5, 3, 100, 130), (1
           (300, 8, 500, 520), (200, 3, 300, 1537), (256, 1, 256, 1792), (500, 2, 512, 1040), (1000, 3, 640, 384), (1500, 4, 1024, 272), (2500, 2, 768, 640), (700, 5, 130, 48),
           (90, 3, 257, 15), (129, 2, 129, 129), (2, 2, 4096, 4096), (30, 30, 512, 1024), (32, 4, 320, 2064), (64, 64, 512, 1024), (60, 5, 1000, 400),
           (1000, 1, 1032, 2320)]
-LARGE = [(9000, 3, 1536, 256), (8200, 2, 2048, 512), (14000, 70, 1024, 384), (13000, 4, 1160, 640), (9001, 2, 1540, 784), (8500, 2, 1602, 256), (9000, 3, 1536, 784), (9000, 2, 1544, 1040)]
+LARGE = [(9000, 3, 1536, 256), (8200, 2, 2048, 512), (14000, 70, 1024, 384), (13000, 4, 1160, 640), (9001, 2, 1540, 784), (8500, 2, 1602, 256), (9000, 3, 1536, 784), (9000, 2, 1544, 1040), (4652, 1, 4096, 400),
+         (5164, 1, 4096, 640)]
 
 
 @pytest.mark.gpu
