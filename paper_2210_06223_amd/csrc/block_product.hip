@@ -15,10 +15,9 @@ namespace {
 // 7 of the step before): step s + 1 has landed, and the loads of step s + 2 go where step s was; they have a step, some 1.6 us, to arrive.
 // FLOATS: the sum of a block of 128, four registers, is added to the whole kLag MFMAs later, when it is there.
 constexpr int kBlockStage = 65536, kBlockSlots = 2 * kScaleSlot, kLag = 2;
-constexpr int kBlockPieces = 6 * (24576 + 4 * kScaleSlot);      // what an eighth of a tile uses, and more than a quarter or a stream
-constexpr int kBlockTiles = 256;                               // tiles that are looked up ahead
-constexpr int kBlockTable = kBlockPieces, kBlockLds = kBlockTable + kBlockTiles * 16;
-static_assert(2 * kBlockStage + 8 * kBlockSlots <= kBlockTable && 4 * (32768 + 8 * kScaleSlot) <= kBlockTable && kBlockLds <= 160 * 1024, "a CU's LDS");
+constexpr int kBlockAside = 2 * kBlockStage + 8 * kBlockSlots, kBlockPieces = 6 * (24576 + 4 * kScaleSlot);
+constexpr int kBlockTable = kBlockPieces, kBlockLds = kBlockTable + 512;                 // (behind what an eighth of a tile uses, which is more than a quarter or a stream does)
+static_assert(kBlockAside + 8 * 64 <= kBlockTable && 4 * (32768 + 8 * kScaleSlot) <= kBlockTable && kBlockLds <= 160 * 1024, "a CU's LDS");
 constexpr int kStepLoads = 8 + kScaleLoads;
 
 // A workgroup's tile.
@@ -56,7 +55,7 @@ struct ScaleStream {
 // are the MFMA's first operand: so a lane has 8 columns next to each other of 16 rows, 16 lanes a row's 256 bytes, and a store is 4 rows of two whole lines each.  What a CU's 128 KiB take by
 // themselves goes by the lines that 16 lanes touch: 1.1 us so, 2.0 of 8 rows, 3.6 of 16 rows by 16 bytes, 7.1 of 16 by 8; 256 CUs at once, 5.3 (memory), 8.1 of 16 by 8.
 // While memory takes what all CUs store at once the loads behind wait (32768 rows, 4096 x 2048: without the stores 209 us, with half of them 235, with all 262): whole lines of a large output
-// go past the caches, 230 us (f32 scales 307 -> 261); 67 MB, which stay in them, 107 us, past them 110.
+// go past the caches, 230 us (f32 scales 307 -> 261; with inputs from memory 288 -> 275, 338 -> 332); 67 MB, which stay in them, 107 us, past them 110.
 // Always kBlockStores stores (by hand: they are counted).  ni: a multiple of 8.
 constexpr int kBlockStores = 16;
 __device__ __forceinline__ void store_block_tile(const ProductArgs& a, const BlockTile& t, int wi, int wj, int lane, const floatx4 (&acc)[8][4]) {
@@ -113,7 +112,26 @@ __global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int wi = wave % 2 * 128, wj = wave / 2 * 64;
 
-  const int unsent = (int)a.rows - __builtin_amdgcn_readfirstlane(bound(a, a.E)), tiles_j = row_tiles<256>(a) - (unsent + 255) / 256;
+  // The experts' rows, one expert a lane (up to 63 of them; else they are looked up anew for each tile): first row, and tiles up to and with it.  In LDS (every wave writes
+  // the same), until a tile is looked up.
+  typedef __attribute__((address_space(3))) unsigned lds_dword;
+  int tiles_j;
+  const bool kept = a.E <= 63;
+  if (kept) {
+    const int lo = bound(a, lane < a.E ? lane : a.E), hi = __shfl(lo, lane < 63 ? lane + 1 : 63);
+    int upto = hi > lo ? (hi - lo + 255) / 256 : 0;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int u = __shfl_up(upto, d);
+      if (lane >= d) upto += u;
+    }
+    tiles_j = __builtin_amdgcn_readlane(upto, 63);
+    *(lds_dword*)(size_t)(lds + kBlockTable + lane * 8) = (unsigned)lo;
+    *(lds_dword*)(size_t)(lds + kBlockTable + lane * 8 + 4) = (unsigned)upto;
+  } else {
+    const int rest = (int)a.rows - __builtin_amdgcn_readfirstlane(bound(a, a.E));
+    tiles_j = row_tiles<256>(a) - (rest + 255) / 256;
+  }
   // the rows that no expert has
   for (long long r = bound(a, a.E) + (long long)blockIdx.x; r < a.rows; r += gridDim.x)
     for (int c = (int)threadIdx.x * 8; c < a.ni * 2; c += 512 * 8) *(uint2_t*)(a.out.data + r * a.out.pitch + c) = uint2_t{0, 0};
@@ -125,48 +143,26 @@ __global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
   const int rest = end > 0 && end % stride <= stride / 2 ? end % stride : 0;
   end -= rest;
 
-  // The workgroup's tiles are looked up ahead of the loop, 64 at once, one a lane, and held in LDS.  (Every wave writes the same: none has to wait for another.)
-  typedef __attribute__((address_space(3))) unsigned lds_dword;
-  auto describe = [&](int p, bool there, unsigned at) {       // p: the lane's tile of the XCD's
+  auto work = [&](int p) {                                    // the XCD's tile p
+    BlockTile w;
     int ti, tj;
-    tile_at(there ? xcd * chunk + p : 0, a.tiles_i, tiles_j, ti, tj);
-    BlockTile w{0, ti * 256, 0, 0};
-    int before = 0;
-    for (int e0 = 0; e0 < a.E && before < tiles_j; e0 += 64) {
-      const int lo = e0 + lane < a.E ? bound(a, e0 + lane) : 0, hi = e0 + lane < a.E ? bound(a, e0 + lane + 1) : 0;
-      int upto = hi > lo ? (hi - lo + 255) / 256 : 0;
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const int u = __shfl_up(upto, d);
-        if (lane >= d) upto += u;
-      }
-      int l = 0, last = 0;                                    // experts whose tiles come before tj, and how many tiles they have
-      for (int e = 0; e < 64; ++e) {
-        const int u = __builtin_amdgcn_readlane(upto, e);
-        if (before + u <= tj) {
-          ++l;
-          last = u;
-        }
-      }
-      const int jl = __shfl(lo, l & 63), jh = __shfl(hi, l & 63);
-      if (l < 64 && tj >= before) {
-        w.expert = e0 + l;
-        w.j0 = jl + (tj - before - last) * 256;
-        w.j_end = jh;
-      }
-      before += __builtin_amdgcn_readlane(upto, 63);
+    tile_at(xcd * chunk + p, a.tiles_i, tiles_j, ti, tj);
+    if (kept) {
+      const int lo = (int)read_dword(lds + kBlockTable + lane * 8), upto = (int)read_dword(lds + kBlockTable + lane * 8 + 4);
+      const int l = __ffsll((long long)__ballot(tj < upto)) - 1;
+      const int before = l ? __builtin_amdgcn_readlane(upto, l - 1) : 0;
+      w.expert = l;
+      w.j0 = __builtin_amdgcn_readlane(lo, l) + (tj - before) * 256;
+      w.j_end = __builtin_amdgcn_readlane(lo, l + 1);
+    } else {
+      int e = 0, j0 = 0, j1 = 0;
+      find_rows(a, 256, tj, e, j0, j1);
+      w.expert = __builtin_amdgcn_readfirstlane(e);
+      w.j0 = __builtin_amdgcn_readfirstlane(j0);
+      w.j_end = __builtin_amdgcn_readfirstlane(j1);
     }
-    if (there) {
-      lds_dword* to = (lds_dword*)(size_t)(at + lane * 16);
-      to[0] = (unsigned)w.expert;
-      to[1] = (unsigned)w.i0;
-      to[2] = (unsigned)w.j0;
-      to[3] = (unsigned)w.j_end;
-    }
-  };
-  auto described = [&](unsigned at) {
-    auto word = [&](int i) { return __builtin_amdgcn_readfirstlane((int)read_dword(at + 4 * i)); };
-    return BlockTile{word(0), word(1), word(2), word(3)};
+    w.i0 = ti * 256;
+    return w;
   };
   const int steps = a.nk <= KS ? 2 : (a.nk + KS - 1) / KS;    // (two at least, so that loads are never further ahead than the next tile)
 
@@ -184,7 +180,23 @@ __global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
     return l;
   };
   Loads l;                                                    // of the tile being loaded
-  int l_k = 0;                                                // its k left (past the last tile: none)
+  int l_k = 0, after_k = 0;                                   // its k left, and that of the next (past the last tile: none)
+  // Those of the next tile wait in LDS, where a wave has a place for them: registers are short.
+  constexpr int WORDS = sizeof(Loads) / 4;
+  const unsigned aside = lds + kBlockAside + wave * 64;
+  union Words { Loads l; unsigned u[WORDS]; __device__ Words() {} };
+  auto put_aside = [&](const Loads& v) {
+    Words w;
+    w.l = v;
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) *(lds_dword*)(size_t)(aside + 4 * i) = w.u[i];
+  };
+  auto take_up = [&] {
+    Words w;
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) w.u[i] = __builtin_amdgcn_readfirstlane(read_dword(aside + 4 * i));
+    l = w.l;
+  };
   const unsigned slots = lds + 2 * kBlockStage + wave * kBlockSlots;
   unsigned l_to = lds, l_slot = slots;
   auto nothing = [](int) {};
@@ -283,25 +295,29 @@ __global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
     sw = SCALES == FLOATS ? (unsigned)__builtin_amdgcn_readfirstlane(sw_next) : sw_next;
   };
 
-  for (int p0 = slot; p0 < end; p0 += kBlockTiles * stride) { // (as many tiles as there is room for at a time)
-    const int left = (end - p0 + stride - 1) / stride, rounds = left < kBlockTiles ? left : kBlockTiles;
-    for (int r = 0; r < rounds; r += 64) describe(p0 + (r + lane) * stride, r + lane < rounds, lds + kBlockTable + r * 16);
-    BlockTile w = described(lds + kBlockTable);
+  int round = 0;
+  if (slot < end) {
+    BlockTile w = work(slot);
     l = feed(w);
     l_k = a.nk;
     issue(nothing);
     issue(nothing);
     counted_barrier<kStepLoads>();
-    young = false;
 #pragma unroll
     for (int j = 0; j < 4; ++j) read_j(j);
     sw = read_dword(c_slot + 256);
     if constexpr (SCALES == FLOATS) sw = __builtin_amdgcn_readfirstlane(sw);
 #pragma unroll
     for (int i = 0; i < 3; ++i) read_i(i);
-    unsigned at_next = lds + kBlockTable + 16;
-    for (int round = 0; round < rounds; ++round, at_next += 16) {
-      const bool more = round + 1 < rounds;
+    while (true) {
+      ++round;
+      const bool more = round * stride + slot < end;
+      BlockTile next = w;
+      if (more) {
+        next = work(round * stride + slot);
+        put_aside(feed(next));
+      }
+      after_k = more ? a.nk : 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i)
 #pragma unroll
@@ -313,11 +329,8 @@ __global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
       }
       for (int s = 0; s < steps; ++s) {
         if (s == steps - 2) {                                  // (loads are two steps ahead)
-          l_k = 0;
-          if (more) {
-            l = feed(described(at_next));
-            l_k = a.nk;
-          }
+          if (more) take_up();
+          l_k = after_k;
         }
         step();
       }
@@ -325,18 +338,17 @@ __global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
 #pragma unroll
         for (int m = 32 - kLag; m < 32; ++m) add_part(m, sw_before);
       store_block_tile(a, w, wi, wj, lane, acc);
+      if (!more) break;
       young = true;
-      if (more) w = described(at_next);
+      w = next;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // (the last loads write to this workgroup's LDS)
-    __syncthreads();
   }
   // What is left in pieces, two a workgroup at most.  Few: eighths of tiles, the reduction shared by two groups of waves (a step of a quarter is 0.6 us, whatever it does: 16640 rows, 2048 x
   // 4096 129 -> 122 us, with scales in 32 bits 149 -> 137).
-  const int cut = 8 * rest <= stride ? 8 : 4, pieces = cut * rest;
-  if (slot < pieces) describe(end + (slot + lane * stride) / cut, slot + lane * stride < pieces, lds + kBlockTable);
-  for (int q = slot; q < pieces; q += stride) {
-    const BlockTile v = described(lds + kBlockTable + q / stride * 16);
+  const int cut = 8 * rest <= stride ? 8 : 4;
+  for (int q = slot; q < cut * rest; q += stride) {
+    const BlockTile v = work(end + q / cut);
     const int i0 = v.i0 + (cut == 8 ? (q & 3) * 64 : (q & 1) * 128), j0 = v.j0 + (cut == 8 ? q >> 2 & 1 : q >> 1 & 1) * 128;
     if (i0 >= a.ni || j0 >= v.j_end) continue;
     __syncthreads();

@@ -43,6 +43,14 @@ __device__ __forceinline__ floatx4 scaled_mfma(intx8 i, intx8 j, floatx4 acc, un
   else
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(i, j, floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0x7f7f7f7f, 0, (int)x);
 }
+// The same with the rows of J as the first operand: four of them in a lane, of one row of I.
+template <int SCALES>
+__device__ __forceinline__ floatx4 turned_mfma(intx8 i, intx8 j, floatx4 acc, unsigned w, unsigned x) {
+  if constexpr (SCALES == POWERS)
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(j, i, acc, 0, 0, 0, (int)x, 0, (int)w);
+  else
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(j, i, floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, (int)x, 0, 0x7f7f7f7f);
+}
 __device__ __forceinline__ floatx4 add_scaled(floatx4 acc, floatx4 part, unsigned w) {
 #pragma unroll
   for (int r = 0; r < 4; ++r) acc[r] = __builtin_fmaf(part[r], __uint_as_float(w), acc[r]);
@@ -252,6 +260,40 @@ __device__ __forceinline__ void store_tile(const ProductArgs& a, unsigned char* 
       }
     });
   }
+}
+
+// The same where the rows of J were the first operand and row 16 i + c of the wave's rows of I in LDS is row 4 c + i in memory: a lane has four columns next to each other of 4 NJ rows,
+// 16 lanes a row's 128 bytes, a whole line.  (What a CU's 128 KiB of stores take goes by the lines that 16 lanes touch: 1.1 us of two whole ones, 7.1 of 16 by 8 bytes.)
+template <int NJ>
+__device__ __forceinline__ void store_turned_tile(const ProductArgs& a, int oi0, int oj0, int j_end, const floatx4 (&acc)[4][NJ]) {
+  const int lane = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+  const float floor = a.relu ? 0.f : -INFINITY;               // (NaN passes)
+  if (oj0 >= j_end || oi0 >= a.ni) return;
+  const bool fours = !((a.ni | (int)(a.out.pitch / 2)) & 3) && !((size_t)a.out.data & 3) && a.out.pitch < (1 << 22);
+  const int rows = j_end - oj0 < 16 * NJ ? j_end - oj0 : 16 * NJ, left = a.ni - oi0 - (lane & 15) * 4;
+  unsigned char* out = a.out.data + (long long)oj0 * a.out.pitch + (long long)oi0 * 2;
+  const product_rsrc_t to = product_rsrc(out, fours ? (unsigned)(rows - 1) * (unsigned)a.out.pitch + (unsigned)(a.ni - oi0) * 2 : 0u);
+#pragma unroll
+  for (int j = 0; j < NJ; ++j)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int row = 16 * j + (lane >> 4) * 4 + r;
+      float v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = acc[i][j][r] < floor ? floor : acc[i][j][r];
+      if (fours) {
+        __builtin_amdgcn_raw_buffer_store_b64(uint2_t{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])}, to, left > 0 ? row * (int)a.out.pitch + (lane & 15) * 8 : -1, 0, 0);
+      } else if (row < rows) {
+        unsigned char* o = out + (long long)row * a.out.pitch + (lane & 15) * 8;
+        if (left >= 4) {
+          *(uint2_any*)o = uint2_t{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (i < left) Elem<__bf16>::put(o + 2 * i, bf16_pair(v[i], 0.f));
+        }
+      }
+    }
 }
 
 // Any alignment and width: 128 x 128 of the output by 4 waves, 64 x 64 each; rows and weights through registers into two LDS stages, the next step's loads in
@@ -573,7 +615,7 @@ __device__ __forceinline__ void tile_product(const ProductArgs& a, unsigned char
   constexpr int STAGE = SI::BYTES + SJ::BYTES, LOADS = SI::SEGS + SJ::SEGS;
   constexpr int COUNTED = LOADS + (SCALES == ROWS ? 0 : kScaleLoads);
   static_assert(NI % 4 == 0, "a ring of four fragments");
-  static_assert(SCALES == ROWS || (FP8 && !IC && !JC && !RAGGED && BI / WI <= 128 && 128 % (BI / WI) == 0 && BJ / WJ <= 64), "a wave's columns in one block of 128, its rows in a load");
+  static_assert(SCALES == ROWS || (FP8 && !IC && !JC && !RAGGED && BI / WI == 64 && BJ / WJ <= 64), "a wave's columns in one block of 128, its rows in a load; see store_turned_tile");
   int lane = (int)threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) % (WI * WJ);
   const int group = WK > 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) / (WI * WJ) : 0;
@@ -598,7 +640,11 @@ __device__ __forceinline__ void tile_product(const ProductArgs& a, unsigned char
   const unsigned di = IC ? KS * pitch_i : 128, dj = JC ? KS * pitch_j : 128;
   unsigned off_i[SI::SEGS], off_j[SJ::SEGS];                  // of this lane's pieces from the tile
 #pragma unroll
-  for (int s = 0; s < SI::SEGS; ++s) off_i[s] = (unsigned)SI::row(wave * SI::SEGS + s, lane) * pitch_i + (unsigned)SI::byte(wave * SI::SEGS + s, lane);
+  for (int s = 0; s < SI::SEGS; ++s) {
+    int row = SI::row(wave * SI::SEGS + s, lane);
+    if constexpr (SCALES != ROWS) row = (row & ~63) + (row & 15) * 4 + (row >> 4 & 3);
+    off_i[s] = (unsigned)row * pitch_i + (unsigned)SI::byte(wave * SI::SEGS + s, lane);
+  }
 #pragma unroll
   for (int s = 0; s < SJ::SEGS; ++s) off_j[s] = (unsigned)SJ::row(wave * SJ::SEGS + s, lane) * pitch_j + (unsigned)SJ::byte(wave * SJ::SEGS + s, lane);
   int l_k = k_end - k0;                                       // what is left of k to load
@@ -675,10 +721,12 @@ __device__ __forceinline__ void tile_product(const ProductArgs& a, unsigned char
       if constexpr (SCALES == FLOATS) {
         constexpr int ALL = NI * NJ;
         const int at = i * NJ + j;
-        part[at % 4] = scaled_mfma<SCALES>(fi[i % 4].all, fj[S][j].all, floatx4{}, 0, sx[S][j]);
+        part[at % 4] = turned_mfma<SCALES>(fi[i % 4].all, fj[S][j].all, floatx4{}, 0, sx[S][j]);
         add_part(at >= LAG ? at - LAG : ALL + at - LAG, at >= LAG ? sw[S] : sw[S ^ 1]);
+      } else if constexpr (SCALES == POWERS) {
+        acc[i][j] = turned_mfma<SCALES>(fi[i % 4].all, fj[S][j].all, acc[i][j], sw[S], sx[S][j]);
       } else if constexpr (FP8) {
-        acc[i][j] = scaled_mfma<SCALES>(fi[i % 4].all, fj[S][j].all, acc[i][j], sw[S], sx[S][j]);
+        acc[i][j] = scaled_mfma<ROWS>(fi[i % 4].all, fj[S][j].all, acc[i][j], 0, 0);
       } else {
         acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fi[i % 4].h[h]), __builtin_bit_cast(bf16x8, fj[S][j].h[h]), acc[i][j], 0, 0, 0);
       }
@@ -746,7 +794,10 @@ __device__ __forceinline__ void tile_product(const ProductArgs& a, unsigned char
       for (int b = 0; b < NI * NJ; ++b) acc[b / NJ][b % NJ] += sums[g * GROUP + b * 64];
   }
   unsigned char* out = a.out.data + (RAGGED ? (long long)expert * a.out_expert : 0);
-  store_tile<FP8 && SCALES == ROWS, F32OUT>(a, out, expert, i0 + wi, j0 + wj, j_end, acc);
+  if constexpr (SCALES == ROWS)
+    store_tile<FP8, F32OUT>(a, out, expert, i0 + wi, j0 + wj, j_end, acc);
+  else
+    store_turned_tile(a, i0 + wi, j0 + wj, j_end, acc);
 }
 
 template <bool FP8, bool IC, bool JC, bool RAGGED, bool F32OUT, int BI, int BJ, int WI, int WJ, int STAGES, int WK = 1, int SCALES = ROWS>
