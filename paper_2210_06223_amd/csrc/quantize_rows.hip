@@ -28,12 +28,14 @@ struct QuantizeRowsArgs {
   int k, E, cols, pieces, blocks, width;    // width: lanes of a row, a power of two, whole blocks
 };
 
-// The n (0 < n) elements of a piece that a row has left, in 8 bits.
-template <class T>
+// The n (0 < n) elements of a piece that a row has left, in 8 bits.  PAST: past the caches.
+template <class T, bool PAST>
 __device__ __forceinline__ void store_eight(unsigned char* p, int n, const unsigned (&q)[2]) {
   constexpr int PER = Elem<T>::PER;
   if (n >= PER) {
-    if constexpr (PER == 8) *(uint2_any*)p = uint2_t{q[0], q[1]};
+    if constexpr (PER == 8 && PAST) __builtin_nontemporal_store(uint2_t{q[0], q[1]}, (uint2_any*)p);
+    else if constexpr (PER == 8) *(uint2_any*)p = uint2_t{q[0], q[1]};
+    else if constexpr (PAST) __builtin_nontemporal_store(q[0], (uint_any*)p);
     else *(uint_any*)p = q[0];
     return;
   }
@@ -42,7 +44,11 @@ __device__ __forceinline__ void store_eight(unsigned char* p, int n, const unsig
     if (j < n) p[j] = (uint8_t)(q[j / 4] >> (8 * (j % 4)));
 }
 
-template <class T>
+// Rows of 128 MB and more go past the caches: 16384 x 2048 bf16 to four experts each, 134 MB, 46 -> 34 us, and with the product that reads them next 217 -> 212 and 185 -> 186 us (64 and 16
+// experts, 1024 columns); of 67 MB 116 -> 122.
+bool rows_past(long long bytes) { return bytes >= 128 << 20; }
+
+template <class T, bool PAST>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantizeRowsArgs a) {
   using El = Elem<T>;
   constexpr int BL = 128 / El::PER;                            // lanes of a block
@@ -69,7 +75,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantizeRowsArgs a) 
       for (int j = 0; j < n; ++j) {
         const long long p = a.position ? a.position[t * a.k + j] : t;
         if (p < 0 || p >= slots) continue;
-        store_eight<T>(a.out.data + p * a.out.pitch + (size_t)c * El::PER, left, q);
+        store_eight<T, PAST>(a.out.data + p * a.out.pitch + (size_t)c * El::PER, left, q);
         if (c % BL == 0) a.scale[p * a.blocks + c / BL] = (uint8_t)byte;
       }
     }
@@ -80,7 +86,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantizeRowsArgs a) 
   const unsigned none[2] = {0, 0};
   for (long long p = sent + first; p < slots; p += stride)
     for (int c = lane; c < a.pieces; c += a.width) {
-      store_eight<T>(a.out.data + p * a.out.pitch + (size_t)c * El::PER, a.cols - c * El::PER, none);
+      store_eight<T, PAST>(a.out.data + p * a.out.pitch + (size_t)c * El::PER, a.cols - c * El::PER, none);
       if (c % BL == 0) a.scale[p * a.blocks + c / BL] = 127;
     }
 }
@@ -93,7 +99,7 @@ struct QuantizeMatricesArgs {
 };
 
 // A workgroup takes a block; thread (r, c) its rows 8 r .. 8 r + 7 and columns 8 c .. 8 c + 7.
-template <class T>
+template <class T, bool PAST>
 __global__ __launch_bounds__(256) void quantize_matrices_kernel(QuantizeMatricesArgs a) {
   using El = Elem<T>;
   constexpr int P = 8 / El::PER;                               // pieces of eight elements
@@ -129,7 +135,7 @@ __global__ __launch_bounds__(256) void quantize_matrices_kernel(QuantizeMatrices
   for (int u = 0; u < 8; ++u) {
     q[u][0] = four(f[u], up);
     q[u][1] = four(f[u] + 4, up);
-    if (i0 + u < a.n && left > 0) store_eight<__bf16>(a.out + first + (long long)u * a.k, left, q[u]);
+    if (i0 + u < a.n && left > 0) store_eight<__bf16, PAST>(a.out + first + (long long)u * a.k, left, q[u]);
   }
   if (!a.out_t) return;
   // 4 x 4 bytes turned: pairs of rows, then pairs of pairs
@@ -157,7 +163,7 @@ __global__ __launch_bounds__(256) void quantize_matrices_kernel(QuantizeMatrices
     if (cb * 128 + col >= a.k || left_t <= 0) continue;
     const uint2_t v = turned[col][c];
     const unsigned w[2] = {v[0], v[1]};
-    store_eight<__bf16>(a.out_t + (expert * a.k + cb * 128 + col) * a.n + ib * 128 + c * 8, left_t, w);
+    store_eight<__bf16, PAST>(a.out_t + (expert * a.k + cb * 128 + col) * a.n + ib * 128 + c * 8, left_t, w);
   }
 }
 
@@ -170,7 +176,9 @@ hipError_t launch_quantize_rows(int dtype, long long tokens, int k, int E, int c
   while (width < 256 && width < pieces) width *= 2;
   const QuantizeRowsArgs a{x, out, scale, position, offsets, tokens, k, E, cols, pieces, (cols + 127) / 128, width};
   const long long b = (tokens + 256 / width - 1) / (256 / width);
-  auto kernel = dtype == LASNET_F32 ? quantize_rows_kernel<float> : quantize_rows_kernel<__bf16>;
+  const bool past = rows_past((position ? tokens * k : tokens) * cols);
+  auto kernel = dtype == LASNET_F32 ? past ? quantize_rows_kernel<float, true> : quantize_rows_kernel<float, false>
+                                    : past ? quantize_rows_kernel<__bf16, true> : quantize_rows_kernel<__bf16, false>;
   kernel<<<dim3((unsigned)(b < 1 << 20 ? b : 1 << 20)), dim3(256), 0, st>>>(a);
   return hipGetLastError();
 }
@@ -178,7 +186,9 @@ hipError_t launch_quantize_rows(int dtype, long long tokens, int k, int E, int c
 hipError_t launch_quantize_matrices(int dtype, int E, int n, int k, const void* W, void* out, uint8_t* scale, void* out_t, uint8_t* scale_t,
                                     hipStream_t st) {
   const QuantizeMatricesArgs a{(const unsigned char*)W, (unsigned char*)out, (unsigned char*)out_t, scale, scale_t, n, k, (n + 127) / 128, (k + 127) / 128};
-  auto kernel = dtype == LASNET_F32 ? quantize_matrices_kernel<float> : quantize_matrices_kernel<__bf16>;
+  const bool past = writes_past((long long)E * n * k * (out_t ? 2 : 1));
+  auto kernel = dtype == LASNET_F32 ? past ? quantize_matrices_kernel<float, true> : quantize_matrices_kernel<float, false>
+                                    : past ? quantize_matrices_kernel<__bf16, true> : quantize_matrices_kernel<__bf16, false>;
   kernel<<<dim3((unsigned)((long long)E * a.nb * a.kb)), dim3(256), 0, st>>>(a);
   return hipGetLastError();
 }

@@ -13,16 +13,14 @@
 namespace lasnet {
 namespace {
 
-// ---- order: a key that is larger for what is chosen earlier.  NaN is above everything; 0: never chosen (-inf, and what is beyond the row). ----
+// ---- order: a key that is larger for what is chosen earlier.  NaN is above everything; -inf (and what is beyond the row) is never chosen: kNone and less. ----
+constexpr unsigned kNone = 0x007fffffu;
 __device__ __forceinline__ unsigned key_of(float v) {
-  const unsigned u = __float_as_uint(v + 0.f);                 // (-0 + 0 = 0: equal values are equal keys)
-  if (v != v) return 0xffffffffu;
-  return u == 0xff800000u ? 0u : u & 0x80000000u ? ~u : u | 0x80000000u;
+  unsigned u = __float_as_uint(v + 0.f);                       // (-0 + 0 = 0: equal values are equal keys)
+  u = v != v ? 0x7fffffffu : u;
+  return u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
 }
-__device__ __forceinline__ float value_of(unsigned key) {
-  if (key == 0xffffffffu) return __uint_as_float(0x7fc00000u);
-  return key == 0 ? -INFINITY : __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
-}
+__device__ __forceinline__ float value_of(unsigned key) { return __uint_as_float(key ^ (key & 0x80000000u ? 0x80000000u : 0xffffffffu)); }
 
 struct ChooseArgs {
   RowsArg logits;
@@ -80,7 +78,7 @@ __global__ __launch_bounds__(256) void choose_kernel(ChooseArgs a) {
   for (long long t = (long long)blockIdx.x * (256 / L) + threadIdx.x / L; t < a.tokens; t += (long long)gridDim.x * (256 / L)) {
     const bool there = !a.mask || a.mask[t];
     float v[C];
-    unsigned key[C], best = 0;
+    unsigned key[C];
     uint4_t piece[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -89,39 +87,41 @@ __global__ __launch_bounds__(256) void choose_kernel(ChooseArgs a) {
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int c = (lane * N + i) * El::PER;
+      const int c = (lane * N + i) * El::PER, left = there ? a.E - c : 0;
       float f[El::PER];
       El::widen(piece[i], f);
+      if (left < El::PER)
+#pragma unroll
+        for (int j = 0; j < El::PER; ++j) f[j] = j < left ? f[j] : -INFINITY;
 #pragma unroll
       for (int j = 0; j < El::PER; ++j) {
-        const bool in = there && c + j < a.E;
-        unsigned u = in ? key_of(f[j]) : 0u;
-        if (PACKED && u) u = (u & 0xffff0000u) | (0xffffu - (unsigned)(c + j));
-        v[i * El::PER + j] = in ? f[j] : -INFINITY;
-        key[i * El::PER + j] = u;
-        best = u > best ? u : best;
+        v[i * El::PER + j] = f[j];
+        key[i * El::PER + j] = PACKED ? (key_of(f[j]) & 0xffff0000u) | (0xffffu - (unsigned)(c + j)) : key_of(f[j]);
       }
     }
     // (a packed key's value: the 16 bits that the expert took were zeros of the value, so ones of a negative one's key)
-    auto value = [](unsigned m) { return value_of(!PACKED || m == 0 ? m : m >= 0xffff0000u ? 0xffffffffu : m & 0x80000000u ? m & 0xffff0000u : m | 0xffffu); };
-    unsigned m = lanes_max<L>(best);
-    const float top = value(m);
-    float sum = 0.f;
-    if (m) {
+    auto value = [](unsigned m) { return value_of(!PACKED ? m : m & 0x80000000u ? m & 0xffff0000u : m | 0xffffu); };
+    if constexpr (SORTED) sort_keys(key);
+    unsigned best = key[0];
+    if constexpr (!SORTED)
 #pragma unroll
-      for (int c = 0; c < C; ++c) sum += exp_of(v[c] - top);
-    }
+      for (int c = 1; c < C; ++c) best = key[c] > best ? key[c] : best;
+    unsigned m = lanes_max<L>(best);
+    const float top = value(m);                                // (of a token without a candidate: -inf)
+    // (NaN or +inf: nothing, which makes NaN of what follows; -inf less itself, too, which makes 0 of it)
+    float sum = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) sum += exp_below(v[c] - top);
     sum = lanes_sum<L>(sum);
     unsigned mine = 0;                                         // the key of this lane's choice
     int expert = -1;
     if constexpr (SORTED) {
-      sort_keys(key);
       auto take = [&](auto most) {                             // most: keys that a lane may give up
         constexpr int M = decltype(most)::value;
         for (int j = 0; j < a.k; ++j) {
           m = lanes_max<L>(key[0]);
           if (lane == j) mine = m;
-          const bool won = key[0] == m;                        // (0: nothing is left of any lane)
+          const bool won = key[0] == m;
 #pragma unroll
           for (int c = 0; c < M; ++c) {
             const unsigned next = c + 1 < C ? key[c + 1 < C ? c + 1 : c] : 0u, now = key[c];
@@ -132,7 +132,7 @@ __global__ __launch_bounds__(256) void choose_kernel(ChooseArgs a) {
       if (a.k <= 4 && C > 4) take(std::integral_constant<int, 4>{});
       else if (a.k <= 8 && C > 8) take(std::integral_constant<int, 8>{});
       else take(std::integral_constant<int, C>{});
-      if (mine) expert = (int)(0xffffu - (mine & 0xffffu));
+      if (mine > kNone) expert = (int)(0xffffu - (mine & 0xffffu));
     } else {
       for (int j = 0; j < a.k; ++j) {
         best = 0;
@@ -150,15 +150,15 @@ __global__ __launch_bounds__(256) void choose_kernel(ChooseArgs a) {
         }
         if (lane == j) {
           mine = m;
-          expert = m ? e : -1;
+          expert = m > kNone ? e : -1;
         }
         const int gone = e - lane * C;
 #pragma unroll
         for (int c = 0; c < C; ++c) key[c] = gone == c ? 0u : key[c];
       }
     }
-    const float lse = top + logf(sum);                         // (sum is 0 of a token without a candidate, with top = -inf)
-    float w = expert >= 0 ? exp_of(value(mine) - top) : 0.f;
+    const float lse = top + logf(sum);
+    float w = expert >= 0 ? exp_below(value(mine) - top) : 0.f;
     const float chosen = lanes_sum<L>(lane < a.k ? w : 0.f);
     w = expert >= 0 ? w / (a.all ? sum : chosen) : 0.f;
     if (lane < a.k) {

@@ -191,12 +191,13 @@ template <int L> __device__ __forceinline__ unsigned lanes_max(unsigned v) { ret
 template <int L> __device__ __forceinline__ unsigned lanes_min(unsigned v) { return lanes_join<L>(v, [](unsigned a, unsigned b) { return a < b ? a : b; }); }
 
 // e^x for x up to 88 to 2 units in the last place: 2^(x log2 e), what the product's rounding and the constant's lose put back to first order.  (0 below 2^-126.)
-__device__ __forceinline__ float exp_of(float x) {
+__device__ __forceinline__ float exp_within(float x) {
   constexpr float c = 1.44269502f, rest = 1.92596299e-8f, ln2 = 0.693147182f;
-  x = x < -200.f ? -200.f : x;                                 // (NaN passes)
   const float t = x * c, r = __builtin_fmaf(x, rest, __builtin_fmaf(x, c, -t)), e = __builtin_amdgcn_exp2f(t);
   return __builtin_fmaf(e, r * ln2, e);
 }
+__device__ __forceinline__ float exp_of(float x) { return exp_within(x < -200.f ? -200.f : x); }       // (NaN passes)
+__device__ __forceinline__ float exp_below(float x) { return exp_within(fmaxf(x, -200.f)); }           // (NaN: 0)
 
 // Sum (or maximum) over the L threads that share a row, the same bits in each.  at: L / 64 floats of LDS that nobody else writes before the next barrier but one.
 template <int L, bool MAX>
