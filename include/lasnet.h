@@ -452,7 +452,8 @@ LASNET_API int lasnet_balance(const lasnet_rows* logits, const float* lse, const
  *   dlogits[t][e] = p (c[e] - sum_e p c) + 2 dloss[1] lse p / T + (weights' part)          c[e] = dloss[0] E counts[e] / (k T^2)
  *   weights' part, s = sum_j weights[j] dweights[j]:  sum over the slots j with expert e of weights[j] (dweights[j] - s)
  *                  LASNET_WEIGHTS_OF_ALL:             sum over those slots of weights[j] dweights[j], minus p s
- * A slot with an expert outside [0, E) adds to s alone; an expert may be in several slots.  A token whose lse is -inf gets zeros.
+ * A slot with an expert outside [0, E) adds to s alone, one of weight 0 nothing (its dweights may be anything); an expert may be in several slots.  A token whose lse is -inf gets
+ * zeros.
  * dlogits: as logits, and may be the same rows.  In fp32, rounded once.  flags: as the forward call's.
  */
 LASNET_API int lasnet_choose_experts_backward(const lasnet_rows* logits, const float* lse, const int32_t* experts, const float* weights, int k,
@@ -460,7 +461,8 @@ LASNET_API int lasnet_choose_experts_backward(const lasnet_rows* logits, const f
                                               uint32_t flags, void* hip_stream);
 
 /*
- * Rows in 8 bits with a scale for each 128 columns:  out = E4M3(x / 2^e), scale = e + 127: the least e, at least -126, with max |x| over the block <= 448 * 2^e (NaN aside).
+ * Rows in 8 bits with a scale for each 128 columns:  out = E4M3(x / 2^e), scale = e + 127: the least e, at least -126, with max |x| over the block <= 448 * 2^e, NaN
+ * aside; an infinity becomes NaN, in a block of 2^120.
  * x: tokens rows, F32 or BF16.  position NULL: out has as many rows (offsets NULL, k and E not looked at).  Else they are laid out by expert on the way, as lasnet_dispatch_rows
  * would (position [tokens * k], offsets [E + 1]): out has tokens * k rows, those from offsets[E] on are zeros with scales of 127.
  * scale: [out.rows][(cols + 127) / 128] bytes, dense.

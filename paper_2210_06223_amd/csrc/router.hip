@@ -512,6 +512,7 @@ __global__ __launch_bounds__(256) void choose_grad_kernel(ChooseGradArgs a) {
       k.expert = a.experts[t * a.k + lane];
     }
   };
+  auto weighed = [](float w, float dw) { return w == 0.f ? 0.f : dw; };         // (of a slot without weight: nothing, also of NaN)
   const long long stride = (long long)gridDim.x * (256 / L);
   long long t = (long long)blockIdx.x * (256 / L) + threadIdx.x / L;
   if (t >= a.tokens) return;
@@ -519,13 +520,13 @@ __global__ __launch_bounds__(256) void choose_grad_kernel(ChooseGradArgs a) {
   fetch(t, now);
   for (; t < a.tokens; t += stride, now = next) {
     fetch(t + stride < a.tokens ? t + stride : t, next);
-    const float lse = now.lse, w = now.w, dw = now.dw;
+    const float lse = now.lse, w = now.w, dw = weighed(w, now.dw);
     const bool there = lse != -INFINITY, own = a.dweights && there;
     const int expert = now.expert;
     float pull = 0.f;
     if (own) {
       pull = w * dw;
-      for (int j = lane + L; j < a.k; j += L) pull += a.weights[t * a.k + j] * a.dweights[t * a.k + j];
+      for (int j = lane + L; j < a.k; j += L) pull += a.weights[t * a.k + j] * weighed(a.weights[t * a.k + j], a.dweights[t * a.k + j]);
       pull = lanes_sum<L>(pull);
     }
     float d[N][El::PER], dot = 0.f;
@@ -562,7 +563,8 @@ __global__ __launch_bounds__(256) void choose_grad_kernel(ChooseGradArgs a) {
         fence();
         for (int j = 0; j < a.k; ++j) {                        // by the group's first lane, slot after slot
           const int e = a.experts[t * a.k + j];
-          if (lane == 0 && e >= 0 && e < a.E) row[e] += part(a.weights[t * a.k + j], a.dweights[t * a.k + j]);
+          const float v = a.weights[t * a.k + j], dv = weighed(v, a.dweights[t * a.k + j]);
+          if (lane == 0 && e >= 0 && e < a.E) row[e] += part(v, dv);
           fence();
         }
       }

@@ -11,7 +11,7 @@ import pytest
 import torch
 
 from paper_2210_06223_amd import binding as B
-from tests.test_call_streams import OnDevice, dev
+from tests.test_call_streams import CURRENT, SIDE, OnDevice, dev, made  # noqa: F401
 from tests.test_row_operators import BF16, F32, HALF, U, close, f64, gen, rand
 
 SHAPES = [(1, 1, 1), (1, 2, 1), (3, 5, 5), (7, 60, 2), (130, 64, 4), (65, 129, 16), (33, 256, 8), (9, 256, 33), (17, 513, 33), (5, 1030, 64), (3, 2500, 8), (3, 4096, 64), (1000, 8, 2),
@@ -227,6 +227,24 @@ def test_gradient_against_differences(of_all):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("of_all", [False, True], ids=["chosen", "all"])
+def test_slots_without_weight_add_nothing(of_all):
+    """What a slot of expert -1 is given (a token with fewer candidates than slots: nothing ever writes there) reaches no gradient, NaN included."""
+    for tokens, E, k in ((7, 5, 8), (3, 40, 20), (4, 20, 33)):
+        g = gen(tokens)
+        l = rand(g, tokens, E)
+        l[0, 2:] = -math.inf
+        l[2] = -math.inf
+        flags = B.LASNET_WEIGHTS_OF_ALL if of_all else 0
+        experts, weights, lse = B.lasnet_choose_experts(l, k, flags=flags)
+        dw = rand(g, tokens, k)
+        want = B.lasnet_choose_experts_backward(l, lse, experts, weights, dweights=dw.masked_fill(experts < 0, 0.0), flags=flags)
+        assert torch.isfinite(want).all() and bool((experts < 0).any())
+        for other in (math.nan, math.inf):
+            assert torch.equal(B.lasnet_choose_experts_backward(l, lse, experts, weights, dweights=dw.masked_fill(experts < 0, other), flags=flags), want)
+
+
+@pytest.mark.gpu
 def test_captured_and_on_another_stream():
     """Two graphs, each with a workspace of its own, replayed in turn on new inputs with other work between; and the calls on a stream of their own."""
     tokens, E, k = 3000, 40, 4
@@ -371,3 +389,43 @@ def test_a_workspace_in_other_memory_is_refused(monkeypatch):
         assert not L.enqueued
         B.lasnet_balance(l, lse, e, workspace=dev(4096, dtype=torch.uint8), **kw)
         assert L.enqueued.pop() == "lasnet_balance"
+
+
+def calls(k):
+    """name, the call, how many outputs and workspaces it makes"""
+    l, lse, e, w = dev(6, 8), dev(6), dev(6, 2, dtype=torch.int32), dev(6, 2)
+    yield "choose", lambda: B.lasnet_choose_experts(l, 2, **k), 3, 0
+    yield "balance", lambda: B.lasnet_balance(l, lse, e, **k), 3, 1
+    yield "backward", lambda: B.lasnet_choose_experts_backward(l, lse, e, w, dweights=w, **k), 1, 0
+
+
+@pytest.mark.parametrize("which", range(3))
+def test_what_a_call_makes_is_memory_of_its_stream(which, made):
+    for given in (None, CURRENT, SIDE):
+        name, run, outputs, workspaces = list(calls({} if given is None else {"stream": given}))[which]
+        made.clear()
+        run()
+        assert [s for _, s in made] == [given or CURRENT] * (outputs + workspaces), name
+        assert [getattr(t, "used_on", []) for t, _ in made] == [[CURRENT] if given is SIDE else []] * outputs + [[]] * workspaces, name
+
+
+@pytest.mark.gpu
+def test_offsets_past_32_bits():
+    """Of bytes and of elements: 1.1 M tokens of 4096 experts in fp32, the last of which are compared with the same tokens by themselves."""
+    tokens, E, k, last = 1100000, 4096, 4, 257
+    l = torch.empty(tokens, E, device="cuda")
+    l[:] = torch.randn(1000, E, generator=gen(1)).cuda().repeat(1100, 1)
+    l[-last:] = torch.randn(last, E, generator=gen(2)).cuda()
+    experts, weights, lse = B.lasnet_choose_experts(l, k)
+    few = B.lasnet_choose_experts(l[-last:].clone(), k)
+    for a, b in zip((experts, weights, lse), few):
+        assert torch.equal(a[-last:], b) and torch.equal(a[:1000], a[1000:2000])
+    counts, share, loss = B.lasnet_balance(l, lse, experts)
+    assert int(counts[E]) == tokens and int(counts[:E].sum()) == tokens * k
+    rest = torch.bincount(experts.flatten().long(), minlength=E).int()
+    assert torch.equal(counts[:E], rest) and abs(float(share.double().sum()) - 1) < E * U
+    dw = torch.randn(tokens, k, generator=gen(3)).cuda()
+    d = B.lasnet_choose_experts_backward(l, lse, experts, weights, dweights=dw, dlogits=l)
+    # (in place: what it read is gone)
+    assert torch.equal(d[-last:], B.lasnet_choose_experts_backward(torch.randn(last, E, generator=gen(2)).cuda(), lse[-last:].clone(), experts[-last:].clone(), weights[-last:].clone(),
+                                                                   dweights=dw[-last:].clone()))
