@@ -12,7 +12,7 @@ import torch
 
 from paper_2210_06223_amd import binding as B
 from paper_2210_06223_amd import build
-from tests.test_call_streams import dev
+from tests.test_call_streams import CURRENT, SIDE, dev, made  # noqa: F401
 from tests.test_router import call, on_device, rows
 from tests.test_row_operators import BF16, E4M3, F32, HALF, U, close, f64, gen, rand
 
@@ -280,3 +280,54 @@ def test_an_output_written_past_the_caches(floats):
     want = x @ W[0].T
     want[25990:] = 0
     assert torch.equal(got.float(), want)
+
+
+@pytest.mark.gpu
+def test_scales_in_32_bits_are_any_numbers():
+    """0, negative, below the normal numbers and large, block by block; W and x of ones and whole scales, so that every sum is exact."""
+    some = [0.0, -1.0, 3.0, -0.375, 2.0 ** -126, 2.0 ** 100, 1.0, -2.0]
+    for R, n, k in ((4, 64, 1024), (300, 200, 1024), (300, 200, 1023), (9000, 2048, 1024)):
+        kb, nb = (k + 127) // 128, (n + 127) // 128
+        x, W = torch.ones(R, k, device="cuda").to(E4M3), torch.ones(1, n, k, device="cuda").to(E4M3)
+        scale = torch.full((R, kb), 127, dtype=torch.uint8, device="cuda")
+        offsets = torch.tensor([0, R], dtype=torch.int32).cuda()
+        for b in range(kb):                                    # one block at a time
+            for v in some:
+                ws = torch.zeros(1, nb, kb)
+                ws[:, :, b] = v
+                got = B.lasnet_block_product(x, scale, offsets, W, ws.cuda())
+                assert (got.double() == float(torch.tensor(min(128, k - 128 * b) * v, dtype=F32).to(BF16))).all(), (R, k, b, v)
+        ws = torch.full((1, nb, kb), 1.0)
+        ws[:, :, 1] = math.inf
+        got = B.lasnet_block_product(x, scale, offsets, W, ws.cuda())
+        assert (got.double() == math.inf).all()
+
+
+@pytest.mark.parametrize("given", [None, CURRENT, SIDE], ids=["none", "current", "other"])
+def test_what_a_call_makes_is_memory_of_its_stream(given, made):
+    x, W, off = dev(6, 8).to(E4M3).as_subclass(type(dev(1))), dev(3, 16, 8).to(E4M3).as_subclass(type(dev(1))), dev(4, dtype=torch.int32)
+    made.clear()
+    B.lasnet_block_product(x, dev(6, 1, dtype=torch.uint8), off, W, dev(3, 1, 1), **({} if given is None else {"stream": given}))
+    assert [s for _, s in made] == [given or CURRENT] and getattr(made[0][0], "used_on", []) == ([CURRENT] if given is SIDE else [])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("floats", [False, True], ids=["e8m0", "f32"])
+@pytest.mark.parametrize("R,n,k", [(600000, 4104, 1040), (4300000, 1024, 640), (560000, 4097, 201)])
+def test_offsets_past_32_bits(R, n, k, floats):
+    """Of bytes and of elements, of the output and of the rows: the last rows are compared with the same rows by themselves.  (Another kernel may run for so few: bf16 of sums of the same
+    whole numbers, which are exact.)"""
+    last, kb, nb = 400, (k + 127) // 128, (n + 127) // 128
+    some = torch.randint(-2, 3, (997, k), generator=gen(1)).to(E4M3).cuda().view(torch.uint8)
+    x = torch.empty(R, k, dtype=torch.uint8, device="cuda")
+    x[:R // 997 * 997].view(-1, 997, k)[:] = some
+    x[R // 997 * 997 - 997:] = some[:1].expand(R - R // 997 * 997 + 997, k)
+    x[-last:] = torch.randint(-2, 3, (last, k), generator=gen(2)).to(E4M3).cuda().view(torch.uint8)
+    x = x.view(E4M3)
+    W = torch.randint(-2, 3, (2, n, k), generator=gen(3)).to(E4M3).cuda()
+    scale = torch.full((R, kb), 127, dtype=torch.uint8, device="cuda")
+    wscale = torch.ones(2, nb, kb, device="cuda") if floats else torch.full((2, nb, kb), 127, dtype=torch.uint8, device="cuda")
+    got = B.lasnet_block_product(x, scale, torch.tensor([0, 997, R], dtype=torch.int32).cuda(), W, wscale)
+    end = B.lasnet_block_product(x[-last:].clone(), scale[-last:].clone(), torch.tensor([0, 0, last], dtype=torch.int32).cuda(), W, wscale)
+    assert torch.equal(got[-last:], end)
+    assert torch.equal(got[997:1994], got[997 * 400:997 * 401])

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_2210_06223_amd import binding as B
-from tests.test_call_streams import dev
+from tests.test_call_streams import CURRENT, SIDE, dev, made  # noqa: F401
 from tests.test_router import call, on_device, rows
 from tests.test_row_operators import BF16, E4M3, F32, f64, gen, rand, scale_ref
 
@@ -168,3 +168,65 @@ def test_tensors_that_are_refused(monkeypatch):
         B.lasnet_quantize_matrices(dev(2, 4, 8), out=dev(2, 8, 4).to(E4M3).as_subclass(type(x)))
     with pytest.raises(ValueError, match="together"):
         B.lasnet_quantize_matrices(dev(2, 4, 8), out_t=dev(2, 8, 4).to(E4M3).as_subclass(type(x)))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_an_infinity_is_nan_and_spoils_no_neighbour(dtype):
+    x = torch.randn(4, 256, generator=gen(1)).to(dtype)
+    x[1, 7], x[2, 200] = math.inf, -math.inf
+    x[1, 8] = 2.0 ** 121
+    clean = [t.cpu() for t in B.lasnet_quantize_rows(x.masked_fill(x.abs() == math.inf, 0).cuda())]
+    q, scale = (t.cpu() for t in B.lasnet_quantize_rows(x.cuda()))
+    m, ms = (t.cpu() for t in B.lasnet_quantize_matrices(x[None].cuda())[:2])
+    assert bits(scale)[1, 0] == 247 and bits(scale)[2, 1] == 247 and (bits(ms) == 247).all()
+    assert torch.isnan(q[1, 7].float()) and torch.isnan(q[2, 200].float()) and q[1, 8].float() == 2.0
+    assert int(torch.isnan(q.float()).sum()) == 2 and torch.equal(torch.isnan(m[0].float()), torch.isinf(x)) and m[0, 1, 8].float() == 2.0
+    keep = torch.ones(4, 256, dtype=torch.bool)
+    keep[1, :128] = keep[2, 128:] = False
+    assert torch.equal(bits(q)[keep], bits(clean[0])[keep])
+
+
+def calls(k):
+    """name, the call, how many outputs it makes"""
+    x, pos, off, W = dev(6, 8, dtype=BF16), dev(6, 2, dtype=torch.int32), dev(4, dtype=torch.int32), dev(3, 8, 16)
+    yield "rows", lambda: B.lasnet_quantize_rows(x, **k), 2
+    yield "rows by expert", lambda: B.lasnet_quantize_rows(x, pos, off, **k), 2
+    yield "matrices", lambda: B.lasnet_quantize_matrices(W, **k), 2
+    yield "matrices, transposed, too", lambda: B.lasnet_quantize_matrices(W, transposed=True, **k), 4
+
+
+@pytest.mark.parametrize("which", range(4))
+def test_what_a_call_makes_is_memory_of_its_stream(which, made):
+    for given in (None, CURRENT, SIDE):
+        name, run, outputs = list(calls({} if given is None else {"stream": given}))[which]
+        made.clear()
+        run()
+        assert [s for _, s in made] == [given or CURRENT] * outputs, name
+        assert [getattr(t, "used_on", []) for t, _ in made] == [[CURRENT] if given is SIDE else []] * outputs, name
+
+
+@pytest.mark.gpu
+def test_offsets_past_32_bits():
+    """Of bytes and of elements: rows, and matrices with their transposes, the last of which are compared with the same ones by themselves."""
+    n, cols, last = 600001, 8200, 130
+    x = torch.empty(n, cols, dtype=BF16, device="cuda")
+    x[:] = torch.randn(1, cols, generator=gen(1)).cuda()
+    x[-last:] = torch.randn(last, cols, generator=gen(2)).cuda()
+    q, scale = B.lasnet_quantize_rows(x)
+    few, few_s = B.lasnet_quantize_rows(x[-last:].clone())
+    assert torch.equal(q.view(torch.uint8)[-last:], few.view(torch.uint8)) and torch.equal(scale.view(torch.uint8)[-last:], few_s.view(torch.uint8))
+    del q
+    position = torch.arange(2 * n, dtype=torch.int32).flip(0).reshape(n, 2).cuda()                   # the last token goes to the first rows
+    q, scale = B.lasnet_quantize_rows(x, position, torch.tensor([0, 2 * n], dtype=torch.int32).cuda())
+    assert torch.equal(q.view(torch.uint8)[1:2 * last:2].flip(0), few.view(torch.uint8)) and torch.equal(scale.view(torch.uint8)[0:2 * last:2].flip(0), few_s.view(torch.uint8))
+    assert bool((q.view(torch.uint8)[2 * last:] == q.view(torch.uint8)[2 * last]).all())
+    del q, x
+    W = torch.empty(5, 1000, 1000001, dtype=BF16, device="cuda")
+    W[:] = torch.randn(1000, 1, generator=gen(3)).cuda()
+    W[4, :, -1001:] = torch.randn(1000, 1001, generator=gen(4)).cuda()
+    got = B.lasnet_quantize_matrices(W, transposed=True)
+    at = 1000001 // 128 * 128 - 896                                                                   # (whole blocks from here)
+    want = B.lasnet_quantize_matrices(W[4:, :, at:].contiguous(), transposed=True)
+    for have, part in zip((got[0][4:, :, at:], got[1][4:, :, at // 128:], got[2][4:, at:], got[3][4:, at // 128:]), want):
+        assert torch.equal(have.view(torch.uint8), part.view(torch.uint8))
