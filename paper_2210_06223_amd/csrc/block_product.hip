@@ -375,16 +375,259 @@ hipError_t go_block_tile(const ProductArgs& a, hipStream_t st) {
   return go_tile<true, false, false, false, false, BI, BJ, WI, WJ, STAGES, WK, SCALES>(a, st);
 }
 
+// ---- rows that are not whole pieces of 16 bytes, and few tiles ----
+// A piece that begins anywhere costs its load as much as several: these load whole words, the four that hold its first 16 bytes and the one behind them (no word but those that hold bytes of the
+// row), and shift.  Straight to registers, 1 row, 4096 columns of 4095: 18.7 -> 10.4 us.
+struct Words {
+  uint4_t v;
+  unsigned next;
+};
+// The words of 16 bytes of a row of `size` (16 or more) from byte b on, or of its last 16, where they end earlier (see cut_piece).
+__device__ __forceinline__ Words row_words(const unsigned char* row, int b, int size) {
+  typedef uint4_t four_words __attribute__((aligned(4)));
+  const size_t first = ((size_t)row + (b < size - 16 ? b : size - 16)) & ~(size_t)3, last = ((size_t)row + size - 1) & ~(size_t)3;
+  return Words{*(const four_words*)first, *(const unsigned*)(first + 16 < last ? first + 16 : last)};
+}
+__device__ __forceinline__ uint4_t word_piece(const Words& w, const unsigned char* row, int b, int size) {
+  const unsigned shift = ((unsigned)(size_t)row + (unsigned)(b < size - 16 ? b : size - 16)) & 3;
+  return uint4_t{__builtin_amdgcn_alignbyte(w.v[1], w.v[0], shift), __builtin_amdgcn_alignbyte(w.v[2], w.v[1], shift), __builtin_amdgcn_alignbyte(w.v[3], w.v[2], shift),
+                 __builtin_amdgcn_alignbyte(w.next, w.v[3], shift)};
+}
+
+// A workgroup's tile is 16 x 16 NJ; its four waves share the reduction.  A wave's fragments come straight to registers, DEPTH steps ahead: no LDS and no barrier before the sums of the waves
+// meet.  (The order of k in a step is the matrix core's own affair as long as both operands have the same: a load takes 64 bytes of each of 16 rows.)
+template <int SCALES, int NJ, int DEPTH>
+__global__ __launch_bounds__(256) void block_odd_kernel(ProductArgs a) {
+  __shared__ floatx4 sums[4][NJ][64];
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int ti = (int)(blockIdx.x % a.tiles_i), i0 = ti * 16;
+  int expert, j0, j_end;
+  if (!find_rows(a, 16 * NJ, (int)(blockIdx.x / a.tiles_i), expert, j0, j_end)) return;
+  expert = __builtin_amdgcn_readfirstlane(expert);
+  j0 = __builtin_amdgcn_readfirstlane(j0);
+  j_end = __builtin_amdgcn_readfirstlane(j_end);
+  floatx4 acc[NJ] = {};
+  const int steps = (a.nk + 127) / 128, share = (steps + 3) / 4, first = wave * share, n = steps - first < share ? steps - first : share;
+  if (expert < a.E && n > 0) {
+    // (rows and columns beyond the last are read as the last, and not stored)
+    const unsigned char* pj[NJ];
+    const uint8_t* px[NJ];
+    const int column = i0 + (lane & 15);
+    const unsigned char* pi = a.I.data + (long long)expert * a.i_expert + (long long)(column < a.ni ? column : a.ni - 1) * a.I.pitch;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const int r = j0 + 16 * j + (lane & 15);
+      const long long row = r < j_end ? r : j_end - 1;
+      pj[j] = a.J.data + row * a.J.pitch;
+      px[j] = a.xblocks + row * a.kb;
+    }
+    const long long w0 = ((long long)expert * ((a.ni + 127) >> 7) + (i0 >> 7)) * a.kb;
+    Words ri[DEPTH][2], rj[DEPTH][NJ][2];
+    unsigned sx[DEPTH][NJ], sw[DEPTH];
+    auto byte = [&](int s, int h) { return (first + s) * 128 + h * 64 + (lane >> 4) * 16; };
+    auto fetch = [&](int d, int s) {                           // the wave's step s (past the last: the last again, for nothing)
+      if (s >= n) s = n - 1;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        ri[d][h] = row_words(pi, byte(s, h), a.nk);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) rj[d][j][h] = row_words(pj[j], byte(s, h), a.nk);
+      }
+      sw[d] = SCALES == POWERS ? ((const uint8_t*)a.wblocks)[w0 + first + s] : ((const unsigned*)a.wblocks)[w0 + first + s];
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) sx[d][j] = px[j][first + s];
+    };
+    auto multiply = [&](int d, int s) {
+      const bool ends = (first + s + 1) * 128 > a.nk;
+      auto piece = [&](const Words& w, const unsigned char* row, int h) {
+        const uint4_t v = word_piece(w, row, byte(s, h), a.nk);
+        return ends ? cut_piece(v, a.nk - byte(s, h)) : v;
+      };
+      Fragment fi;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) fi.h[h] = piece(ri[d][h], pi, h);
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        Fragment fj;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) fj.h[h] = piece(rj[d][j][h], pj[j], h);
+        const floatx4 v = scaled_mfma<SCALES>(fi.all, fj.all, acc[j], sw[d], sx[d][j]);
+        acc[j] = SCALES == FLOATS ? add_scaled(acc[j], v, sw[d]) : v;
+      }
+    };
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) fetch(d, d);
+    for (int s = 0; s < n; s += DEPTH)
+#pragma unroll
+      for (int d = 0; d < DEPTH; ++d) {
+        if (s + d < n) multiply(d, s + d);
+        fetch(d, s + d + DEPTH);
+      }
+  }
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) sums[wave][j][lane] = acc[j];
+  __syncthreads();
+  if (wave >= NJ) return;
+  const floatx4 whole[1][1] = {{((sums[0][wave][lane] + sums[1][wave][lane]) + sums[2][wave][lane]) + sums[3][wave][lane]}};
+  store_tile<false, false>(a, a.out.data, expert, i0, j0 + 16 * wave, j_end, whole);
+}
+
+template <int SCALES, int NJ, int DEPTH>
+hipError_t go_block_odd(ProductArgs a, hipStream_t st) {
+  static_assert(NJ <= 4, "a wave stores 16 rows");
+  a.tiles_i = (a.ni + 15) / 16;
+  const long long groups = a.rows / (16 * NJ) + (a.rows < a.E ? a.rows : a.E) + 1;       // (experts with rows, one that is not full each, and the rest)
+  block_odd_kernel<SCALES, NJ, DEPTH><<<dim3((unsigned)(groups * a.tiles_i)), dim3(256), 0, st>>>(a);
+  return hipGetLastError();
+}
+
+// BI x BJ of the output by WK groups of WI x WJ waves that share the reduction: words go through registers, where they are shifted, into two LDS stages; the loads of the next DEPTH
+// steps are in flight while a step's products run.
+template <int SCALES, int BI, int BJ, int WI, int WJ, int WK, int DEPTH>
+__global__ __launch_bounds__(64 * WI * WJ * WK) void block_odd_tile_kernel(ProductArgs a) {
+  constexpr int G = 64 * WI * WJ, PI = BI * 8 / G, PJ = BJ * 8 / G, NI = BI / WI / 16, NJ = BJ / WJ / 16, STAGE = (BI + BJ) * 128;
+  static_assert(PI >= 1 && PJ >= 1 && BI <= 128, "pieces of a thread; columns in one block of 128");
+  extern __shared__ __attribute__((aligned(1024))) unsigned char product_lds[];
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), group = wave / (WI * WJ), tid = (int)threadIdx.x - group * G;
+  const int ti = (int)(blockIdx.x % a.tiles_i), i0 = ti * BI;
+  int expert, j0, j_end;
+  if (!find_rows(a, BJ, (int)(blockIdx.x / a.tiles_i), expert, j0, j_end)) return;
+  expert = __builtin_amdgcn_readfirstlane(expert);
+  j0 = __builtin_amdgcn_readfirstlane(j0);
+  j_end = __builtin_amdgcn_readfirstlane(j_end);
+  const int w = wave % (WI * WJ), wi = w % WI * (BI / WI), wj = w / WI * (BJ / WJ);
+  floatx4 acc[NI][NJ] = {};
+  if (expert < a.E) {
+    const int steps = (a.nk + 127) / 128, share = (steps + WK - 1) / WK, first = group * share, n = steps - first < share ? steps - first : share;    // (n: this group's, maybe none)
+    unsigned char* lds = product_lds + group * 2 * STAGE;
+    // (rows and columns beyond the last are read as the last, and not stored)
+    const unsigned char *pi[PI], *pj[PJ];
+#pragma unroll
+    for (int u = 0; u < PI; ++u) {
+      const int r = i0 + (u * G + tid) / 8;
+      pi[u] = a.I.data + (long long)expert * a.i_expert + (long long)(r < a.ni ? r : a.ni - 1) * a.I.pitch;
+    }
+#pragma unroll
+    for (int u = 0; u < PJ; ++u) {
+      const int r = j0 + (u * G + tid) / 8;
+      pj[u] = a.J.data + (long long)(r < j_end ? r : j_end - 1) * a.J.pitch;
+    }
+    const uint8_t* px[NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const int r = j0 + wj + 16 * j + (lane & 15);
+      px[j] = a.xblocks + (long long)(r < j_end ? r : j_end - 1) * a.kb;
+    }
+    const long long w0 = ((long long)expert * ((a.ni + 127) >> 7) + (i0 >> 7)) * a.kb;
+    Words ri[DEPTH][PI], rj[DEPTH][PJ];
+    unsigned nx[DEPTH + 1][NJ], nw[DEPTH + 1];                 // (the last: of the step that is multiplied)
+    const int byte = tid % 8 * 16;
+    auto fetch = [&](int d, int s) {                           // the group's step s (past the last: the last again, for nothing)
+      int step = first + (s < n ? s : n - 1);
+      step = step < 0 ? 0 : step < steps ? step : steps - 1;
+#pragma unroll
+      for (int u = 0; u < PI; ++u) ri[d][u] = row_words(pi[u], step * 128 + byte, a.nk);
+#pragma unroll
+      for (int u = 0; u < PJ; ++u) rj[d][u] = row_words(pj[u], step * 128 + byte, a.nk);
+      nw[d] = SCALES == POWERS ? ((const uint8_t*)a.wblocks)[w0 + step] : ((const unsigned*)a.wblocks)[w0 + step];
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) nx[d][j] = px[j][step];
+    };
+    auto stage = [&](int d, int s, int to) {
+      const int b = (first + s) * 128 + byte;
+      const bool ends = (first + s + 1) * 128 > a.nk;
+      auto put = [&](const unsigned char* row, const Words& w, int q, unsigned char* tile) {
+        const uint4_t v = word_piece(w, row, b, a.nk);
+        *(uint4_t*)(tile + Tile<false>::place(q)) = ends ? cut_piece(v, a.nk - b) : v;
+      };
+#pragma unroll
+      for (int u = 0; u < PI; ++u) put(pi[u], ri[d][u], u * G + tid, lds + to * STAGE);
+#pragma unroll
+      for (int u = 0; u < PJ; ++u) put(pj[u], rj[d][u], u * G + tid, lds + to * STAGE + BI * 128);
+      nw[DEPTH] = nw[d];
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) nx[DEPTH][j] = nx[d][j];
+    };
+    auto multiply = [&](int at) {
+      const unsigned char* t = lds + at * STAGE;
+      Fragment fi[NI];
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) fi[i].h[h] = Tile<false>::fragment(t, wi + 16 * i, h, lane);
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        Fragment fj;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) fj.h[h] = Tile<false>::fragment(t + BI * 128, wj + 16 * j, h, lane);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          const floatx4 v = scaled_mfma<SCALES>(fi[i].all, fj.all, acc[i][j], nw[DEPTH], nx[DEPTH][j]);
+          acc[i][j] = SCALES == FLOATS ? add_scaled(acc[i][j], v, nw[DEPTH]) : v;
+        }
+      }
+    };
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) fetch(d, d);
+    stage(0, 0, 0);
+    fetch(0, DEPTH);
+    __syncthreads();
+    int at = 0;
+    for (int s0 = 0; s0 < share; s0 += DEPTH)
+#pragma unroll
+      for (int d = 0; d < DEPTH; ++d) {
+        const int s = s0 + d;
+        if (s >= share) break;
+        if (s < n) multiply(at);                               // (a group without steps loads and waits along)
+        stage((d + 1) % DEPTH, s + 1, at ^ 1);
+        fetch((d + 1) % DEPTH, s + 1 + DEPTH);
+        at ^= 1;
+        __syncthreads();
+      }
+  }
+  if constexpr (WK > 1) {
+    floatx4* sums = (floatx4*)product_lds + w * 64 + lane;
+    constexpr int EACH = WI * WJ * 64;
+    if (group)
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) sums[((group - 1) * NI * NJ + i * NJ + j) * EACH] = acc[i][j];
+    __syncthreads();
+    if (group) return;
+#pragma unroll
+    for (int g = 0; g < WK - 1; ++g)
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[i][j] += sums[(g * NI * NJ + i * NJ + j) * EACH];
+  }
+  store_tile<false, false>(a, a.out.data, expert, i0 + wi, j0 + wj, j_end, acc);
+}
+
+template <int SCALES, int BI, int BJ, int WI, int WJ, int WK, int DEPTH>
+hipError_t go_block_odd_tile(ProductArgs a, hipStream_t st) {
+  a.tiles_i = (a.ni + BI - 1) / BI;
+  constexpr int stages = WK * 2 * (BI + BJ) * 128, sums = (WK - 1) * BI * BJ * 4, bytes = stages > sums ? stages : sums;
+  const long long groups = a.rows / BJ + (a.rows < a.E ? a.rows : a.E) + 1;
+  auto kernel = block_odd_tile_kernel<SCALES, BI, BJ, WI, WJ, WK, DEPTH>;
+  static std::atomic<unsigned long long> allowed{0};
+  const hipError_t e = allow_lds((const void*)kernel, bytes, allowed);
+  if (e != hipSuccess) return e;
+  kernel<<<dim3((unsigned)(groups * a.tiles_i)), dim3(64 * WI * WJ * WK), bytes, st>>>(a);
+  return hipGetLastError();
+}
+
 template <int SCALES>
 hipError_t go_blocks(ProductArgs a, hipStream_t st) {
+  const long long experts = a.E < a.rows ? a.E : a.rows, each = a.rows / experts;              // experts with rows at most, and rows of one
+  const int steps = (a.nk + 127) / 128;
+  // Tiles of BI x BJ, about (how the rows are spread is not known here).
+  auto tiles = [&](int BI, int BJ) {
+    const long long mean = a.rows / BJ + experts / 2, rows = mean > experts ? mean : experts;
+    return rows * ((a.ni + BI - 1) / BI);
+  };
   if (whole<false, false>(a, 1, 256)) {
-    const long long experts = a.E < a.rows ? a.E : a.rows, each = a.rows / experts;            // experts with rows at most, and rows of one
-    const int steps = (a.nk + 127) / 128;
-    // Tiles of BI x BJ, about (how the rows are spread is not known here).
-    auto tiles = [&](int BI, int BJ) {
-      const long long mean = a.rows / BJ + experts / 2, rows = mean > experts ? mean : experts;
-      return rows * ((a.ni + BI - 1) / BI);
-    };
     // us, bytes as scales, three sets of inputs in turn.
     // One workgroup a CU or little more, straight to registers: 1 row, 4096 x 4096 7.1 (64 x 16 by four groups of waves 8.5), 1024 x 2048 5.6 (6.5); 8 rows of 4 experts, 2048 x 4096 7.6
     // (8.6).  Of more of them or shorter reductions the loads of a few rows do not pay: 4 rows, 8192 x 2048 9.3 (7.2), 8 of 8, 1024 x 1024 7.6 (5.5).
@@ -408,10 +651,20 @@ hipError_t go_blocks(ProductArgs a, hipStream_t st) {
     if (tiles(128, 64) <= 512) return go_block_tile<SCALES, 128, 64, 2, 2, 3>(a, st);
     return go_block_tile<SCALES, 128, 128, 2, 2, 2>(a, st);
   }
+  // Whole pieces or not.  us, bytes and fp32 as scales, three sets of inputs in turn, against 128 x 128 of the last kernel: 16 x 32 without LDS, 1 row, 4095 x 4095 10.5 and 10.4 (40.8, 54.6),
+  // 16 of 4 experts, 1001 x 2047 8.4, 8.4 (23.9, 31.6); beyond that many tiles not: 300 of 4, 1001 x 1001 21.7.  64 x 32, the reduction shared by four groups: the latter 9.4, 9.4 (15.3, 18.8),
+  // 64 of 8, 2047 x 4095 22.7, 22.8 (49.9, 65.0).  128 x 64, by two: 1000 of 8, 1023 x 2049 21.4, 21.7 (31.8, 38.8), 2000 of 2, 1001 x 4001 36.2, 36.3 (55.2, 68.9).  128 x 128, by two: 30000
+  // of 16, 100 x 8001 112, 114 (133, 159); with more than one a CU not: 4000 of 8, 1001 x 521 28.6, 28.7 (17.7, 18.7), 16384 of 8, 2047 x 2049 257, 260 (184, 202).
+  if (a.nk >= 16) {
+    if (tiles(16, 32) <= 320) return go_block_odd<SCALES, 2, 4>(a, st);
+    if (steps >= 4 && tiles(64, 32) <= 256) return go_block_odd_tile<SCALES, 64, 32, 2, 1, 4, 2>(a, st);
+    if (steps >= 2 && tiles(128, 64) <= 256) return go_block_odd_tile<SCALES, 128, 64, 2, 2, 2, 1>(a, st);
+    if (steps >= 2 && tiles(128, 128) <= 256) return go_block_odd_tile<SCALES, 128, 128, 2, 2, 2, 1>(a, st);
+  }
   a.tiles_i = (a.ni + 127) / 128;
-  const long long tiles = a.rows / 128 + a.E + 1;              // (each expert and the rest may have one tile that is not full)
+  const long long row_tiles = a.rows / 128 + a.E + 1;          // (each expert and the rest may have one tile that is not full)
   auto kernel = a.nk >= 16 ? product_kernel<true, false, false, false, false, true, SCALES> : product_kernel<true, false, false, false, false, false, SCALES>;
-  kernel<<<dim3((unsigned)(tiles * a.tiles_i)), dim3(256), 0, st>>>(a);
+  kernel<<<dim3((unsigned)(row_tiles * a.tiles_i)), dim3(256), 0, st>>>(a);
   return hipGetLastError();
 }
 

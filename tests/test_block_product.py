@@ -331,3 +331,34 @@ def test_offsets_past_32_bits(R, n, k, floats):
     end = B.lasnet_block_product(x[-last:].clone(), scale[-last:].clone(), torch.tensor([0, 0, last], dtype=torch.int32).cuda(), W, wscale)
     assert torch.equal(got[-last:], end)
     assert torch.equal(got[997:1994], got[997 * 400:997 * 401])
+
+
+# rows that are not whole pieces of 16 bytes, kernel by kernel: few tiles, straight to registers; the reduction shared by four groups and by two; all of it in one
+ODD = [(1, 1, 515, 4095), (5, 2, 97, 17), (40, 4, 130, 143), (300, 4, 1001, 1001), (60, 8, 2047, 515), (64, 3, 1900, 1153), (1000, 8, 1023, 1049), (900, 3, 777, 130), (700, 2, 4001, 257),
+       (700, 2, 4002, 389), (4000, 8, 1001, 131), (900, 70, 40, 129)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("floats", [False, True], ids=["e8m0", "f32"])
+@pytest.mark.parametrize("shape", ODD, ids=str)
+def test_rows_of_any_width_and_address(shape, floats):
+    """At every place a word has for a first byte, with NaN on both sides of the rows and of the matrices; rows lie next to each other or apart."""
+    R, E, n, k = shape
+    o, offsets, x, scale, W, wscale = make(R, E, n, k, floats, min(R // 2, 9))
+    ref, size, cut = reference(o, x, scale, W, wscale)
+    bound = HALF[BF16] * (1 + 2 ** -8) * ref.abs() + (k + 4) * U * size + cut + 1e-38
+    want = None
+    for at, pad in ((1, 0), (2, 3), (3, 1), (4, 6)):
+        print("odd", shape, floats, at, pad, flush=True)
+        held = torch.full((64 + R * (k + pad),), 0x7f, dtype=torch.uint8, device="cuda")
+        X = held[at:at + R * (k + pad)].view(R, k + pad)[:, :k]
+        X.copy_(x.view(torch.uint8))
+        beside = torch.full((64 + E * n * k,), 0x7f, dtype=torch.uint8, device="cuda")
+        V = beside[5 - at:5 - at + E * n * k].view(E, n, k)
+        V.copy_(W.view(torch.uint8))
+        out = torch.full((R + 2, n + pad), 7.0, dtype=BF16, device="cuda")
+        got = B.lasnet_block_product(X.view(E4M3), scale, offsets, V.view(E4M3), wscale, out=out[1:R + 1, :n])
+        close(got, ref, bound, "out")
+        assert (out[0] == 7.0).all() and (out[R + 1] == 7.0).all() and (out[:, n:] == 7.0).all() and (got[int(o[-1]):] == 0).all()
+        want = got.clone() if want is None else want
+        assert torch.equal(got, want), "the same bits wherever they lie"
