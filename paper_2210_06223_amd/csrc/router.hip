@@ -4,7 +4,7 @@
 //   balance    counts[e], share[e] = mean_t p[t][e] with p = exp(l - lse), loss = (E sum_e counts[e] / (k T) share[e], mean_t lse[t]^2)
 //   gradient   p (c - sum_e p c) + 2 lse p d1 / T + that of the weights, with c[e] = d0 E counts[e] / (k T^2)
 //
-// A token's logits lie in the registers of L lanes (16, 32 or 64), read once.  Exponentials, sums and statistics are held in 32 bits, sums over tokens in 64; only the
+// A token's logits lie in the registers of L lanes (8 to 64), read once.  Exponentials, sums and statistics are held in 32 bits, sums over tokens in 64; only the
 // gradient is rounded, once, to the logits' type.
 #include <utility>
 
@@ -175,10 +175,12 @@ hipError_t go_choose(const ChooseArgs& a, hipStream_t st) {
   choose_kernel<T, L, N><<<dim3((unsigned)(b < 1 << 20 ? b : 1 << 20)), dim3(256), 0, st>>>(a);
   return hipGetLastError();
 }
+// As few lanes a token as hold it: 65536 tokens of 60 experts bf16, 6 each, by 8 lanes 7.2 us, by 16 11.8.
 template <class T>
 hipError_t pick_choose(const ChooseArgs& a, hipStream_t st) {
   constexpr int PER = Elem<T>::PER, SIXTEEN = 16 / PER;        // pieces of sixteen logits
   const int pieces = (a.E + PER - 1) / PER;
+  if (pieces <= 8 && a.k <= 8) return go_choose<T, 8, 1>(a, st);
   if (a.k <= 16) {
     if (pieces <= 16) return go_choose<T, 16, 1>(a, st);
     if (SIXTEEN == 4 && pieces <= 32) return go_choose<T, 16, 2>(a, st);
@@ -446,12 +448,14 @@ hipError_t go_balance(const BalanceArgs& a, hipStream_t st) {
   balance_join_kernel<<<dim3((unsigned)join_groups(a.E)), dim3(kBalance), 0, st>>>(a);
   return hipGetLastError();
 }
+// 23948 tokens of 340 experts fp32 by 128 lanes each 17.2 us, by 256 22.7.
 template <class T>
 hipError_t pick_balance(const BalanceArgs& a, hipStream_t st) {
   const int pieces = (a.E + Elem<T>::PER - 1) / Elem<T>::PER;
   if (pieces <= 16) return go_balance<T, 16, 1>(a, st);
   if (pieces <= 32) return go_balance<T, 32, 1>(a, st);
   if (pieces <= 64) return go_balance<T, 64, 1>(a, st);
+  if (pieces <= 128) return go_balance<T, 128, 1>(a, st);
   if (pieces <= 256) return go_balance<T, 256, 1>(a, st);
   return go_balance<T, 1024, 1>(a, st);
 }
@@ -607,13 +611,16 @@ hipError_t go_choose_grad(const ChooseGradArgs& a, hipStream_t st) {
   choose_grad_kernel<T, L, N><<<dim3((unsigned)(b < 2048 ? b : 2048)), dim3(256), bytes, st>>>(a);
   return hipGetLastError();
 }
+// 65536 tokens of 60 experts bf16 by 8 lanes 12.3 us, by 16 15.3; 23948 of 340 fp32 in two pieces a lane 17.3, in four 23.0.
 template <class T>
 hipError_t pick_choose_grad(const ChooseGradArgs& a, hipStream_t st) {
   const int pieces = (a.E + Elem<T>::PER - 1) / Elem<T>::PER;
   constexpr int MOST = 4096 / 64 / Elem<T>::PER;
+  if (pieces <= 8 && a.k <= 8) return go_choose_grad<T, 8, 1>(a, st);
   if (pieces <= 16) return go_choose_grad<T, 16, 1>(a, st);
   if (pieces <= 32) return go_choose_grad<T, 32, 1>(a, st);
   if (pieces <= 64) return go_choose_grad<T, 64, 1>(a, st);
+  if (pieces <= 128) return go_choose_grad<T, 64, 2>(a, st);
   if (pieces <= 256) return go_choose_grad<T, 64, 4>(a, st);
   return go_choose_grad<T, 64, MOST>(a, st);
 }

@@ -166,11 +166,18 @@ __device__ __forceinline__ float wave_max(float v) {
   for (int d = L / 2; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
   return v;
 }
-// The same without LDS: rotations within 16 lanes, then the rows of 16 and the halves of a wave change places (a result is the same bits in every lane; v: 32 bits of any kind).
+// The same without LDS: rotations within 16 lanes, then the rows of 16 and the halves of a wave change places (a result is the same bits in every lane; v: 32 bits of any kind).  8 lanes: the
+// mirrored lane, the neighbour, the neighbours' neighbour.
 template <int L, class T, class Op>
 __device__ __forceinline__ T lanes_join(T v, Op op) {
-  static_assert(sizeof(T) == 4 && L >= 16 && L <= 64, "whole rows of lanes");
-  auto turned = [](T x, auto by) { return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x120 + decltype(by)::value, 0xf, 0xf, true)); };   // row_ror
+  static_assert(sizeof(T) == 4 && (L == 8 || L == 16 || L == 32 || L == 64), "half rows of lanes, or whole ones");
+  auto moved = [](T x, auto how) { return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(how)::value, 0xf, 0xf, true)); };
+  if constexpr (L == 8) {
+    v = op(v, moved(v, std::integral_constant<int, 0x141>{}));           // row_half_mirror
+    v = op(v, moved(v, std::integral_constant<int, 0xb1>{}));            // quad_perm 1 0 3 2
+    return op(v, moved(v, std::integral_constant<int, 0x4e>{}));         // quad_perm 2 3 0 1
+  }
+  auto turned = [&](T x, auto by) { return moved(x, std::integral_constant<int, 0x120 + decltype(by)::value>{}); };                                                       // row_ror
   v = op(v, turned(v, std::integral_constant<int, 8>{}));
   v = op(v, turned(v, std::integral_constant<int, 4>{}));
   v = op(v, turned(v, std::integral_constant<int, 2>{}));

@@ -429,3 +429,15 @@ def test_offsets_past_32_bits():
     # (in place: what it read is gone)
     assert torch.equal(d[-last:], B.lasnet_choose_experts_backward(torch.randn(last, E, generator=gen(2)).cuda(), lse[-last:].clone(), experts[-last:].clone(), weights[-last:].clone(),
                                                                    dweights=dw[-last:].clone()))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("E", [7, 8, 31, 32, 33, 64, 65, 257, 340, 512, 513, 1000, 1024, 1025, 2048, 2049])
+def test_every_number_of_lanes(E, monkeypatch):
+    """Widths on both sides of where a token gets twice the lanes, through all three calls."""
+    import tests.test_router as module
+    monkeypatch.setattr(module, "SHAPES", [(37, E, k) for k in (1, 3, 7)] + ([(300, E, 8), (37, E, 9)] if E > 8 else []))
+    for dtype in (F32, BF16):
+        test_choice(dtype, E % 2 == 0)
+        test_balance(dtype)
+        test_gradient(dtype, E % 2 == 0)
