@@ -238,10 +238,23 @@ __device__ __forceinline__ double far_sum(double v) {
     return of(l[0], h[0]) + of(l[1], h[1]);
   }
 }
+// The sum over a wave, the same bits in each lane (see lanes_join).
+__device__ __forceinline__ double lanes_sum(double v) {
+  auto turned = [&](auto by) {
+    const unsigned long long u = __builtin_bit_cast(unsigned long long, v);
+    const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)u, 0x120 + decltype(by)::value, 0xf, 0xf, true);           // row_ror
+    const unsigned hi = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)(u >> 32), 0x120 + decltype(by)::value, 0xf, 0xf, true);
+    return __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
+  };
+  v += turned(std::integral_constant<int, 8>{});
+  v += turned(std::integral_constant<int, 4>{});
+  v += turned(std::integral_constant<int, 2>{});
+  v += turned(std::integral_constant<int, 1>{});
+  return far_sum<32>(far_sum<16>(v));
+}
 // Sum of the workgroup's values, in every thread.  join: 16 doubles, one set for each call.
 __device__ __forceinline__ double join_all(double v, double* join) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+  v = lanes_sum(v);
   if ((threadIdx.x & 63) == 0) join[threadIdx.x >> 6] = v;
   __syncthreads();
   double sum = 0.;
@@ -377,7 +390,7 @@ __global__ __launch_bounds__(kBalance) void balance_kernel(BalanceArgs a) {
 // A wave takes 64 columns of every 16th part.
 __global__ __launch_bounds__(kBalance) void balance_join_kernel(BalanceArgs a) {
   constexpr int W = kBalance / 64;
-  __shared__ double join[3][W];
+  __shared__ double join[2][W];
   __shared__ double sums[W][kJoinCols];
   __shared__ int counts[W][kJoinCols];
   __shared__ int last;
@@ -396,9 +409,20 @@ __global__ __launch_bounds__(kBalance) void balance_join_kernel(BalanceArgs a) {
     }
   sums[wave][lane] = sum;
   counts[wave][lane] = count;
-  squares = join_all(squares, join[0]);
-  tokens = join_all(tokens, join[1]);                          // (behind whose barrier the sums are there)
+  squares = lanes_sum(squares);
+  tokens = lanes_sum(tokens);
+  if (lane == 0) {
+    join[0][wave] = squares;
+    join[1][wave] = tokens;
+  }
+  __syncthreads();
   if (wave == 0) {
+    squares = tokens = 0.;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      squares += join[0][w];
+      tokens += join[1][w];
+    }
     sum = 0.;
     count = 0;
 #pragma unroll
@@ -412,8 +436,7 @@ __global__ __launch_bounds__(kBalance) void balance_join_kernel(BalanceArgs a) {
       a.share[e] = (float)share;
       loss = (double)count * share;
     }
-#pragma unroll
-    for (int d = 32; d; d >>= 1) loss += __shfl_xor(loss, d);
+    loss = lanes_sum(loss);
     if (gridDim.x == 1) {
       if (lane == 0) put_loss(a, loss, squares, tokens);
     } else if (lane == 0) {
@@ -427,8 +450,7 @@ __global__ __launch_bounds__(kBalance) void balance_join_kernel(BalanceArgs a) {
   if (!last || wave) return;
   __threadfence();
   loss = lane < (int)gridDim.x ? __hip_atomic_load(a.part_loss + lane, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.;
-#pragma unroll
-  for (int d = 32; d; d >>= 1) loss += __shfl_xor(loss, d);
+  loss = lanes_sum(loss);
   if (lane == 0) put_loss(a, loss, squares, tokens);
 }
 
