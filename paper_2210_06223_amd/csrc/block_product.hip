@@ -659,11 +659,13 @@ hipError_t go_blocks(ProductArgs a, hipStream_t st) {
   }
   // Whole pieces or not.  us, bytes and fp32 as scales, three sets of inputs in turn, against 128 x 128 of the last kernel: 16 x 32 without LDS, 1 row, 4095 x 4095 10.5 and 10.4 (40.8, 54.6),
   // 16 of 4 experts, 1001 x 2047 8.4, 8.4 (23.9, 31.6); beyond that many tiles not: 300 of 4, 1001 x 1001 21.7.  64 x 32, the reduction shared by four groups: the latter 9.4, 9.4 (15.3, 18.8),
-  // 64 of 8, 2047 x 4095 22.7, 22.8 (49.9, 65.0).  128 x 64, by two: 1000 of 8, 1023 x 2049 21.4, 21.7 (31.8, 38.8), 2000 of 2, 1001 x 4001 36.2, 36.3 (55.2, 68.9).  128 x 128, by two: 30000
+  // 64 of 8, 2047 x 4095 22.7, 22.8 (49.9, 65.0).  64 x 64, by four: 256 rows, 4095 x
+  // 4095 28.4, 27.8 (56.4, 70.5; 128 x 64 35.1, 35.9).  128 x 64, by two: 1000 of 8, 1023 x 2049 21.4, 21.7 (31.8, 38.8), 2000 of 2, 1001 x 4001 36.2, 36.3 (55.2, 68.9).  128 x 128, by two: 30000
   // of 16, 100 x 8001 112, 114 (133, 159); with more than one a CU not: 4000 of 8, 1001 x 521 28.6, 28.7 (17.7, 18.7), 16384 of 8, 2047 x 2049 257, 260 (184, 202).
   if (a.nk >= 16) {
     if (tiles(16, 32) <= 320) return go_block_odd<SCALES, 2, 4>(a, st);
     if (steps >= 4 && tiles(64, 32) <= 256) return go_block_odd_tile<SCALES, 64, 32, 2, 1, 4, 2>(a, st);
+    if (steps >= 4 && tiles(64, 64) <= 256) return go_block_odd_tile<SCALES, 64, 64, 2, 2, 4, 1>(a, st);
     if (steps >= 2 && tiles(128, 64) <= 256) return go_block_odd_tile<SCALES, 128, 64, 2, 2, 2, 1>(a, st);
     if (steps >= 2 && tiles(128, 128) <= 256) return go_block_odd_tile<SCALES, 128, 128, 2, 2, 2, 1>(a, st);
   }

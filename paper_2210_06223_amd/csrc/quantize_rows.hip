@@ -56,9 +56,10 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantizeRowsArgs a) 
   const int lane = (int)threadIdx.x % a.width, per = 256 / a.width;
   const long long first = (long long)blockIdx.x * per + threadIdx.x / a.width, stride = (long long)gridDim.x * per;
   const long long slots = a.position ? a.tokens * a.k : a.tokens;
+  const int part = (int)blockIdx.y, parts = (int)gridDim.y;    // workgroups that share a row
   for (long long t = first; t < a.tokens; t += stride) {
     const unsigned char* x = a.x.data + t * a.x.pitch;
-    for (int c0 = 0; c0 < a.pieces; c0 += a.width) {           // (every lane of a block comes along)
+    for (int c0 = part * a.width; c0 < a.pieces; c0 += parts * a.width) {                 // (every lane of a block comes along)
       const int c = c0 + lane, left = a.cols - c * El::PER;
       float f[El::PER];
       El::widen(load_piece<T>(x + (size_t)c * 16, left), f);
@@ -86,7 +87,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantizeRowsArgs a) 
   const long long s = a.offsets[a.E], sent = s < 0 ? 0 : s < slots ? s : slots;
   const unsigned none[2] = {0, 0};
   for (long long p = sent + first; p < slots; p += stride)
-    for (int c = lane; c < a.pieces; c += a.width) {
+    for (int c = part * a.width + lane; c < a.pieces; c += parts * a.width) {
       store_eight<T, PAST>(a.out.data + p * a.out.pitch + (size_t)c * El::PER, a.cols - c * El::PER, none);
       if (c % BL == 0) a.scale[p * a.blocks + c / BL] = 127;
     }
@@ -177,10 +178,12 @@ hipError_t launch_quantize_rows(int dtype, long long tokens, int k, int E, int c
   while (width < 256 && width < pieces) width *= 2;
   const QuantizeRowsArgs a{x, out, scale, position, offsets, tokens, k, E, cols, pieces, (cols + 127) / 128, width};
   const long long b = (tokens + 256 / width - 1) / (256 / width);
+  // (few wide rows are shared by workgroups, a thousand in all: 59 rows of 7520 fp32 to eight experts each 16.7 -> 4.6 us, 500 of 8192 bf16 to six 11.2 -> 8.7, 3 of 131072 fp32 50.5 -> 3.3)
+  const long long shares = b >= 1024 ? 1 : 1024 / b, chunks = (pieces + width - 1) / width;
   const bool past = rows_past((position ? tokens * k : tokens) * cols);
   auto kernel = dtype == LASNET_F32 ? past ? quantize_rows_kernel<float, true> : quantize_rows_kernel<float, false>
                                     : past ? quantize_rows_kernel<__bf16, true> : quantize_rows_kernel<__bf16, false>;
-  kernel<<<dim3((unsigned)(b < 1 << 20 ? b : 1 << 20)), dim3(256), 0, st>>>(a);
+  kernel<<<dim3((unsigned)(b < 1 << 20 ? b : 1 << 20), (unsigned)(chunks < shares ? chunks : shares)), dim3(256), 0, st>>>(a);
   return hipGetLastError();
 }
 

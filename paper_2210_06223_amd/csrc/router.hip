@@ -68,7 +68,7 @@ __device__ __forceinline__ void sort_keys(unsigned (&key)[C]) {
 //
 // A choice is a maximum over the lanes.  bf16: the 16 bits of a value's key and those of its expert are one number, no two are equal, and one maximum gives both; up to 16 a lane
 // are sorted once, so that a choice costs its lane a shift.  fp32: the maximum, then the lowest expert that has it.  Bound by these instructions (memory would take 1.9):
-// 16384 tokens of 256 experts bf16, 8 each, 6.7 us.  Unsorted keys and maxima through LDS: 13.2.  8 tokens of 64 experts, 2.2: a launch and one token's chain.
+// 16384 tokens of 256 experts bf16, 8 each, 6.4 to 7.3 us.  Unsorted keys and maxima through LDS: 13.2.  8 tokens of 64 experts, 2.2: a launch and one token's chain.
 template <class T, int L, int N>
 __global__ __launch_bounds__(256) void choose_kernel(ChooseArgs a) {
   using El = Elem<T>;
@@ -196,7 +196,7 @@ hipError_t pick_choose(const ChooseArgs& a, hipStream_t st) {
 // Two launches: workgroups sum runs of tokens, others join the sums of 64 columns each; the last of those to end (a counter tells, which the first launch cleared) adds up the loss
 // from their parts, in order.  One launch where one workgroup does.
 //
-// Bound by exp and by what a launch takes to begin and to join its waves: 32768 tokens of 256 experts fp32 (34 MB, out of the caches) 9.6 us and 7.1 for the join, 4099 of 60 bf16 6.6 and 5.8;
+// Bound by exp and by what a launch takes to begin and to join its waves: 32768 tokens of 256 experts fp32 (34 MB, out of the caches) 9.2 us and 5.9 for the join, 4099 of 60 bf16 6.7 and 4.7;
 // workgroups of 256 or 512 threads, or loads further ahead, took as long.
 constexpr int kBalance = 1024;                                 // threads of a workgroup
 constexpr int kJoinCols = 64;                                  // columns of a workgroup of the second launch

@@ -335,7 +335,7 @@ def test_offsets_past_32_bits(R, n, k, floats):
 
 # rows that are not whole pieces of 16 bytes, kernel by kernel: few tiles, straight to registers; the reduction shared by four groups and by two; all of it in one
 ODD = [(1, 1, 515, 4095), (5, 2, 97, 17), (40, 4, 130, 143), (300, 4, 1001, 1001), (60, 8, 2047, 515), (64, 3, 1900, 1153), (1000, 8, 1023, 1049), (900, 3, 777, 130), (700, 2, 4001, 257),
-       (700, 2, 4002, 389), (4000, 8, 1001, 131), (900, 70, 40, 129)]
+       (700, 2, 4002, 389), (4000, 8, 1001, 131), (900, 70, 40, 129), (1200, 20, 333, 1001), (256, 1, 4094, 519)]
 
 
 @pytest.mark.gpu
