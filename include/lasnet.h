@@ -435,7 +435,7 @@ LASNET_API int lasnet_choose_experts(const lasnet_rows* logits, const uint8_t* m
                                      uint32_t flags, void* hip_stream);
 
 /*
- * How evenly the experts are used.  logits, lse, experts as above (experts may be others: entries outside [0, E), slots beyond a capacity, do not count).  With T = the tokens
+ * How evenly the experts are used.  logits, lse, experts as above (or the list that lasnet_route gets: entries outside [0, E), slots beyond a capacity, do not count).  With T = the tokens
  * whose lse is not -inf, p[t][e] = exp(logits[t][e] - lse[t]):
  *   counts [E + 1]   rows of each expert; counts[E] = T
  *   share  [E]       1/T sum_t p[t][e]
@@ -452,8 +452,10 @@ LASNET_API int lasnet_balance(const lasnet_rows* logits, const float* lse, const
  *   dlogits[t][e] = p (c[e] - sum_e p c) + 2 dloss[1] lse p / T + (weights' part)          c[e] = dloss[0] E counts[e] / (k T^2)
  *   weights' part, s = sum_j weights[j] dweights[j]:  sum over the slots j with expert e of weights[j] (dweights[j] - s)
  *                  LASNET_WEIGHTS_OF_ALL:             sum over those slots of weights[j] dweights[j], minus p s
- * A slot with an expert outside [0, E) adds to s alone, one of weight 0 nothing (its dweights may be anything); an expert may be in several slots.  A token whose lse is -inf gets
- * zeros.
+ * experts, weights: as lasnet_choose_experts wrote them, also where slots were dropped afterwards (beyond an expert's capacity): the weights are shares of a sum that a dropped slot's logit is in.
+ * A dropped slot has a dweights of 0, as lasnet_combine_rows_backward writes it; its -1 belongs in the lists for lasnet_route and lasnet_balance alone.  A slot with an expert outside [0, E)
+ * adds to s, and its own logit's term, which has no place, is left out: with a weight other than 0 (LASNET_WEIGHTS_OF_ALL: and dweights other than 0) what comes out is not the gradient.
+ * A slot of weight 0 adds nothing (its dweights may be anything); an expert may be in several slots.  A token whose lse is -inf gets zeros.
  * dlogits: as logits, and may be the same rows.  In fp32, rounded once.  flags: as the forward call's.
  */
 LASNET_API int lasnet_choose_experts_backward(const lasnet_rows* logits, const float* lse, const int32_t* experts, const float* weights, int k,

@@ -859,7 +859,8 @@ def _chosen(experts: torch.Tensor) -> int:
 
 def lasnet_balance(logits: torch.Tensor, lse: torch.Tensor, experts: torch.Tensor, counts: Optional[torch.Tensor] = None, share: Optional[torch.Tensor] = None,
                    loss: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
-    """(counts int32 [E + 1], share [E], loss [2]): rows of each expert (and, last, the tokens that took part), mean probabilities, the balance loss and the mean of lse^2."""
+    """(counts int32 [E + 1], share [E], loss [2]): rows of each expert (and, last, the tokens that took part), mean probabilities, the balance loss and the mean of lse^2.
+    experts: as lasnet_route gets them (-1: a slot that was dropped)."""
     L = lib()
     if stream is None and counts is not None and share is not None and loss is not None:
         need = L.lasnet_balance_workspace_bytes(logits.shape[0], logits.shape[1]) if workspace is None and logits.dim() == 2 else 0
@@ -885,7 +886,8 @@ def lasnet_balance(logits: torch.Tensor, lse: torch.Tensor, experts: torch.Tenso
 def lasnet_choose_experts_backward(logits: torch.Tensor, lse: torch.Tensor, experts: torch.Tensor, weights: torch.Tensor, dweights: Optional[torch.Tensor] = None,
                                    counts: Optional[torch.Tensor] = None, dloss: Optional[torch.Tensor] = None, dlogits: Optional[torch.Tensor] = None,
                                    flags: int = 0, stream=None) -> torch.Tensor:
-    """dlogits (as logits) from the gradient dweights of the weights and dloss [2] of lasnet_balance's loss (with its counts)."""
+    """dlogits (as logits) from the gradient dweights of the weights and dloss [2] of lasnet_balance's loss (with its counts).  experts, weights: as chosen, slots that were dropped
+    afterwards included (their dweights are 0)."""
     if stream is None and dlogits is not None:
         L = lib()
         st = _marshal.choose_experts_backward(L.at_choose_experts_backward, logits, lse, experts, weights, dweights, counts, dloss, dlogits, flags)

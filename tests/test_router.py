@@ -441,3 +441,67 @@ def test_every_number_of_lanes(E, monkeypatch):
         test_choice(dtype, E % 2 == 0)
         test_balance(dtype)
         test_gradient(dtype, E % 2 == 0)
+
+
+# ---------------------------------------------------------------- slots dropped after the choice
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("of_all", [False, True], ids=["chosen", "all"])
+@pytest.mark.parametrize("tokens,E,k", [(12, 9, 3), (5, 70, 20), (3, 40, 33)])
+def test_gradient_with_dropped_slots_against_differences(tokens, E, k, of_all):
+    """The way of a layer with capacities: the list with -1 in the dropped slots' places goes to lasnet_route and lasnet_balance, the list as it was chosen to the gradient, with the dweights that
+    lasnet_combine_rows_backward writes (0 for a dropped slot).  Against differences of the 64-bit loss = dloss . loss + dout . out (counts held), where a dropped slot's logit is in the sum that
+    the weights are shares of.  At a step of 1e-4 the quotient is within 1e-6 (third derivatives of less than 100, a sixth of them times the step squared; terms of 1e2 and 1e-16 of them over the step); fp32: dweights
+    carry C + 2 u and the gradient 4 m + E + 32 u of its terms, together at most w (|dweights| + |s|), so twice the largest of dweights, and the balance's, under 4 here."""
+    g, C = gen(tokens + E), 4
+    l, dloss = rand(g, tokens, E), torch.tensor([1.3, 0.4]).cuda()
+    y, dout = rand(g, tokens * k, C), rand(g, tokens, C)
+    flags = B.LASNET_WEIGHTS_OF_ALL if of_all else 0
+    experts, weights, lse = B.lasnet_choose_experts(l, k, flags=flags)
+    dropped = (torch.rand(tokens, k, generator=g) < 0.3)
+    dropped[0, 0] = True
+    sent = experts.masked_fill(dropped.cuda(), -1)
+    counts, _, _ = B.lasnet_balance(l, lse, sent)
+    offsets, _, position = B.lasnet_route(sent, E)
+    _, dweights = B.lasnet_combine_rows_backward(dout, y, position, offsets, weights=weights)
+    assert (dweights.view(tokens, k).cpu()[dropped] == 0).all()
+    d = f64(B.lasnet_choose_experts_backward(l, lse, experts, weights, dweights=dweights, counts=counts, dloss=dloss, flags=flags))
+    e, p, D, Y, G = experts.cpu().long(), position.cpu().long(), f64(dloss), f64(y), f64(dout)
+    rows_ = Y[p.clamp(min=0)] * (~dropped)[..., None]
+    n = counts.cpu()[:E].double()
+
+    def value(v):
+        s = torch.logsumexp(v, 1)
+        w = torch.gather(v, 1, e)
+        w = torch.exp(w - s[:, None]) if of_all else torch.softmax(w, 1)
+        return D[0] * E * (n / (k * tokens) * torch.softmax(v, 1).mean(0)).sum() + D[1] * (s * s).mean() + (G * (w[..., None] * rows_).sum(1)).sum()
+
+    v, h = f64(l), 1e-4
+    slack = 1e-6 + (8 * float(v.abs().max()) + E + 64) * U * (2 * float(f64(dweights).abs().max()) + 4)
+    for t in range(tokens):
+        for i in range(E):
+            up, down = v.clone(), v.clone()
+            up[t, i] += h
+            down[t, i] -= h
+            assert abs(float(value(up) - value(down)) / (2 * h) - float(d[t, i])) < slack, (t, i)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_what_a_slot_without_an_expert_leaves_out(dtype):
+    """A slot of weight w whose expert is given as -1 leaves w (dweights - s) out of its logit's gradient (so the row of the weights' part does not add up to zero), and nothing else."""
+    for tokens, E, k in ((40, 9, 3), (9, 70, 20), (5, 40, 33)):
+        g = gen(tokens + 2 * E)
+        l, dw = rand(g, tokens, E, dtype=dtype), rand(g, tokens, k)
+        experts, weights, lse = B.lasnet_choose_experts(l, k)
+        dropped = torch.rand(tokens, k, generator=g) < 0.4
+        dw[dropped.cuda()] = 0.0
+        whole = f64(B.lasnet_choose_experts_backward(l, lse, experts, weights, dweights=dw))
+        given = f64(B.lasnet_choose_experts_backward(l, lse, experts.masked_fill(dropped.cuda(), -1), weights, dweights=dw))
+        w, s = f64(weights), (f64(weights) * f64(dw)).sum(1, keepdim=True)
+        left = torch.zeros(tokens, E + 1, dtype=torch.float64)
+        left.scatter_(1, torch.where(dropped, experts.cpu().long(), E), -w * s)
+        size = w.max() * (f64(dw).abs() * w).sum(1, keepdim=True)
+        # (the terms' sizes; each side is rounded once to its type)
+        close(whole - given, left[:, :E], HALF[dtype] * (1 + 2 ** -7) * (whole.abs() + given.abs()) + (k + 40) * U * (size + whole.abs()) + 1e-38, "left out")
+        close(whole.sum(1), torch.zeros(tokens, dtype=torch.float64), HALF[dtype] * (1 + 2 ** -7) * whole.abs().sum(1) + (E + 40) * U * (size[:, 0] * k + whole.abs().sum(1)) + 1e-38, "sum of a row")
