@@ -863,7 +863,8 @@ def lasnet_balance(logits: torch.Tensor, lse: torch.Tensor, experts: torch.Tenso
     experts: as lasnet_route gets them (-1: a slot that was dropped)."""
     L = lib()
     if stream is None and counts is not None and share is not None and loss is not None:
-        need = L.lasnet_balance_workspace_bytes(logits.shape[0], logits.shape[1]) if workspace is None and logits.dim() == 2 else 0
+        E = logits.shape[-1] if logits.dim() >= 2 else 0
+        need = L.lasnet_balance_workspace_bytes(logits.numel() // E, E) if E and workspace is None else 0
         st = _marshal.balance(L.at_balance, logits, lse, experts, counts, share, loss, _workspace(workspace, need, logits.device, None)[2])
         if st is not None:
             _check(st, "lasnet_balance")

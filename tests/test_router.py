@@ -505,3 +505,55 @@ def test_what_a_slot_without_an_expert_leaves_out(dtype):
         # (the terms' sizes; each side is rounded once to its type)
         close(whole - given, left[:, :E], HALF[dtype] * (1 + 2 ** -7) * (whole.abs() + given.abs()) + (k + 40) * U * (size + whole.abs()) + 1e-38, "left out")
         close(whole.sum(1), torch.zeros(tokens, dtype=torch.float64), HALF[dtype] * (1 + 2 ** -7) * whole.abs().sum(1) + (E + 40) * U * (size[:, 0] * k + whole.abs().sum(1)) + 1e-38, "sum of a row")
+
+
+# ---------------------------------------------------------------- logits of more than two dimensions
+
+def test_a_workspace_for_logits_of_any_dimensions(monkeypatch):
+    """Where the outputs are given and no workspace, one is made for as many tokens as the logits have rows, in two dimensions or four."""
+    asked, got = [], []
+
+    class Library:
+        at_balance = 0
+
+        def lasnet_balance_workspace_bytes(self, tokens, E):
+            asked.append((tokens, E))
+            return 512
+
+    class Marshal:
+        @staticmethod
+        def balance(at, logits, lse, experts, counts, share, loss, workspace):
+            got.append(workspace)
+            return 0
+
+    monkeypatch.setattr(B, "lib", Library)
+    monkeypatch.setattr(B, "_marshal", Marshal)
+    outputs = dict(counts=dev(9, dtype=torch.int32), share=dev(8), loss=dev(2))
+    for shape in ((6, 8), (2, 3, 8), (1, 3, 2, 8)):
+        B.lasnet_balance(dev(*shape), dev(6), dev(6, 2, dtype=torch.int32), **outputs)
+        assert asked.pop() == (6, 8) and got.pop().numel() == 512, shape
+    for shape in ((), (8,), (6, 0)):                           # (no rows: refused behind, not here)
+        B.lasnet_balance(dev(*shape), dev(6), dev(6, 2, dtype=torch.int32), **outputs)
+        assert not asked and got.pop() is None, shape
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens", [2 * 8 * 16, 2 * 32 * 32], ids=["one workgroup", "many"])
+def test_logits_of_four_dimensions(tokens):
+    """[N, H, W, E] through the three calls, outputs given or not, on both sides of where the balance needs a workspace: the same bits as [N H W, E]."""
+    E, k, g = 24, 2, gen(tokens)
+    l, dloss = rand(g, tokens, E), torch.tensor([0.5, 0.1]).cuda()
+    assert (B.lib().lasnet_balance_workspace_bytes(tokens, E) > 0) == (tokens > 1000)
+
+    def path(l, given):
+        new = lambda *s, dtype=F32: torch.empty(*s, dtype=dtype, device="cuda") if given else None
+        experts, weights, lse = B.lasnet_choose_experts(l, k, experts=new(tokens, k, dtype=torch.int32), weights=new(tokens, k), lse=new(tokens))
+        balance = B.lasnet_balance(l, lse, experts, counts=new(E + 1, dtype=torch.int32), share=new(E), loss=new(2))
+        d = B.lasnet_choose_experts_backward(l, lse, experts, weights, dweights=weights, counts=balance[0], dloss=dloss, dlogits=torch.empty_like(l) if given else None)
+        assert d.shape == l.shape
+        return [experts, weights, lse, *balance, d.reshape(tokens, E)]
+
+    want = path(l, False)
+    for shape in ((tokens, E), (2, -1, E), (2, -1, 16, E)):
+        for given in (False, True):
+            assert all(torch.equal(a, b) for a, b in zip(path(l.view(shape), given), want)), (shape, given)
