@@ -483,7 +483,7 @@ LASNET_API int lasnet_quantize_matrices(const void* W, int dtype, int E, int n, 
  * The experts' products of such rows and matrices: for every row p of expert e
  *   out[p][i] = sum over blocks b of 2^(scale[p][b] - 127) * wscale[e][i / 128][b] * sum_{c in b} x[p][c] * W[e][i][c]
  * x: E4M3, scale [rows][(cols + 127) / 128]; W: [E][out.cols][x.cols], E4M3, dense; wscale: [E][(out.cols + 127) / 128][(cols + 127) / 128], wscale_dtype LASNET_E8M0
- * (bytes, as lasnet_quantize_matrices writes them: applied by the matrix core) or LASNET_F32.  A block's sum is the matrix core's own, as with lasnet_expert_product; blocks are added
+ * (bytes, as lasnet_quantize_matrices writes them: applied by the matrix core) or LASNET_F32 (whose power of two is; neither scale by itself leaves fp32's range).  A block's sum is the matrix core's own, as with lasnet_expert_product; blocks are added
  * in fp32, and out (BF16) is rounded once.  Rows from offsets[E] on are set to zero.  flags, offsets: as there.
  * The gradient of x is the same product of dy and the transposed matrices; that of W: lasnet_expert_product_dw of the rows in BF16.
  */

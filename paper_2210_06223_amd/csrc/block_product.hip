@@ -243,8 +243,8 @@ __global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
   floatx4 acc[8][4];
   Fragment fi[4], fj[4];
   unsigned sx[4], sw = 0, sw_next = 0;
-  unsigned sw_before = 0;
-  floatx4 part[kLag];                                         // FLOATS: the sums of a block of 128
+  float m_now = 0.f, m_before = 0.f;                          // FLOATS: the scales' m, of this step and the one before; sw is their power
+  floatx4 part[kLag];                                         // ... and the sums of a block of 128
   unsigned c = lds, c_slot = slots;                           // the step that fragments are read from
   unsigned at_i = S::lane_base(0, lane) + c + 32768 + wi * 128;                           // where a lane reads block 0 of I's from (and of J's, wi and wj apart)
   auto read_i = [&](int i) { S::fragment(at_i, i, fi[i % 4]); };
@@ -254,7 +254,15 @@ __global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
     S::fragment(at_i + (unsigned)((wj - wi) * 128 - 32768), j, fj[j]);
     sx[j] = read_dword(c_slot + (of & 15) * 4 + 64 * j);
   };
-  auto add_part = [&](int m, unsigned w) {                    // that of the m-th MFMA of a step
+  auto take_scale = [&](unsigned w) {
+    if constexpr (SCALES == FLOATS) {
+      m_now = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(scale_mantissa(w))));
+      sw = scale_power(w);
+    } else {
+      sw = w;
+    }
+  };
+  auto add_part = [&](int m, float w) {                       // that of the m-th MFMA of a step
     floatx4& sum = acc[m / 4][m % 4 ^ 2];
     sum = add_scaled(sum, part[m % kLag], w);
   };
@@ -262,8 +270,8 @@ __global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
     const int j = p ^ 2, m = 4 * i + p;
     __builtin_amdgcn_sched_barrier(0);
     if constexpr (SCALES == FLOATS) {
-      add_part(m >= kLag ? m - kLag : 32 + m - kLag, m >= kLag ? sw : sw_before);
-      part[m % kLag] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fj[j].all, fi[i % 4].all, floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, (int)sx[j], 0, 0x7f7f7f7f);
+      add_part(m >= kLag ? m - kLag : 32 + m - kLag, m >= kLag ? m_now : m_before);
+      part[m % kLag] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fj[j].all, fi[i % 4].all, floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, (int)sx[j], 0, (int)sw);
     } else {
       acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fj[j].all, fi[i % 4].all, acc[i][j], 0, 0, 0, (int)sx[j], 0, (int)sw);
     }
@@ -303,8 +311,8 @@ __global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
         }
       }
     }
-    sw_before = sw;
-    sw = SCALES == FLOATS ? (unsigned)__builtin_amdgcn_readfirstlane(sw_next) : sw_next;
+    m_before = m_now;
+    take_scale(sw_next);
   };
 
   int round = 0;
@@ -317,8 +325,7 @@ __global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
     counted_barrier<kStepLoads>();
 #pragma unroll
     for (int j = 0; j < 4; ++j) read_j(j);
-    sw = read_dword(c_slot + 256);
-    if constexpr (SCALES == FLOATS) sw = __builtin_amdgcn_readfirstlane(sw);
+    take_scale(read_dword(c_slot + 256));
 #pragma unroll
     for (int i = 0; i < 3; ++i) read_i(i);
     while (true) {
@@ -335,7 +342,7 @@ __global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
       if constexpr (SCALES == FLOATS) {
-        sw_before = 0;
+        m_before = 0.f;
 #pragma unroll
         for (int r = 0; r < kLag; ++r) part[r] = floatx4{0.f, 0.f, 0.f, 0.f};
       }
@@ -348,7 +355,7 @@ __global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
       }
       if constexpr (SCALES == FLOATS)
 #pragma unroll
-        for (int m = 32 - kLag; m < 32; ++m) add_part(m, sw_before);
+        for (int m = 32 - kLag; m < 32; ++m) add_part(m, m_before);
       store_block_tile(a, w, wi, wj, lane, acc);
       if (!more) break;
       young = true;
@@ -463,8 +470,8 @@ __global__ __launch_bounds__(256) void block_odd_kernel(ProductArgs a) {
         Fragment fj;
 #pragma unroll
         for (int h = 0; h < 2; ++h) fj.h[h] = piece(rj[d][j][h], pj[j], h);
-        const floatx4 v = scaled_mfma<SCALES>(fi.all, fj.all, acc[j], sw[d], sx[d][j]);
-        acc[j] = SCALES == FLOATS ? add_scaled(acc[j], v, sw[d]) : v;
+        const floatx4 v = scaled_mfma<SCALES>(fi.all, fj.all, acc[j], SCALES == FLOATS ? scale_power(sw[d]) : sw[d], sx[d][j]);
+        acc[j] = SCALES == FLOATS ? add_scaled(acc[j], v, scale_mantissa(sw[d])) : v;
       }
     };
 #pragma unroll
@@ -574,8 +581,8 @@ __global__ __launch_bounds__(64 * WI * WJ * WK) void block_odd_tile_kernel(Produ
         for (int h = 0; h < 2; ++h) fj.h[h] = Tile<false>::fragment(t + BI * 128, wj + 16 * j, h, lane);
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-          const floatx4 v = scaled_mfma<SCALES>(fi[i].all, fj.all, acc[i][j], nw[DEPTH], nx[DEPTH][j]);
-          acc[i][j] = SCALES == FLOATS ? add_scaled(acc[i][j], v, nw[DEPTH]) : v;
+          const floatx4 v = scaled_mfma<SCALES>(fi[i].all, fj.all, acc[i][j], SCALES == FLOATS ? scale_power(nw[DEPTH]) : nw[DEPTH], nx[DEPTH][j]);
+          acc[i][j] = SCALES == FLOATS ? add_scaled(acc[i][j], v, scale_mantissa(nw[DEPTH])) : v;
         }
       }
     };

@@ -31,9 +31,16 @@ struct ProductArgs {
 
 // Which scales 8-bit operands have (SCALES).  ROWS: one for each row of J and of I, applied where the sums are stored.  Blocks of 128 of the reduction, those of I shared by 128 of
 // its rows: POWERS: both powers of two, bytes 127 + e, which the matrix core applies to the products for nothing; FLOATS: J's powers of two, likewise, and I's in
-// 32 bits, with which the sum of a block, 128 products from 0, is added to the whole: an fma for each element and step, run while the matrix core multiplies.
+// 32 bits, m 2^e with m from 1 to 2: the matrix core applies 2^e, too (it adds the two exponents: neither scale by itself takes a sum out of fp32's range), and with m the sum of a block,
+// 128 products from 0, is added to the whole: an fma for each element and step, run while the matrix core multiplies.
 enum { ROWS = 0, POWERS = 1, FLOATS = 2 };
-// A step's product with the scales of its block.  w: byte or float; part: where the sum of a block of FLOATS is before it is added.
+// The byte and m of a scale in 32 bits.  (Below the normal numbers: 2^-127 and an m of less than 1.  Infinities and NaN are m's; their byte is a number, 255 being NaN.)
+__device__ __forceinline__ unsigned scale_power(unsigned w) {
+  const unsigned e = w >> 23 & 255;
+  return e < 254 ? e : 254;
+}
+__device__ __forceinline__ float scale_mantissa(unsigned w) { return __builtin_amdgcn_ldexpf(__uint_as_float(w), 127 - (int)(w >> 23 & 255)); }
+// A step's product with the scales of its block.  w: byte (of FLOATS: scale_power's).
 template <int SCALES>
 __device__ __forceinline__ floatx4 scaled_mfma(intx8 i, intx8 j, floatx4 acc, unsigned w, unsigned x) {
   if constexpr (SCALES == ROWS)
@@ -41,7 +48,7 @@ __device__ __forceinline__ floatx4 scaled_mfma(intx8 i, intx8 j, floatx4 acc, un
   else if constexpr (SCALES == POWERS)
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(i, j, acc, 0, 0, 0, (int)w, 0, (int)x);
   else
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(i, j, floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0x7f7f7f7f, 0, (int)x);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(i, j, floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, (int)w, 0, (int)x);
 }
 // The same with the rows of J as the first operand: four of them in a lane, of one row of I.
 template <int SCALES>
@@ -49,11 +56,11 @@ __device__ __forceinline__ floatx4 turned_mfma(intx8 i, intx8 j, floatx4 acc, un
   if constexpr (SCALES == POWERS)
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(j, i, acc, 0, 0, 0, (int)x, 0, (int)w);
   else
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(j, i, floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, (int)x, 0, 0x7f7f7f7f);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(j, i, floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, (int)x, 0, (int)w);
 }
-__device__ __forceinline__ floatx4 add_scaled(floatx4 acc, floatx4 part, unsigned w) {
+__device__ __forceinline__ floatx4 add_scaled(floatx4 acc, floatx4 part, float m) {
 #pragma unroll
-  for (int r = 0; r < 4; ++r) acc[r] = __builtin_fmaf(part[r], __uint_as_float(w), acc[r]);
+  for (int r = 0; r < 4; ++r) acc[r] = __builtin_fmaf(part[r], m, acc[r]);
   return acc;
 }
 
@@ -408,8 +415,8 @@ __global__ __launch_bounds__(256) void product_kernel(ProductArgs a) {
         f.u[1] = Tile<JC>::fragment(lds[s][1], wj + 16 * j, 1, lane);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const floatx4 v = scaled_mfma<SCALES>(fi[i], f.v, acc[i][j], sw, sx[j]);
-          acc[i][j] = SCALES == FLOATS ? add_scaled(acc[i][j], v, sw) : v;
+          const floatx4 v = scaled_mfma<SCALES>(fi[i], f.v, acc[i][j], SCALES == FLOATS ? scale_power(sw) : sw, sx[j]);
+          acc[i][j] = SCALES == FLOATS ? add_scaled(acc[i][j], v, scale_mantissa(sw)) : v;
         }
       }
     } else {
@@ -695,7 +702,9 @@ __device__ __forceinline__ void tile_product(const ProductArgs& a, unsigned char
   floatx4 acc[NI][NJ] = {};
   Fragment fi[4], fj[2][NJ];
   unsigned sx[2][NJ], sw[2] = {0, 0};                         // scales of this step and the next
-  constexpr int LAG = NJ > 1 ? 3 : 2;                         // (the scale of the step before is kept up to block NI - 2)
+  constexpr int LAG = NJ > 1 ? 3 : 2;
+  unsigned power = 0;                                         // FLOATS: this step's scale, and the m of the step before
+  float m_now = 0.f, m_before = 0.f;
   floatx4 part[4] = {};                                       // FLOATS: sums of blocks, each added to its whole LAG MFMAs later
   const unsigned bi = SI::lane_base(wi, lane), bj = SJ::lane_base(wj, lane) + SI::BYTES;
   unsigned at = lds, at_i = bi + at;                          // at: the stage that is read
@@ -710,7 +719,7 @@ __device__ __forceinline__ void tile_product(const ProductArgs& a, unsigned char
       sw[stage.value] = read_dword(s_at + 256);
     }
   };
-  auto add_part = [&](int m, unsigned w) { acc[m / NJ][m % NJ] = add_scaled(acc[m / NJ][m % NJ], part[m % 4], w); };
+  auto add_part = [&](int m, float w) { acc[m / NJ][m % NJ] = add_scaled(acc[m / NJ][m % NJ], part[m % 4], w); };
   constexpr int MFMAS = (FP8 ? 1 : 2) * NJ;                   // of a block
   auto multiply = [&](auto stage, int i, int m0, int m1) {
     constexpr int S = decltype(stage)::value;
@@ -721,8 +730,8 @@ __device__ __forceinline__ void tile_product(const ProductArgs& a, unsigned char
       if constexpr (SCALES == FLOATS) {
         constexpr int ALL = NI * NJ;
         const int at = i * NJ + j;
-        part[at % 4] = turned_mfma<SCALES>(fi[i % 4].all, fj[S][j].all, floatx4{}, 0, sx[S][j]);
-        add_part(at >= LAG ? at - LAG : ALL + at - LAG, at >= LAG ? sw[S] : sw[S ^ 1]);
+        part[at % 4] = turned_mfma<SCALES>(fi[i % 4].all, fj[S][j].all, floatx4{}, power, sx[S][j]);
+        add_part(at >= LAG ? at - LAG : ALL + at - LAG, at >= LAG ? m_now : m_before);
       } else if constexpr (SCALES == POWERS) {
         acc[i][j] = turned_mfma<SCALES>(fi[i % 4].all, fj[S][j].all, acc[i][j], sw[S], sx[S][j]);
       } else if constexpr (FP8) {
@@ -735,6 +744,11 @@ __device__ __forceinline__ void tile_product(const ProductArgs& a, unsigned char
   };
   auto step = [&](auto stage) {
     constexpr int S = decltype(stage)::value;
+    if constexpr (SCALES == FLOATS) {
+      power = scale_power(sw[S]);
+      m_before = m_now;
+      m_now = scale_mantissa(sw[S]);
+    }
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       if (i + 3 < NI) read_i(i + 3);
@@ -775,7 +789,7 @@ __device__ __forceinline__ void tile_product(const ProductArgs& a, unsigned char
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // (the last loads write to this workgroup's LDS)
     if constexpr (SCALES == FLOATS)
 #pragma unroll
-      for (int m = NI * NJ - LAG; m < NI * NJ; ++m) add_part(m, steps & 1 ? sw[0] : sw[1]);
+      for (int m = NI * NJ - LAG; m < NI * NJ; ++m) add_part(m, m_now);
   }
   if constexpr (WK > 1) {
     floatx4* sums = (floatx4*)product_lds + wave * NI * NJ * 64 + lane;        // [group - 1][wave][block][lane]
@@ -992,7 +1006,7 @@ __global__ __launch_bounds__(256) void product_few_kernel(ProductArgs a) {
 #pragma unroll
         for (int j = 0; j < NJ; ++j)
           if constexpr (SCALES == FLOATS)
-            acc[j] = add_scaled(acc[j], scaled_mfma<SCALES>(fi[d].all, fj[d][j].all, acc[j], 0, sx[d][j]), sw[d]);
+            acc[j] = add_scaled(acc[j], scaled_mfma<SCALES>(fi[d].all, fj[d][j].all, acc[j], scale_power(sw[d]), sx[d][j]), scale_mantissa(sw[d]));
           else if constexpr (FP8)
             acc[j] = scaled_mfma<SCALES>(fi[d].all, fj[d][j].all, acc[j], sw[d], sx[d][j]);
           else

@@ -362,3 +362,22 @@ def test_rows_of_any_width_and_address(shape, floats):
         assert (out[0] == 7.0).all() and (out[R + 1] == 7.0).all() and (out[:, n:] == 7.0).all() and (got[int(o[-1]):] == 0).all()
         want = got.clone() if want is None else want
         assert torch.equal(got, want), "the same bits wherever they lie"
+
+
+@pytest.mark.gpu
+def test_scales_in_32_bits_at_the_ends_of_their_range():
+    """The same with fp32 scales of the matrices: no part of a scale meets a sum before the row's does.  1.5, 1.25 and the sums are exact; k products of one size, so the result is."""
+    one, least = 1.0, 2.0 ** -9                                # (e4m3's smallest number)
+    for R, n, k in ((4, 64, 256), (16, 64, 512), (64, 512, 1024), (300, 128, 256), (300, 128, 250), (40, 1536, 650), (9000, 2048, 256), (9000, 2048, 250)):
+        offsets = torch.tensor([0, R], dtype=torch.int32).cuda()
+        kb, nb = (k + 127) // 128, (n + 127) // 128
+        for v, sx, w in ((one, 254, 1.5 * 2.0 ** -100), (one, 27, 1.5 * 2.0 ** 118), (least, 27, 1.5 * 2.0 ** 127), (least, 1, 1.25 * 2.0 ** 126), (one, 100, -1.25 * 2.0 ** 20),
+                         (one, 254, 1.25 * 2.0 ** -140), (one, 254, 2.0 ** -149), (one, 254, 0.0), (one, 1, math.inf), (least, 250, -math.inf)):
+            print("fp32 scales", R, n, k, v, sx, w, flush=True)
+            x, W = torch.full((R, k), v, device="cuda").to(E4M3), torch.full((1, n, k), v, device="cuda").to(E4M3)
+            scale = torch.full((R, kb), sx, dtype=torch.uint8, device="cuda")
+            wscale = torch.full((1, nb, kb), w, device="cuda")
+            got = B.lasnet_block_product(x, scale, offsets, W, wscale)
+            want = k * v * v * w * 2.0 ** (sx - 127)
+            assert math.isinf(w) or w == 0.0 or 2.0 ** -126 <= abs(want) < 2.0 ** 128
+            assert (got.double() == float(torch.tensor(want).to(BF16))).all(), (R, n, k, v, sx, w, float(got[0, 0]), want)
