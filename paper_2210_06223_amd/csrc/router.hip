@@ -509,6 +509,7 @@ __global__ __launch_bounds__(256) void choose_grad_kernel(ChooseGradArgs a) {
     for (int e = lane; e < pitch; e += L) row[e] = 0.f;
   // what a probability of 1 would get from the balance loss, expert by expert
   float c[N][El::PER] = {}, z = 0.f;
+  bool wild = false;
   if (a.dloss) {
     const float T_ = (float)(a.counts[a.E] > 0 ? a.counts[a.E] : 1), unit = a.dloss[0] / T_ * ((float)a.E / ((float)a.k * T_));
     z = 2.f * a.dloss[1] / T_;
@@ -518,7 +519,13 @@ __global__ __launch_bounds__(256) void choose_grad_kernel(ChooseGradArgs a) {
       for (int j = 0; j < El::PER; ++j) {
         const int e = (i * L + lane) * El::PER + j;
         if (e < a.E) c[i][j] = unit * (float)a.counts[e];
+        if (!(fabsf(c[i][j]) < INFINITY)) {
+          wild = true;
+          c[i][j] = 0.f;
+        }
       }
+    // An infinite or NaN dloss makes NaN of the tokens that take part, through a term that only they have: 0 times it would reach the others, which get zeros.
+    if (__ballot(wild)) z = __uint_as_float(0x7fc00000u);
   }
   const unsigned long long group = (L == 64 ? ~0ull : (1ull << (L & 63)) - 1) << ((int)(threadIdx.x & 63) / L * L);     // the group's lanes
   // what is read of a token; the next one's is asked for before this one's is used.  Slot j: lane j (and j + L ...).

@@ -557,3 +557,23 @@ def test_logits_of_four_dimensions(tokens):
     for shape in ((tokens, E), (2, -1, E), (2, -1, 16, E)):
         for given in (False, True):
             assert all(torch.equal(a, b) for a, b in zip(path(l.view(shape), given), want)), (shape, given)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("of_all", [False, True], ids=["chosen", "all"])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_tokens_that_take_no_part_get_zeros_whatever_the_loss_is(dtype, of_all):
+    """An infinite or NaN gradient of the loss (an overflow of a scaled one), logits and dweights that are NaN: zeros for a token whose lse is -inf, also beside others in its wave."""
+    for tokens, E, k in ((50, 8, 2), (50, 60, 2), (9, 200, 6), (7, 500, 8), (5, 1000, 33), (3, 4000, 4)):
+        g = gen(E)
+        l, dw = rand(g, tokens, E, dtype=dtype), rand(g, tokens, k)
+        mask = torch.arange(tokens) % 3 != 1
+        l[~mask.cuda()] = math.nan
+        dw[~mask.cuda()] = math.nan
+        flags = B.LASNET_WEIGHTS_OF_ALL if of_all else 0
+        experts, weights, lse = B.lasnet_choose_experts(l, k, mask=mask.cuda(), flags=flags)
+        counts, _, _ = B.lasnet_balance(l, lse, experts)
+        for dloss in ((math.inf, 0.1), (math.nan, 0.1), (0.1, math.inf), (0.1, math.nan), (-math.inf, math.inf)):
+            d = B.lasnet_choose_experts_backward(l, lse, experts, weights, dweights=dw, counts=counts, dloss=torch.tensor(dloss).cuda(), flags=flags)
+            assert (d[~mask.cuda()] == 0).all(), (tokens, E, k, dloss)
+            assert not torch.isfinite(d[mask.cuda()].float()).all()
