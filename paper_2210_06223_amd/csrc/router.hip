@@ -301,7 +301,6 @@ __global__ __launch_bounds__(kBalance) void balance_kernel(BalanceArgs a) {
         piece[u][i] = load_piece<T>(a.logits.data + t * a.logits.pitch + (size_t)c * El::BYTES, t < a.tokens ? a.E - c : 0);
       }
     }
-    float sum[C] = {};                                         // of U tokens in 32 bits
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (lse[u] == -INFINITY) continue;
@@ -312,11 +311,9 @@ __global__ __launch_bounds__(kBalance) void balance_kernel(BalanceArgs a) {
         float f[El::PER];
         El::widen(piece[u][i], f);
 #pragma unroll
-        for (int j = 0; j < El::PER; ++j) sum[i * El::PER + j] += exp_of(f[j] - lse[u]);
+        for (int j = 0; j < El::PER; ++j) acc[i * El::PER + j] += (double)exp_of(f[j] - lse[u]);
       }
     }
-#pragma unroll
-    for (int c = 0; c < C; ++c) acc[c] += (double)sum[c];
   }
   // the sums of a wave's tokens (lanes with the same columns), then of all units: as many at a time as LDS has room for
   auto same_columns = [](double v) {

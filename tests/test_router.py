@@ -577,3 +577,24 @@ def test_tokens_that_take_no_part_get_zeros_whatever_the_loss_is(dtype, of_all):
             d = B.lasnet_choose_experts_backward(l, lse, experts, weights, dweights=dw, counts=counts, dloss=torch.tensor(dloss).cuda(), flags=flags)
             assert (d[~mask.cuda()] == 0).all(), (tokens, E, k, dloss)
             assert not torch.isfinite(d[mask.cuda()].float()).all()
+
+
+# ---------------------------------------------------------------- what the header promises of sums and of tokens that take no part
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_sums_over_tokens_keep_what_32_bits_lose(dtype):
+    """A quarter (or one) of the tokens has p = 1, the others about 2^-25, less than half a unit of it: in 64 bits the small ones count, in 32 they would vanish next to a 1.  The bound: of the
+    small ones' own exponentials 16 u of them, and the rounding of share, u."""
+    for E, tokens in ((2, 256), (2, 4096), (60, 1024), (200, 512), (500, 64), (1500, 40), (4000, 16), (2, 40000)):
+        small = -17.25                                         # e^-17.25 = 1.08 2^-25, exact in bf16
+        for first in (tokens // 4, 1):
+            print("sums", E, tokens, first, dtype, flush=True)
+            l = torch.full((tokens, E), small, dtype=dtype, device="cuda")
+            l[:first] = 0.0
+            lse, experts = torch.zeros(tokens, device="cuda"), torch.zeros(tokens, 1, dtype=torch.int32, device="cuda")
+            _, share, loss = B.lasnet_balance(l, lse, experts)
+            low = (tokens - first) * math.exp(small) / tokens
+            want = first / tokens + low
+            assert (f64(share) - want).abs().max() <= U * want + 16 * U * low, (E, tokens, first, float(share[0]) - want)
+            assert abs(float(loss[0]) - E * want) <= 2 * U * E * want + 16 * U * E * low
