@@ -171,7 +171,7 @@ __global__ __launch_bounds__(512, 2) void block_stream_kernel(ProductArgs a) {
     w.i0 = ti * 256;
     return w;
   };
-  const int steps = a.nk <= KS ? 2 : (a.nk + KS - 1) / KS;    // (two at least, so that loads are never further ahead than the next tile)
+  const int steps = (a.nk + KS - 1) / KS;                     // (two at least: nk >= 256, so that loads are never further ahead than the next tile)
 
   // ---- loads ----
   const unsigned pitch_i = (unsigned)a.I.pitch, pitch_j = (unsigned)a.J.pitch, kb = (unsigned)a.nk;

@@ -264,14 +264,14 @@ __device__ __forceinline__ double join_all(double v, double* join) {
 }
 
 // Groups of L lanes take tokens in turn, U at once; a lane keeps its columns' sums.
-template <class T, int L, int N>
+template <class T, int L>
 __global__ __launch_bounds__(kBalance) void balance_kernel(BalanceArgs a) {
   using El = Elem<T>;
-  constexpr int G = kBalance / L, U = N == 1 ? 4 : 1, C = N * El::PER;
+  constexpr int G = kBalance / L, U = 4, C = El::PER;
   __shared__ double join[kBalance / 64];
   __shared__ double units[kBalanceUnits];                      // [P][E + 2]: the sums of P units (waves, or groups of more)
   __shared__ int hist[4096];
-  const int tid = (int)threadIdx.x, lane = tid % L, group = tid / L;
+  const int tid = (int)threadIdx.x, lane = tid % L, group = tid / L, c0 = lane * C;      // c0: the lane's first column
   if (blockIdx.x == 0 && tid == 0 && a.groups > 1) *a.ended = 0;
   for (int e = tid; e < a.E; e += kBalance) hist[e] = 0;
   __syncthreads();
@@ -290,29 +290,22 @@ __global__ __launch_bounds__(kBalance) void balance_kernel(BalanceArgs a) {
   const long long stride = (long long)gridDim.x * G;
   for (long long t0 = (long long)blockIdx.x * G + group; t0 < a.tokens; t0 += U * stride) {
     float lse[U];
-    uint4_t piece[U][N];
+    uint4_t piece[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const long long t = t0 + u * stride;
       lse[u] = t < a.tokens ? a.lse[t] : -INFINITY;
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const int c = (i * L + lane) * El::PER;
-        piece[u][i] = load_piece<T>(a.logits.data + t * a.logits.pitch + (size_t)c * El::BYTES, t < a.tokens ? a.E - c : 0);
-      }
+      piece[u] = load_piece<T>(a.logits.data + t * a.logits.pitch + (size_t)c0 * El::BYTES, t < a.tokens ? a.E - c0 : 0);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (lse[u] == -INFINITY) continue;
       squares += (double)lse[u] * lse[u];
       tokens += 1.;
+      float f[C];
+      El::widen(piece[u], f);
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        float f[El::PER];
-        El::widen(piece[u][i], f);
-#pragma unroll
-        for (int j = 0; j < El::PER; ++j) acc[i * El::PER + j] += (double)exp_of(f[j] - lse[u]);
-      }
+      for (int j = 0; j < C; ++j) acc[j] += (double)exp_of(f[j] - lse[u]);
     }
   }
   // the sums of a wave's tokens (lanes with the same columns), then of all units: as many at a time as LDS has room for
@@ -333,12 +326,8 @@ __global__ __launch_bounds__(kBalance) void balance_kernel(BalanceArgs a) {
     const int u = tid / UNIT - u0;
     if (u >= 0 && u < P && tid % UNIT < L) {
 #pragma unroll
-      for (int i = 0; i < N; ++i)
-#pragma unroll
-        for (int j = 0; j < El::PER; ++j) {
-          const int c = (i * L + lane) * El::PER + j;
-          if (c < a.E) units[u * all + c] = acc[i * El::PER + j];
-        }
+      for (int j = 0; j < C; ++j)
+        if (c0 + j < a.E) units[u * all + c0 + j] = acc[j];
       if (lane == 0) {
         units[u * all + a.E] = squares;
         units[u * all + a.E + 1] = tokens;
@@ -459,9 +448,9 @@ int balance_groups(long long tokens, int E) {
 }
 int join_groups(int E) { return (E + kJoinCols - 1) / kJoinCols; }
 
-template <class T, int L, int N>
+template <class T, int L>
 hipError_t go_balance(const BalanceArgs& a, hipStream_t st) {
-  balance_kernel<T, L, N><<<dim3((unsigned)a.groups), dim3(kBalance), 0, st>>>(a);
+  balance_kernel<T, L><<<dim3((unsigned)a.groups), dim3(kBalance), 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.groups == 1) return e;
   balance_join_kernel<<<dim3((unsigned)join_groups(a.E)), dim3(kBalance), 0, st>>>(a);
@@ -471,12 +460,12 @@ hipError_t go_balance(const BalanceArgs& a, hipStream_t st) {
 template <class T>
 hipError_t pick_balance(const BalanceArgs& a, hipStream_t st) {
   const int pieces = (a.E + Elem<T>::PER - 1) / Elem<T>::PER;
-  if (pieces <= 16) return go_balance<T, 16, 1>(a, st);
-  if (pieces <= 32) return go_balance<T, 32, 1>(a, st);
-  if (pieces <= 64) return go_balance<T, 64, 1>(a, st);
-  if (pieces <= 128) return go_balance<T, 128, 1>(a, st);
-  if (pieces <= 256) return go_balance<T, 256, 1>(a, st);
-  return go_balance<T, 1024, 1>(a, st);
+  if (pieces <= 16) return go_balance<T, 16>(a, st);
+  if (pieces <= 32) return go_balance<T, 32>(a, st);
+  if (pieces <= 64) return go_balance<T, 64>(a, st);
+  if (pieces <= 128) return go_balance<T, 128>(a, st);
+  if (pieces <= 256) return go_balance<T, 256>(a, st);
+  return go_balance<T, 1024>(a, st);
 }
 
 // ---- the gradient ----
