@@ -45,9 +45,10 @@ __device__ __forceinline__ void store_eight(unsigned char* p, int n, const unsig
     if (j < n) p[j] = (uint8_t)(q[j / 4] >> (8 * (j % 4)));
 }
 
-// Rows of 128 MB and more go past the caches: 16384 x 2048 bf16 to four experts each, 134 MB, 46 -> 34 us, and with the product that reads them next 217 -> 212 and 185 -> 186 us (64 and 16
-// experts, 1024 columns); of 67 MB 116 -> 122.
-bool rows_past(long long bytes) { return bytes >= 128 << 20; }
+// Large outputs go past the caches: by the time of this pass and the product that reads its rows next (six pairs of 2 to 8 copies, 1024 to 7168 columns, 16 and 64 experts, products of 256 to
+// 4096 columns; three sets of inputs in turn).  Against ordinary stores the pair takes, in the mean of the six and at the worst, at 32 MiB +7 % (+15), 64 +2 (+4), 96 0 (+5), 112 -0.5 (+1),
+// 128 -0.3 (+2), 144 -2 (0), 160 -2 (0), 320 -2 (-1).  The pass alone is as fast or faster from 64 MiB on (112 MiB: 4 copies of 2048 columns 40 -> 31 us, 2 of 4096 51 either way).
+bool rows_past(long long bytes) { return bytes >= 112 << 20; }
 
 template <class T, bool PAST>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantizeRowsArgs a) {

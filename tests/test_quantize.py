@@ -230,3 +230,26 @@ def test_offsets_past_32_bits():
     want = B.lasnet_quantize_matrices(W[4:, :, at:].contiguous(), transposed=True)
     for have, part in zip((got[0][4:, :, at:], got[1][4:, :, at // 128:], got[2][4:, at:], got[3][4:, at // 128:]), want):
         assert torch.equal(have.view(torch.uint8), part.view(torch.uint8))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("cols", [1024, 1001])
+def test_outputs_past_the_caches_and_in_them(cols, dtype):
+    """Outputs of 104 and 120 MiB, on both sides of where they go past the caches: the bits of the same rows in small calls, in place and laid out by expert."""
+    k, E, g = 4, 8, gen(cols)
+    for mib in (104, 120):
+        tokens = (mib << 20) // (cols * k)
+        x = torch.randn(tokens, cols, generator=g).to(dtype).cuda()
+        parts = [B.lasnet_quantize_rows(x[i:i + 4096]) for i in range(0, tokens, 4096)]
+        q, s = (torch.cat([p[j].view(torch.uint8) for p in parts]) for j in range(2))
+        offsets, _, position = B.lasnet_route(torch.randint(-1, E, (tokens, k), generator=g, dtype=torch.int32).cuda(), E)
+        out, scale = B.lasnet_quantize_rows(x, position=position, offsets=offsets)
+        at, sent = position.flatten().long(), position.flatten() >= 0
+        token = torch.arange(tokens, device="cuda").repeat_interleave(k)
+        assert torch.equal(out.view(torch.uint8)[at[sent]], q[token[sent]]) and torch.equal(scale.view(torch.uint8)[at[sent]], s[token[sent]]), mib
+        n = int(offsets[E])
+        assert n == int(sent.sum()) and not out.view(torch.uint8)[n:].any() and (scale.view(torch.uint8)[n:] == 127).all()
+        many = x.repeat(k, 1)
+        out, scale = B.lasnet_quantize_rows(many)
+        assert torch.equal(out.view(torch.uint8), q.repeat(k, 1)) and torch.equal(scale.view(torch.uint8), s.repeat(k, 1)), mib
