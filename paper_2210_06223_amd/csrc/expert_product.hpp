@@ -660,7 +660,8 @@ __device__ __forceinline__ void tile_product(const ProductArgs& a, unsigned char
   const unsigned slots = (unsigned)(size_t)(lds_byte*)product_lds + WK * STAGES * STAGE + (group * WI * WJ + wave) * STAGES * kScaleSlot;
   unsigned s_to = slots, s_at = slots;
   ScaleFeed<SCALES> ls;
-  if constexpr (SCALES != ROWS) ls.start(a, expert < a.E ? expert : 0, i0 + wi, j0 + wj, j_end, k0 / KS, lane);
+  // (a group that begins at the end: behind the last block, whose scale times nothing would be NaN were it infinite)
+  if constexpr (SCALES != ROWS) ls.start(a, expert < a.E ? expert : 0, i0 + wi, j0 + wj, j_end, (k0 + KS - 1) / KS, lane);
   // A step's loads, between the parts of `meanwhile` (which does what is due anyway, in LOADS parts).
   const unsigned to_i = wave * SI::SEGS * 1024, to_j = SI::BYTES + wave * SJ::SEGS * 1024;
   auto load = [&](auto meanwhile) {

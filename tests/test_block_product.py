@@ -381,3 +381,18 @@ def test_scales_in_32_bits_at_the_ends_of_their_range():
             want = k * v * v * w * 2.0 ** (sx - 127)
             assert math.isinf(w) or w == 0.0 or 2.0 ** -126 <= abs(want) < 2.0 ** 128
             assert (got.double() == float(torch.tensor(want).to(BF16))).all(), (R, n, k, v, sx, w, float(got[0, 0]), want)
+
+
+@pytest.mark.gpu
+def test_an_infinite_scale_is_no_nan_whatever_shares_the_reduction():
+    """A group of waves whose share of the reduction begins behind its end (five or nine steps in four shares, the last not whole) adds nothing: an infinite scale of the last block stays infinite."""
+    for R, E, n, k in ((200, 50, 256, 528), (200, 50, 256, 1040), (100, 4, 256, 1552), (32, 4, 2048, 2064), (200, 50, 256, 640), (300, 2, 512, 784), (64, 8, 255, 527), (9000, 1, 1536, 784)):
+        print("infinite scale", R, E, n, k, flush=True)
+        x, W = torch.ones(R, k, device="cuda").to(E4M3), torch.ones(E, n, k, device="cuda").to(E4M3)
+        offsets = (torch.arange(E + 1) * R // E).to(torch.int32).cuda()
+        kb, nb = (k + 127) // 128, (n + 127) // 128
+        scale, wscale = torch.full((R, kb), 127, dtype=torch.uint8, device="cuda"), torch.ones(E, nb, kb, device="cuda")
+        wscale[:, 0, -1] = -math.inf
+        got = B.lasnet_block_product(x, scale, offsets, W, wscale)
+        assert (got[:, :128] == -math.inf).all(), (R, E, n, k, got[0, 0])
+        assert (got[:, 128:].double() == float(torch.tensor(float(k)).to(BF16))).all()
