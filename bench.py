@@ -66,18 +66,29 @@ def parse_args():
     return ap.parse_args()
 
 
-def source_signature():
+# Sources of the operators on rows and of the binding: no part of the block's kernels, which include none of them.
+ROW_SOURCES = ("norm_rows.hip", "route_rows.hip", "router.hip", "quantize_rows.hip", "expert_product.hip", "expert_product.hpp", "block_product.hip", "row_ops.hpp", "row_api.hip",
+               "marshal.cpp")
+
+
+def source_signature(without=()):
     """sha1 over the kernel sources: a stored counter profile belongs to the build it was taken from."""
     h = hashlib.sha1()
     for f in sorted(glob.glob(os.path.join(ROOT, "paper_2210_06223_amd", "csrc", "*"))):
-        h.update(open(f, "rb").read())
+        if os.path.basename(f) not in without:
+            h.update(open(f, "rb").read())
     return h.hexdigest()[:16]
+
+
+def block_signature():
+    """The same over what the block's kernels are built from: a profile of them outlives a change to the operators on rows."""
+    return source_signature(ROW_SOURCES)
 
 
 def stored_traffic(workload, schedule):
     """HBM-side bytes per launch of the block's kernels from the rocprofv3 counter summary under profiles/
-    (a line `TRAFFIC_BYTES_PER_LAUNCH <schedule> <bytes> sources <sha>`); None if there is none or if the
-    kernel sources have changed since it was taken."""
+    (a line `TRAFFIC_BYTES_PER_LAUNCH <schedule> <bytes> sources <sha>`, block_signature()); None if there is none or if the
+    block's kernel sources have changed since it was taken."""
     path = os.path.join(ROOT, "profiles", "bench_%s_hbm_traffic_pmc.txt" % workload)
     if not os.path.exists(path):
         return None, None
@@ -85,7 +96,7 @@ def stored_traffic(workload, schedule):
         m = re.match(r"TRAFFIC_BYTES_PER_LAUNCH\s+(\w+)\s+(\d+)\s+sources\s+(\w+)", line.strip())
         if m and m.group(1) == schedule:
             rel = os.path.relpath(path, ROOT)
-            if m.group(3) != source_signature():
+            if m.group(3) != block_signature():
                 return None, rel + " (stale: kernel sources changed since it was taken)"
             return int(m.group(2)), rel
     return None, None

@@ -53,3 +53,39 @@ def test_committed_traffic_profiles_carry_a_machine_readable_line():
         txt = open(os.path.join(ROOT, "profiles", "bench_%s_hbm_traffic_pmc.txt" % w)).read()
         assert re.search(r"^TRAFFIC_BYTES_PER_LAUNCH (fused|tiled|stream) \d+ sources [0-9a-f]{16}$", txt, re.M), w
         assert "rocprofv3 --pmc FETCH_SIZE" in txt and "rocprofv3 --pmc WRITE_SIZE" in txt
+
+
+def _csrc_copy(tmp_path):
+    pkg = tmp_path / "paper_2210_06223_amd" / "csrc"
+    pkg.mkdir(parents=True)
+    src = os.path.join(ROOT, "paper_2210_06223_amd", "csrc")
+    for f in os.listdir(src):
+        (pkg / f).write_bytes(open(os.path.join(src, f), "rb").read())
+    return pkg
+
+
+def test_a_change_to_the_operators_on_rows_leaves_the_blocks_profile_valid(tmp_path, monkeypatch):
+    pkg = _csrc_copy(tmp_path)
+    monkeypatch.setattr(bench, "ROOT", str(tmp_path))
+    (tmp_path / "profiles").mkdir()
+    (tmp_path / "profiles" / "bench_w_hbm_traffic_pmc.txt").write_text("TRAFFIC_BYTES_PER_LAUNCH fused 7 sources %s\n" % bench.block_signature())
+    for f in bench.ROW_SOURCES:
+        with open(pkg / f, "ab") as fh:
+            fh.write(b"\n")
+    assert bench.stored_traffic("w", "fused")[0] == 7
+    for f in sorted(set(os.listdir(pkg)) - set(bench.ROW_SOURCES)):            # any other file's change, a new file's among them, makes it stale
+        before = (pkg / f).read_bytes()
+        (pkg / f).write_bytes(before + b"\n")
+        assert bench.stored_traffic("w", "fused")[0] is None, f
+        (pkg / f).write_bytes(before)
+    (pkg / "new.hpp").write_text("")
+    (pkg / "new.hip").write_text("x")
+    assert bench.stored_traffic("w", "fused")[0] is None
+
+
+def test_the_blocks_sources_include_none_of_the_rows():
+    src = os.path.join(ROOT, "paper_2210_06223_amd", "csrc")
+    assert set(bench.ROW_SOURCES) <= set(os.listdir(src))
+    for f in set(os.listdir(src)) - set(bench.ROW_SOURCES):
+        for name in re.findall(r'#\s*include\s*[<"]([^">]+)[">]', open(os.path.join(src, f)).read()):
+            assert os.path.basename(name) not in bench.ROW_SOURCES, (f, name)
