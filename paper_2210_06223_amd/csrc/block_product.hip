@@ -667,6 +667,7 @@ hipError_t go_blocks(ProductArgs a, hipStream_t st) {
       return go_block_stream<SCALES>(a, st);
     // 128 x 64 in three stages, two a CU, up to two rounds, else 128 x 128: 1000 rows of 8 experts, 1024 x 1024 8.1 (128 x 128 11.9), 1500 of 4, 1024 x 8192 30 (56); 4096 rows, 2048 x 1024
     // 21.0 (17.9), 4001 of 8, 1000 x 528 13.7 (11.7).  128 x 128 by eight waves: 2048 rows, 2048 x 4096 26.6 (28.8 and 32.7), 2048 of 16, 4096 x 2048 55 (51, 57).
+    // In two stages a step waits for the loads of that very step: 4224 rows, 1056 x 5024, a tile or two a CU, 50, 1.2 a step, of which its MFMAs take 0.2.  (More stages there: not tried.)
     if (tiles(128, 64) <= 512) return go_block_tile<SCALES, 128, 64, 2, 2, 3>(a, st);
     return go_block_tile<SCALES, 128, 128, 2, 2, 2>(a, st);
   }

@@ -4,7 +4,8 @@
 //
 // Bound by memory: everything is read once into registers, the maximum is a reduction over the lanes (the workgroup) that hold a block, and q is rounded once, to nearest
 // even; the division by a power of two moves the exponent alone.  16384 x 2048 bf16 to four experts each 36 us (203 MB, 5.6 TB/s), 4099 x 1001 fp32 6.3; 16 matrices 4096 x 2048 with their
-// transposes 95 us (537 MB, 5.6 TB/s), 8 of 1000 x 520 fp32 9.9: 320 workgroups, so one chain of loads, maximum, turn and stores.
+// transposes 95 us (537 MB, 5.6 TB/s), 8 of 1000 x 520 fp32 9.9: 320 workgroups, so one chain of loads, maximum, turn and stores; where a row ends inside a
+// thread's eight columns its loads go by elements, a branch and a wait each (1368 x 158 bf16, 22 workgroups, 9.2 us; 704 x 848, 42, 5.7).
 #include "row_ops.hpp"
 
 namespace lasnet {

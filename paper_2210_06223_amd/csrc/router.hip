@@ -33,7 +33,7 @@ struct ChooseArgs {
   bool all;
 };
 
-// The exchanges that sort C numbers: odd-even merges of sorted runs.
+// The exchanges that sort C numbers: Batcher's odd-even merge sort.
 template <int C>
 struct Exchanges {
   int n = 0, a[64] = {}, b[64] = {};
@@ -196,8 +196,9 @@ hipError_t pick_choose(const ChooseArgs& a, hipStream_t st) {
 // Two launches: workgroups sum runs of tokens, others join the sums of 64 columns each; the last of those to end (a counter tells, which the first launch cleared) adds up the loss
 // from their parts, in order.  One launch where one workgroup does.
 //
-// Bound by exp and by what a launch takes to begin and to join its waves: 32768 tokens of 256 experts fp32 (34 MB, out of the caches) 9.2 us and 5.9 for the join, 4099 of 60 bf16 6.7 and 4.7;
-// workgroups of 256 or 512 threads, or loads further ahead, took as long.
+// 32768 tokens of 256 experts fp32 (34 MB, 6.5 us from memory) 9.3 us and 5.9 for the join, 4099 of 60 bf16 6.7 and 4.7: what two launches, the second waiting for the first, take to begin, to read
+// and to join their waves.  Of both calls' 15.8 and 11.7 us the count of the slots, which comes before the first logits, is 0.4, the exponentials 0.4 and 0.3 (16384 of 1000 bf16: 3.4 of 20.6).
+// Workgroups of 256 or 512 threads, or loads further ahead, took as long.
 constexpr int kBalance = 1024;                                 // threads of a workgroup
 constexpr int kJoinCols = 64;                                  // columns of a workgroup of the second launch
 constexpr int kBalanceUnits = 4098;                            // doubles of LDS: one unit's of the most experts
