@@ -7,7 +7,7 @@
 //   fewer            64 x 16 to 128 x 128, a tile a workgroup, loads straight to LDS, the reduction shared by groups of waves where tiles are few
 //   few rows         fragments straight to registers
 //   odd rows         (not whole pieces of 16 bytes) words through registers; many tiles of them 128 x 128
-// 8192 x 8192 x 8192: 392 to 400 us with bytes as scales (2750 to 2800 TFLOP/s; a product of that size without scales reaches 3260 here), 460 to 463 in fp32 (2380).  A step reads 192 KiB from LDS and writes 64,
+// 8192 x 8192 x 8192: 392 to 400 us with bytes as scales (2750 to 2800 TFLOP/s; a product of that size without scales reaches 3260 here), 460 to 470 in fp32 (2340 to 2390).  A step reads 192 KiB from LDS and writes 64,
 // about what its MFMAs take, too; but four waves of 128 x 128, which read 128, took 441 (eight 411 then): one wave a SIMD waits for itself.  fp32 scales add four multiply-adds an MFMA to the vector unit.
 #include "expert_product.hpp"
 

@@ -34,7 +34,7 @@ struct ProductArgs {
 // 32 bits, m 2^e with m from 1 to 2: the matrix core applies 2^e, too (it adds the two exponents: neither scale by itself takes a sum out of fp32's range), and with m the sum of a block,
 // 128 products from 0, is added to the whole: an fma for each element and step, run while the matrix core multiplies.
 enum { ROWS = 0, POWERS = 1, FLOATS = 2 };
-// The byte and m of a scale in 32 bits.  (Below the normal numbers: 2^-127 and an m of less than 1.  Infinities and NaN are m's; their byte is a number, 255 being NaN.)
+// The byte and m of a scale in 32 bits.  (Below the normal numbers: 2^-127 and an m of less than 2.  Infinities and NaN are m's; their byte is a number, 255 being NaN.)
 __device__ __forceinline__ unsigned scale_power(unsigned w) {
   const unsigned e = w >> 23 & 255;
   return e < 254 ? e : 254;

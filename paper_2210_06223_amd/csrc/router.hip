@@ -196,7 +196,7 @@ hipError_t pick_choose(const ChooseArgs& a, hipStream_t st) {
 // Two launches: workgroups sum runs of tokens, others join the sums of 64 columns each; the last of those to end (a counter tells, which the first launch cleared) adds up the loss
 // from their parts, in order.  One launch where one workgroup does.
 //
-// 32768 tokens of 256 experts fp32 (34 MB, 6.5 us from memory) 9.3 us and 5.9 for the join, 4099 of 60 bf16 6.7 and 4.7: what two launches, the second waiting for the first, take to begin, to read
+// 32768 tokens of 256 experts fp32 (34 MB, 6.5 us from memory) 9.5 us and 6.0 for the join, 4099 of 60 bf16 6.6 and 4.7: what two launches, the second waiting for the first, take to begin, to read
 // and to join their waves.  Of both calls' 15.8 and 11.7 us the count of the slots, which comes before the first logits, is 0.4, the exponentials 0.4 and 0.3 (16384 of 1000 bf16: 3.4 of 20.6).
 // Workgroups of 256 or 512 threads, or loads further ahead, took as long.
 constexpr int kBalance = 1024;                                 // threads of a workgroup
@@ -485,7 +485,7 @@ struct ChooseGradArgs {
 
 // L lanes a token.  The weights' part lands on k of the E logits: each slot's lane writes its number to its expert's place in a row of LDS and reads it back, which tells whether any
 // expert is there twice (then the slots add one after the other); its part goes the same way, and the lanes that hold the logits read the row.
-// 32768 tokens of 256 experts fp32, 8 each, 15.4 us: memory (69 MB, partly in the caches) and exp; 4099 of 60 bf16, 5.3.
+// 32768 tokens of 256 experts fp32, 8 each, 15.6 us: memory (69 MB, 13.4 us); 4099 of 60 bf16, 5.4.
 template <class T, int L, int N>
 __global__ __launch_bounds__(256) void choose_grad_kernel(ChooseGradArgs a) {
   using El = Elem<T>;
